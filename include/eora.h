@@ -324,6 +324,87 @@ int eora_linear_sp24_group(const void* x, const eora_sp_member* members, int n_m
                            int M, int d_in, int r, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Between the linears of a decoder layer: the requests' own low-rank pairs beside a projection, and
+ * from the query, key and value projections to the input of the output projection, over a paged cache
+ * of keys and values.  Serving only: no gradients.  Arrays of indices, ranks, scalings and head scales
+ * need the alignment of their elements only; all other pointers are 16-byte aligned, as everywhere.
+ * The workspaces need no clearing; calls that may overlap in time need different ones.
+ * ------------------------------------------------------------------------------------------ */
+/* Many requests' adapters at once, beside a projection that they share (eora_linear_q() and its like have
+ * written `base`):
+ *      y[m] = base[m] + s_a * (x[m].A_a^T).B_a^T,      a = adapter_of_row[m]
+ * Only the pairs that rows select are read, so the pool may hold any number of them; eora_linear_q_multi() streams all of
+ * its pairs (ranks together <= 512) and needs no second launch.
+ * A_pool, B_pool: n_adapters slots, one after the other; slot a holds A_a (r x d_in) and B_a (d_out x r) as
+ *      eora_pack_factor_*() or eora_factors_store_*() write them (ab_bits 16, 4 or 3), its scales (ab_bits 4 and 3) lie
+ *      at slot a of A_scales and B_scales.
+ * ranks: n_adapters int32 or NULL (all r): only the first ranks[a] rows of A_a and columns of B_a are used, rounded up to
+ *      whole tiles of B (32; ab_bits 4 and 3: min(128, r)): a smaller pair is stored with zeros behind it.
+ *      Values above r count as r, values <= 0 as no adapter.
+ * scalings: n_adapters fp32 or NULL (all 1).
+ * adapter_of_row: M int32; values outside [0, n_adapters): y[m] = base[m].
+ * base: fp16 M x d_out, or NULL (zeros); may be y itself, and must not overlap it otherwise.
+ * t = x.A^T is held in fp32 (multiplied with B's tiles as two fp16 of 22 bits together, whatever its magnitude); the sum with
+ * base is rounded once.  Equal inputs give bit-equal outputs; a row's sums do not depend on the other rows'
+ * contents, but may be split differently when M changes.
+ * Constraints: M >= 0 (0: no-op), d_in % 128 == 0, d_out % 16 == 0, 1 <= n_adapters, r as for eora_linear_q (> 0).
+ * Errors: EORA_ERR_NULL / UNSUPPORTED (ab_bits) / SHAPE / ALIGN / WORKSPACE / LAUNCH. */
+size_t eora_adapters_workspace_bytes(int M, int d_in, int d_out, int r);      /* never shrinks as M or r grows; 0: invalid */
+int eora_linear_adapters(const void* x, const void* A_pool, const void* B_pool, const void* A_scales, const void* B_scales,
+                         const void* ranks, const void* scalings, const void* adapter_of_row, const void* base, void* y,
+                         int M, int d_in, int d_out, int r, int n_adapters, int ab_bits,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* The cache: n_pages pages of page_size tokens.  pages_k, pages_v: n_pages x n_kv_heads x page_size x head_dim, fp16
+ * (cache_bits 16) or e4m3 codes (cache_bits 8: OCP 8-bit floats, 4 exponent and 3 mantissa bits, no infinities) that stand
+ * for code * k_scale[head] (code * v_scale[head]), n_kv_heads fp32 each, NULL for cache_bits 16.  Token `slot` is
+ * token slot % page_size of page slot / page_size.
+ * Constraints: head_dim 64, 128 or 256, page_size % 16 == 0, n_pages * page_size < 2^31. */
+
+/* What new tokens pass through on their way to the cache, in one pass over q, k and v (fp16, M rows q_stride, k_stride and
+ * v_stride elements apart, heads of a row one after the other):
+ *   norm      each head of q and k: x * rsqrt(mean(x^2) + eps) * weight (head_dim fp16; q_weight / k_weight NULL: no norm)
+ *   rotation  the first rot_dim columns of each head of q and k, in pairs (i, i + rot_dim/2), or (2i, 2i+1) if interleaved:
+ *             (a, b) -> (a c - b s, b c + a s), (c, s) = rotations[position][i] (n_positions x rot_dim/2 x 2 fp32)
+ *   store     q to q_out (fp16, M x n_heads x head_dim; may be q where q_stride == n_heads * head_dim), k and v to token
+ *             slots[m] of the cache (cache_bits 8: the nearest e4m3 code of value / scale, saturating at 448; NaN is kept).
+ * positions: M int32 (NULL with rot_dim 0); outside [0, n_positions) the row's rotated columns are NaN.
+ * slots: M int64; outside [0, n_pages * page_size) (-1, say, for a padding row) the row's k and v are not stored.  Two rows
+ * with one slot: which is stored is undefined.
+ * fp32 arithmetic, one rounding at the store.  Constraints: M >= 0 (0: no-op), strides % 8 == 0, rot_dim % 16 == 0,
+ * 0 <= rot_dim <= head_dim, the cache's above.
+ * Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits) / SHAPE / VALUE (eps) / ALIGN / LAUNCH. */
+int eora_cache_append(const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
+                      const void* rotations, const void* positions, const void* slots, void* q_out,
+                      void* pages_k, void* pages_v, const void* k_scale, const void* v_scale,
+                      int M, int n_heads, int n_kv_heads, int head_dim, int q_stride, int k_stride, int v_stride,
+                      int rot_dim, int interleaved, int n_positions, float eps,
+                      int n_pages, int page_size, int cache_bits, void* stream);
+
+/* Attention of one token per request over its pages: for query head i of request b, kv head i / (n_heads / n_kv_heads),
+ *      p_t = softmax over t of (scale * q . k_t),   out = sum_t p_t v_t,   lse = log sum_t exp(scale * q . k_t)
+ * over tokens max(0, lengths[b] - window) <= t < lengths[b] (window 0: all).  Token t is token t % page_size of page
+ * page_table[b][t / page_size].
+ * q: fp16, B rows q_stride elements apart.  page_table: B x max_pages int32; entries outside [0, n_pages) are no page: their
+ * tokens are masked, as are scores of -inf.  lengths: B int32, taken as 0 .. max_pages * page_size.  A request without a
+ * token (length 0, or all masked) has out = 0 and lse = -inf.  What the cache holds in other places is
+ * never used, NaN included.
+ * out: fp16 B x n_heads x head_dim; lse: fp32 B x n_heads or NULL (natural logarithm: with it results over parts of a cache
+ * can be joined).  Several tokens of one request (a short prompt): one row each, with the lengths that each may see.
+ * Scores, sums and out are fp32 until the end; a weight is rounded to fp16 for its product with v.  Equal inputs give
+ * bit-equal outputs; how the tokens are split between workgroups, and so the last bits, depends on the lengths of all requests.
+ * workspace: eora_cache_attention_workspace_bytes() for the largest call (max_tokens = max_pages * page_size).
+ * Constraints: 0 <= B <= 8192 (0: no-op), n_heads % n_kv_heads == 0, q_stride % 8 == 0, max_pages >= 1,
+ * max_pages * page_size <= 2^30, B * (heads in blocks of 16) * max_tokens / 32 < 2e9, scale finite, the cache's above.
+ * Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits) / SHAPE / VALUE (scale) / ALIGN / WORKSPACE / LAUNCH. */
+size_t eora_cache_attention_workspace_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_tokens);      /* 0: invalid */
+int eora_cache_attention(const void* q, const void* pages_k, const void* pages_v, const void* k_scale, const void* v_scale,
+                         const void* page_table, const void* lengths, void* out, void* lse,
+                         int B, int n_heads, int n_kv_heads, int head_dim, int q_stride,
+                         int n_pages, int page_size, int cache_bits, int max_pages, int window, float scale,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Parity exports (integer / exact work, compared bit for bit against the CPU oracle).
  * ------------------------------------------------------------------------------------------ */
 /* codes_u8: d_out x d_in row-major; zeros_u8: d_out x d_in/group row-major. */

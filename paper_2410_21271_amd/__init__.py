@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     linear_q, linear_q_static, linear_q_group, linear_sp24, unpack_q, dequant_q, expand_sp24,
     sp24q4_tiles_bytes, sp24q4_meta_bytes, pack_sp24q4, linear_sp24q4, expand_sp24q4,
     factors_workspace_bytes, factors, linear_q_multi, factors_store_f16, factors_store_q, linear_sp24_group,
+    adapters_workspace_bytes, new_adapters_workspace, linear_adapters, cache_append,
+    cache_attention_workspace_bytes, new_attention_workspace, cache_attention,
 )

@@ -82,6 +82,11 @@ def _load():
         "eora_dequant_q": (ci, [vp, vp, vp, vp, ci, ci, ci, ci, vp]),
         "eora_expand_sp24": (ci, [vp, vp, vp, ci, ci, vp]),
         "eora_expand_sp24q4": (ci, [vp, vp, vp, ci, ci, vp]),
+        "eora_adapters_workspace_bytes": (sz, [ci] * 4),
+        "eora_linear_adapters": (ci, [vp] * 10 + [ci] * 6 + [vp, sz, vp]),
+        "eora_cache_append": (ci, [vp] * 13 + [ci] * 10 + [ctypes.c_float] + [ci] * 3 + [vp]),
+        "eora_cache_attention_workspace_bytes": (sz, [ci] * 5),
+        "eora_cache_attention": (ci, [vp] * 9 + [ci] * 10 + [ctypes.c_float, vp, sz, vp]),
         "eora_factors_workspace_bytes": (sz, [ci, ci, ci]),
         "eora_factors_store_f16": (ci, [vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp]),
         "eora_factors_store_q": (ci, [vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp]),
@@ -103,7 +108,8 @@ EXPORTS = ["eora_status_string", "eora_qweight_bytes", "eora_qzeros_bytes", "eor
            "eora_sp24q4_tiles_bytes", "eora_sp24q4_meta_bytes", "eora_pack_sp24q4", "eora_linear_sp24q4", "eora_expand_sp24q4",
            "eora_factors_workspace_bytes", "eora_factors", "eora_linear_q_multi", "eora_pack_factor_q3", "eora_factors_store_f16", "eora_factors_store_q", "eora_linear_sp24_group",
            "eora_debug_last_launch", "eora_debug_probe", "eora_linear_q_static", "eora_debug_set_resident_min_blocks", "eora_debug_set_factors_route",
-           "eora_debug_prefill_parts", "eora_debug_factors_near", "eora_debug_factors_parts", "eora_debug_prefill_plan", "eora_debug_last_prefill"]
+           "eora_debug_prefill_parts", "eora_debug_factors_near", "eora_debug_factors_parts", "eora_debug_prefill_plan", "eora_debug_last_prefill",
+           "eora_adapters_workspace_bytes", "eora_linear_adapters", "eora_cache_append", "eora_cache_attention_workspace_bytes", "eora_cache_attention"]
 
 
 def status_string(status):
@@ -391,6 +397,46 @@ def linear_q_multi(x, qweight, scales, qzeros, A_all, B_all, A_scales, B_scales,
     _check(lib.eora_linear_q_multi(_dp(x), _dp(qweight), _dp(scales), _dp(qzeros), _dp(A_all), _dp(B_all), _dp(A_scales),
                                    _dp(B_scales), _dp(adapter_of_row), _dp(y), M, d_in, d_out, r, n_adapters, w_bits, group,
                                    ab_bits, _dp(workspace), _nbytes(workspace), _stream()), "linear_q_multi")
+
+
+# ------------------------------------------------------------------ between the linears of a decoder layer
+def adapters_workspace_bytes(M, d_in, d_out, r):
+    return lib.eora_adapters_workspace_bytes(M, d_in, d_out, r)
+
+
+def new_adapters_workspace(M, d_in, d_out, r):
+    return _torch.empty(adapters_workspace_bytes(M, d_in, d_out, r), dtype=_torch.uint8, device="cuda")
+
+
+def linear_adapters(x, A_pool, B_pool, A_scales, B_scales, ranks, scalings, adapter_of_row, base, y, M, d_in, d_out, r,
+                    n_adapters, ab_bits, workspace):
+    _check(lib.eora_linear_adapters(_dp(x), _dp(A_pool), _dp(B_pool), _dp(A_scales), _dp(B_scales), _dp(ranks), _dp(scalings),
+                                    _dp(adapter_of_row), _dp(base), _dp(y), M, d_in, d_out, r, n_adapters, ab_bits,
+                                    _dp(workspace), _nbytes(workspace), _stream()), "linear_adapters")
+
+
+def cache_append(q, k, v, q_weight, k_weight, rotations, positions, slots, q_out, pages_k, pages_v, k_scale, v_scale, M, n_heads,
+                 n_kv_heads, head_dim, q_stride, k_stride, v_stride, rot_dim, interleaved, n_positions, eps, n_pages, page_size,
+                 cache_bits):
+    _check(lib.eora_cache_append(_dp(q), _dp(k), _dp(v), _dp(q_weight), _dp(k_weight), _dp(rotations), _dp(positions), _dp(slots),
+                                 _dp(q_out), _dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), M, n_heads, n_kv_heads, head_dim,
+                                 q_stride, k_stride, v_stride, rot_dim, int(bool(interleaved)), n_positions, eps, n_pages, page_size,
+                                 cache_bits, _stream()), "cache_append")
+
+
+def cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens):
+    return lib.eora_cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens)
+
+
+def new_attention_workspace(B, n_heads, n_kv_heads, head_dim, max_tokens):
+    return _torch.empty(cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens), dtype=_torch.uint8, device="cuda")
+
+
+def cache_attention(q, pages_k, pages_v, k_scale, v_scale, page_table, lengths, out, lse, B, n_heads, n_kv_heads, head_dim, q_stride,
+                    n_pages, page_size, cache_bits, max_pages, window, scale, workspace):
+    _check(lib.eora_cache_attention(_dp(q), _dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), _dp(page_table), _dp(lengths),
+                                    _dp(out), _dp(lse), B, n_heads, n_kv_heads, head_dim, q_stride, n_pages, page_size, cache_bits,
+                                    max_pages, window, scale, _dp(workspace), _nbytes(workspace), _stream()), "cache_attention")
 
 
 # ------------------------------------------------------------------ calibration (Alg. 1 steps 1-6)

@@ -1,6 +1,7 @@
 // C-ABI entry points: argument validation and the static choice of kernel.  No device memory is
 // allocated here and nothing is kept between calls.
 #include "eora.h"
+#include "checks.hpp"
 #include "kernels.hpp"
 
 #include <atomic>
@@ -37,23 +38,11 @@ static_assert(HDR_WORDS * 4 <= WS_HEADER, "header too small");
 
 int g_spin_limit = 1 << 22;                // bounded wait of the up-projection (about a second)
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
-
 int check_backbone_shape(int M, int d_in, int d_out, int r)
 {
     if (M < 0 || d_in <= 0 || d_out <= 0 || r < 0) return EORA_ERR_SHAPE;
     if (d_out % 16 || d_in % 128 || r > MAX_RANK) return EORA_ERR_SHAPE;
     return EORA_OK;
-}
-
-// Set EORA_VERBOSE=1 to have a refused launch explain itself on stderr.
-bool failed(hipError_t e, const char* what)
-{
-    if (e == hipSuccess) return false;
-    static const bool verbose = getenv("EORA_VERBOSE") != nullptr;      // read once per process
-    if (verbose) fprintf(stderr, "eora: %s: %s\n", what, hipGetErrorString(e));
-    return true;
 }
 
 int check_group(int d_in, int group)
