@@ -429,7 +429,7 @@ def cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens
 
 
 def new_attention_workspace(B, n_heads, n_kv_heads, head_dim, max_tokens):
-    return _torch.empty(cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens), dtype=_torch.uint8, device="cuda")
+    return _torch.zeros(cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens), dtype=_torch.uint8, device="cuda")
 
 
 def cache_attention(q, pages_k, pages_v, k_scale, v_scale, page_table, lengths, out, lse, B, n_heads, n_kv_heads, head_dim, q_stride,

@@ -12,12 +12,13 @@
 // has column dim / 16 * n + b as its row n, and a lane's operand is a transposition of 16-bit values in its own registers.  No LDS, no exchange between lanes in the loop.
 //
 // Softmax: m is a reference, common to the lanes of a head, not the exact maximum: it is raised, and O and the sum rescaled, only when a score
-// exceeds it by 2^8 or more (weights up to 256 are as exact in fp16 as weights up to 1).  Scores, sums and O are fp32; a weight is
+// exceeds it by 8 or more (weights up to 256 are as exact in fp16 as weights up to 1).  Scores, sums and O are fp32; a weight is
 // rounded to fp16 (nearest-even) for the product with V, the sum takes it unrounded.
 //
-// Split: the tiles of all (request, kv head) pairs in one row are cut into equal runs, one a workgroup, whatever the lengths are: a request of 100 000 tokens is spread
-// over the whole chip, and one of 10 costs a tile.  A run that ends inside a pair leaves its (m, sum, O) in the workspace and a second
-// kernel joins them, in the order of the tiles.
+// Split: all units (a request's kv head, or block of 16 of its query heads) in one row are cut into equal runs, whatever the lengths are: a request of 100 000
+// tokens is spread over the whole chip, and one of 10 costs a tile.  A workgroup whose run lies in one unit works on it together and adds up in
+// LDS; otherwise each wavefront has its own part of the run.  Results of parts of a unit go to the workspace past the caches; the
+// last one to arrive (one counter a unit) joins them, in the order of the tiles, whoever it is: the bits do not depend on the order of arrival.
 #include "serving.hpp"
 #include "tiles.hpp"
 
@@ -26,21 +27,23 @@ namespace {
 
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int TILE = 32;
-constexpr int MIN_RUN = 4;                     // tiles of a workgroup at least: one a wavefront
+constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs)
+constexpr int MIN_RUN = 16, FEW = 8;           // cost of a workgroup's run at least: requests of one length, of several
+constexpr int MAX_WG = 1024;
+constexpr int SLOTS = 2 * NW * MAX_WG;
+constexpr int COUNTERS = SLOTS + NW * MAX_WG;  // words before the partial results: a counter for each group of them, and for each unit
 constexpr float RAISE = 8.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+static_assert(START < NW, "the run of a workgroup holds a tile of each unit that it touches alone");
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tokens and tiles of a request
+// tokens and tiles of a request of n tokens
 struct Span {
     int lo, hi, first, tiles;
 };
-__device__ __forceinline__ Span span_of(const AttendArgs& a, int b)
+__device__ __forceinline__ Span span_of(const AttendArgs& a, int n)
 {
-    const int most = a.width * a.page;
-    int n = a.lengths[b];
-    n = n < 0 ? 0 : (n > most ? most : n);
     Span s;
     s.hi = n;
     s.lo = a.window > 0 && n > a.window ? n - a.window : 0;
@@ -49,15 +52,18 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int b)
     return s;
 }
 
-// ends[b + 1] = tiles of one kv head in requests 0 .. b; ends[0] = 0.  All threads of the workgroup.
-__device__ __forceinline__ void count_tiles(const AttendArgs& a, int* ends, int* scratch)
+// Requests, in LDS: plan[b].y: tokens; plan[b + 1].x: cost of one kv head in requests 0 .. b; plan[0].x = 0.  All threads of the workgroup.
+__device__ __forceinline__ void add_costs(const AttendArgs& a, int2* plan, int* scratch)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = a.width * a.page;
     int before = 0;
-    if (threadIdx.x == 0) ends[0] = 0;
+    if (threadIdx.x == 0) plan[0].x = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
-        int v = b < a.B ? span_of(a, b).tiles : 0;
+        int n = b < a.B ? a.lengths[b] : 0;
+        n = n < 0 ? 0 : (n > most ? most : n);
+        const int tiles = span_of(a, n).tiles;
+        int v = tiles > 0 ? tiles + START : 0;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int w = __shfl_up(v, o, 64);
@@ -72,144 +78,346 @@ __device__ __forceinline__ void count_tiles(const AttendArgs& a, int* ends, int*
             v += w < wave ? x : 0;
             sum += x;
         }
-        if (b < a.B) ends[b + 1] = before + v;
+        if (b < a.B) {
+            plan[b + 1].x = before + v;
+            plan[b].y = n;
+        }
         before += sum;
         __syncthreads();
     }
 }
 
-// The runs: workgroup g of `n` has tiles [cut(g), cut(g + 1)) of `total`
+// The units in one row, each START + tiles long (the first START places stand for what a unit costs beside its tiles), cut into equal runs:
+// wavefront w of n workgroups has [cut(w), cut(w + 1)).
 struct Runs {
-    unsigned total, n;
-    __device__ unsigned cut(unsigned g) const { return (unsigned)((unsigned long long)g * total / n); }
-    // the workgroup whose run holds a tile
-    __device__ unsigned owner(unsigned tile) const
+    unsigned total, n;                         // total >= 4 n, unless there is one unit of one or two tiles: no run is empty
+    __device__ unsigned cut(unsigned w) const { return (unsigned)((unsigned long long)w * total / (n * NW)); }
+    // the wavefront whose run holds a place
+    __device__ unsigned owner(unsigned at) const
     {
-        unsigned g = (unsigned)((unsigned long long)tile * n / total);
-        while (cut(g + 1) <= tile) ++g;
-        while (cut(g) > tile) --g;
-        return g;
+        unsigned w = (unsigned)((unsigned long long)at * (n * NW) / total);
+        while (cut(w + 1) <= at) ++w;
+        while (cut(w) > at) --w;
+        return w;
     }
 };
-__device__ __forceinline__ Runs runs_of(const AttendArgs& a, int tiles)
+__device__ __forceinline__ Runs runs_of(const AttendArgs& a, const int2* plan)
 {
+    const unsigned pairs = (unsigned)(a.kv * a.hblocks), units = (unsigned)a.B * pairs;
     Runs r;
-    r.total = (unsigned)tiles * (unsigned)(a.kv * a.hblocks);
-    const unsigned most = (r.total + MIN_RUN - 1) / MIN_RUN;
-    r.n = most < (unsigned)a.nwg ? most : (unsigned)a.nwg;
+    r.total = (unsigned)plan[a.B].x * pairs;
+    r.n = (unsigned)a.nwg;
+    if (units < r.n && (unsigned)plan[1].x * (unsigned)a.B == (unsigned)plan[a.B].x) {
+        // requests of one length: a whole number of workgroups a unit
+        const unsigned k = (r.total + units * MIN_RUN - 1) / (units * MIN_RUN), most = r.n / units;
+        r.n = units * (k > most ? most : (k < 1 ? 1 : k));
+    } else if (r.n > r.total / FEW + 1) {
+        r.n = r.total / FEW + 1;
+    }
+    if (r.n > r.total / NW) r.n = r.total / NW;
+    if (r.n == 0 && r.total) r.n = 1;
     return r;
 }
 
-// Where a unit (request b, kv head h, block hb of its query heads) begins: units of a request follow each other
 struct Unit {
-    int b, pair;                               // pair = h * hblocks + hb
-    unsigned begin, end;                       // tiles
+    int b, pair;                               // pair = kv head * hblocks + block of query heads
+    unsigned begin, end;                       // places
 };
-__device__ __forceinline__ Unit unit_at(const AttendArgs& a, const int* ends, unsigned tile)
+__device__ __forceinline__ Unit unit_at(const AttendArgs& a, const int2* plan, unsigned at)
 {
     const unsigned pairs = (unsigned)(a.kv * a.hblocks);
-    int lo = 0, hi = a.B;                      // ends[lo] * pairs <= tile < ends[hi] * pairs
+    int lo = 0, hi = a.B;                      // plan[lo].x * pairs <= at < plan[hi].x * pairs
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if ((unsigned)ends[mid] * pairs <= tile) lo = mid;
+        if ((unsigned)plan[mid].x * pairs <= at) lo = mid;
         else hi = mid;
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);
     Unit u;
     u.b = lo;
-    const unsigned begin = (unsigned)ends[lo] * pairs, tiles = (unsigned)(ends[lo + 1] - ends[lo]);
-    u.pair = (int)((tile - begin) / tiles);
-    u.begin = begin + (unsigned)u.pair * tiles;
-    u.end = u.begin + tiles;
+    const unsigned begin = (unsigned)__builtin_amdgcn_readfirstlane(plan[lo].x) * pairs;
+    const unsigned cost = (unsigned)__builtin_amdgcn_readfirstlane(plan[lo + 1].x - plan[lo].x);
+    u.pair = (int)((at - begin) / cost);
+    u.begin = begin + (unsigned)u.pair * cost;
+    u.end = u.begin + cost;
     return u;
 }
-
-// A partial result: rows x (m, sum), then, from a 16-byte boundary, rows x dim of O
-__host__ __device__ constexpr int part_head(int rows) { return (2 * rows + 3) & ~3; }
-__device__ __forceinline__ float* part_at(const AttendArgs& a, unsigned g, int second)
+// the one behind it (there is one)
+__device__ __forceinline__ Unit unit_after(const AttendArgs& a, const int2* plan, const Unit& u)
 {
-    return a.parts + ((size_t)2 * g + second) * (size_t)(part_head(a.rows) + a.rows * a.dim);
+    Unit v;
+    v.b = u.b;
+    v.pair = u.pair + 1;
+    v.begin = u.end;
+    v.end = u.end + (u.end - u.begin);
+    if (v.pair == a.kv * a.hblocks) {
+        v.pair = 0;
+        int cost;
+        do {
+            ++v.b;
+            cost = __builtin_amdgcn_readfirstlane(plan[v.b + 1].x - plan[v.b].x);
+        } while (cost == 0);
+        v.end = v.begin + (unsigned)cost;
+    }
+    return v;
 }
 
-// eight (keys) x W (columns) 16-bit values, one register row a key -> W registers rows of eight keys
-template <int W>
-__device__ __forceinline__ void transpose_keys(const uint32_t (&in)[8][W / 2], Frag (&out)[W])
+// Whether the wavefronts of a workgroup go through its run together, tile by tile in turn, with their results added up in LDS at each unit's end: in one unit,
+// or where units are long.  Otherwise each has a quarter of the run for itself (short units would leave three of four idle).
+constexpr unsigned LONG = 8;                   // tiles
+__device__ __forceinline__ bool together_at(const AttendArgs& a, const Runs& r, const int2* plan, unsigned g)
+{
+    const unsigned pairs = (unsigned)(a.kv * a.hblocks), at = r.cut(NW * g), to = r.cut(NW * g + NW);
+    const Unit first = unit_at(a, plan, at);
+    if (to <= first.end) return true;
+    const Unit last = unit_at(a, plan, to - 1);
+    return to - at >= LONG * ((unsigned)(last.b - first.b) * pairs + (unsigned)last.pair - (unsigned)first.pair + 1u);
+}
+
+// Who contributes to a unit that is cut: workgroups g0 .. g1, once where their wavefronts go together, else (g0, g1) their wavefronts
+// w0 .. w1 that have tiles of it.  Contribution c, in the order of the tiles, has its result in slot(c).
+struct Parts {
+    unsigned w0, w1, g0, g1, first, count;     // first: contributions of workgroup g0
+    bool whole0;
+};
+__device__ __forceinline__ Parts parts_of(const AttendArgs& a, const Runs& r, const int2* plan, const Unit& u)
+{
+    Parts p;
+    p.w0 = r.owner(u.begin + START);
+    p.w1 = r.owner(u.end - 1);
+    p.g0 = p.w0 / NW;
+    p.g1 = p.w1 / NW;
+    p.whole0 = together_at(a, r, plan, p.g0);
+    const bool whole1 = p.g1 > p.g0 && together_at(a, r, plan, p.g1);
+    const unsigned last = p.g1 > p.g0 ? NW * p.g0 + NW - 1 : p.w1;
+    p.first = p.whole0 ? 1 : last - p.w0 + 1;
+    p.count = p.first + (p.g1 > p.g0 ? p.g1 - p.g0 - 1 + (whole1 ? 1 : p.w1 - NW * p.g1 + 1) : 0);
+    return p;
+}
+// A wavefront may end one cut unit and begin another: two slots each, the second for the beginning of a unit.  A workgroup's common results have those of its
+// first wavefront.
+__device__ __forceinline__ unsigned slot_of(const Parts& p, unsigned c)
+{
+    if (c < p.first) return 2 * (p.whole0 ? NW * p.g0 : p.w0 + c) + (c == 0);
+    const unsigned d = c - p.first;
+    return d < p.g1 - p.g0 - 1 ? 2 * NW * (p.g0 + 1 + d) : 2 * (NW * p.g1 + (d - (p.g1 - p.g0 - 1)));
+}
+
+// A partial result: rows x (m, sum), then rows x dim of O.  Stores and loads go past the caches of an XCD, eight bytes each (relaxed, agent scope).
+__device__ __forceinline__ float* part_at(const AttendArgs& a, unsigned slot) { return a.parts + COUNTERS + (size_t)slot * ((size_t)a.rows * (a.dim + 2)); }
+__device__ __forceinline__ void put2(float* p, float x, float y)
+{
+    const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
+    __hip_atomic_store((unsigned long long*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* p)
+{
+    const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+// One lane, after its wavefront's (workgroup's) stores are through: whether this is the last of `count` to arrive.  The counter is left at zero.
+__device__ __forceinline__ bool arrive(const AttendArgs& a, unsigned counter, unsigned count)
+{
+    unsigned* at = (unsigned*)a.parts + counter;
+    const bool last = __hip_atomic_fetch_add(at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == count;
+    if (last) __hip_atomic_store(at, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return last;
+}
+__device__ __forceinline__ void stores_through() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// exp2(m - to), 0 for no tokens
+__device__ __forceinline__ float factor(float m, float to) { return m == -INFINITY ? 0.f : exp2_(m - to); }
+
+// where a query head's results go
+__device__ __forceinline__ size_t head_at(const AttendArgs& a, const Unit& u, int row)
+{
+    const int h = u.pair / a.hblocks;
+    return (size_t)u.b * a.heads + h * a.group + 16 * (u.pair - h * a.hblocks) + row;
+}
+__device__ __forceinline__ float lse_of(float m, float sum) { return LN2 * (m + __log2f(sum)); }
+
+// Contributions c0, c0 + step, .. (`count` of them) of a unit, joined by one wavefront (wave 0 of 1) or by the workgroup (its wavefronts take
+// 64 float2 of the rows x dim of O in turn): the unit's result, or, for a group of contributions, a contribution in the place of the first.
+template <int DIM, int CH, int BATCH>          // CH times 64 float2 and BATCH contributions are requested at a time
+__device__ __forceinline__ void join(const AttendArgs& a, const Parts& p, const Unit& u, unsigned c0, unsigned step, unsigned count, int nrows, int wave, int waves, bool final, float vs)
+{
+    const int lane = threadIdx.x & 63, words = nrows * (DIM / 2);
+    float m0 = -INFINITY, l0 = 0.f;
+    for (int e0 = 64 * wave; e0 < words; e0 += 64 * waves * CH) {
+        int e[CH], row[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = e0 + 64 * waves * i + lane;
+            e[i] = at < words ? at : words - 1;
+            row[i] = e[i] / (DIM / 2);
+        }
+        float m = -INFINITY, l = 0.f;          // of row `lane`
+        float2 acc[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) acc[i] = make_float2(0.f, 0.f);
+#pragma clang loop unroll(disable)
+        for (unsigned c = 0; c < count; c += BATCH) {
+            float2 ml[BATCH], x[BATCH][CH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {  // (beyond the last: the last again, of no weight)
+                const float* src = part_at(a, slot_of(p, c0 + step * (c + k < count ? c + k : count - 1)));
+                ml[k] = get2(src + 2 * (lane < nrows ? lane : 0));
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[k][i] = get2(src + 2 * a.rows + 2 * e[i]);
+            }
+            float up = m;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) up = fmaxf(up, ml[k].x);
+            const float f = factor(m, up);
+            l = m == -INFINITY ? l : l * f;
+            m = up;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const float g = __shfl(f, row[i], 64);
+                acc[i].x *= g;
+                acc[i].y *= g;
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (c + k >= count) break;
+                const float fk = factor(ml[k].x, up);
+                l += ml[k].x == -INFINITY ? ml[k].y : ml[k].y * fk;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float gk = __shfl(fk, row[i], 64);
+                    acc[i].x += x[k][i].x * gk;
+                    acc[i].y += x[k][i].y * gk;
+                }
+            }
+        }
+        if (e0 == 0 && final && lane < nrows && a.lse) a.lse[head_at(a, u, lane)] = lse_of(m, l);
+        m0 = m;
+        l0 = l;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const bool there = e0 + 64 * waves * i + lane < words;
+            if (final) {
+                const float sum = __shfl(l, row[i], 64), by = vs / sum;
+                const h2 y = {(_Float16)(sum == 0.f ? 0.f : acc[i].x * by), (_Float16)(sum == 0.f ? 0.f : acc[i].y * by)};
+                if (there) *(h2*)(a.out + head_at(a, u, 0) * DIM + 2 * e[i]) = y;
+            } else if (there) {
+                put2(part_at(a, slot_of(p, c0)) + 2 * a.rows + 2 * e[i], acc[i].x, acc[i].y);
+            }
+        }
+    }
+    if (!final) {
+        if (waves > 1) __syncthreads();        // all have read the first contribution's (m, sum)
+        if (wave == 0 && lane < nrows) put2(part_at(a, slot_of(p, c0)) + 2 * lane, m0, l0);
+    }
+}
+
+// A wavefront (the workgroup) has stored contribution c: the last of a group of contributions to arrive joins the group, the last group's the unit.
+// Groups of the square root of their number: one workgroup would take 25 us for the 128 contributions of one of eight heads of a long request.
+template <int DIM, int CH, int BATCH>
+__device__ __forceinline__ void finish(const AttendArgs& a, const Parts& p, const Unit& u, unsigned c, int nrows, int wave, int waves, int* scratch, float vs)
+{
+    const unsigned size = p.count <= 16 ? p.count : (unsigned)ceilf(sqrtf((float)p.count)), groups = (p.count + size - 1) / size;
+    const unsigned k = c / size, here = (k + 1) * size <= p.count ? size : p.count - k * size;
+    auto last_of = [&](unsigned counter, unsigned count) {
+        stores_through();
+        bool last = false;
+        if (waves == 1) {
+            if ((threadIdx.x & 63) == 0) last = arrive(a, counter, count);
+            return (bool)__builtin_amdgcn_readfirstlane(last);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) scratch[0] = arrive(a, counter, count);
+        __syncthreads();
+        return scratch[0] != 0;
+    };
+    if (!last_of(slot_of(p, k * size), here)) return;
+    join<DIM, CH, BATCH>(a, p, u, k * size, 1, here, nrows, wave, waves, groups == 1, vs);
+    if (groups == 1 || !last_of(SLOTS + p.w0, groups)) return;         // (a wavefront begins one cut unit at most)
+    join<DIM, CH, BATCH>(a, p, u, 0, size, groups, nrows, wave, waves, true, vs);
+}
+
+// eight (keys) x two columns of 16-bit values, one word a key -> two operands of eight keys
+__device__ __forceinline__ void transpose_keys(const uint32_t (&in)[8], Frag& a, Frag& b)
 {
 #pragma unroll
-    for (int c = 0; c < W / 2; ++c)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            out[2 * c].u[k] = __builtin_amdgcn_perm(in[2 * k + 1][c], in[2 * k][c], 0x05040100u);
-            out[2 * c + 1].u[k] = __builtin_amdgcn_perm(in[2 * k + 1][c], in[2 * k][c], 0x07060302u);
-        }
+    for (int k = 0; k < 4; ++k) {
+        a.u[k] = __builtin_amdgcn_perm(in[2 * k + 1], in[2 * k], 0x05040100u);
+        b.u[k] = __builtin_amdgcn_perm(in[2 * k + 1], in[2 * k], 0x07060302u);
+    }
 }
 
 // two e4m3 codes -> two fp16, exactly (scale 1)
 template <bool HIGH>
 __device__ __forceinline__ uint32_t two_codes(uint32_t w)
 {
-    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-    const half2v v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH);
-    return __builtin_bit_cast(uint32_t, v);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
+// Tiles of 8 KiB two at a time in registers, larger ones one: eight wavefronts a compute unit have 64 to 128 KiB in flight.
 template <int DIM, int BITS>
-__global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a)
+constexpr int tiles_ahead() { return 1; }
+
+// wavefronts a SIMD: what the registers of an instantiation leave room for
+template <int DIM, int BITS>
+constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
+
+template <int DIM, int BITS>
+__global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kernel(const AttendArgs a)
 {
     constexpr int NT = DIM / 32;               // k-steps of the first product
     constexpr int W = DIM / 16;                // columns of V a lane holds, blocks of O^T
     constexpr int BYTES = BITS / 8;
     constexpr int KL = BITS == 16 ? NT : DIM / 64;        // 16-byte loads of a key row a lane makes
     constexpr int VW = W * BYTES / 4;          // words of a value row a lane holds
-    static_assert(DIM % 64 == 0, "");
     typedef uint32_t words __attribute__((ext_vector_type(VW < 4 ? VW : 4)));
     constexpr int VL = VW < 4 ? 1 : VW / 4;    // loads of a value row
+    constexpr int AHEAD = tiles_ahead<DIM, BITS>();
 
     __shared__ int scratch[NW];
     __shared__ float red_m[NW][16], red_l[NW][16];
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* red_o = (float*)smem;               // NW x rows x DIM
-    int* ends = (int*)(red_o + NW * a.rows * DIM);
+    int2* plan = (int2*)(red_o + NW * a.rows * DIM);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    count_tiles(a, ends, scratch);
-    __syncthreads();
-    const Runs runs = runs_of(a, ends[a.B]);
     const unsigned g = blockIdx.x;
+    add_costs(a, plan, scratch);
+    __syncthreads();
+    // requests without a token have no unit
+    for (int b = (int)g; b < a.B; b += (int)gridDim.x) {
+        if (plan[b + 1].x != plan[b].x) continue;
+        for (int e = threadIdx.x; e < a.heads * (DIM / 8); e += THREADS) *(u4*)(a.out + (size_t)b * a.heads * DIM + 8 * e) = u4{0, 0, 0, 0};
+        if (a.lse)
+            for (int e = threadIdx.x; e < a.heads; e += THREADS) a.lse[(size_t)b * a.heads + e] = -INFINITY;
+    }
+    const Runs runs = runs_of(a, plan);
     if (g >= runs.n) return;
-    const unsigned run_end = runs.cut(g + 1);
 
-    for (unsigned at = runs.cut(g); at < run_end;) {
-        const Unit u = unit_at(a, ends, at);
-        const unsigned stop = run_end < u.end ? run_end : u.end;
-        const Span span = span_of(a, u.b);
+    const bool together = together_at(a, runs, plan, g);
+    unsigned at = runs.cut(NW * g + (together ? 0 : wave));
+    const unsigned stop_at = runs.cut(NW * g + (together ? NW : wave + 1));
+
+    Unit u = unit_at(a, plan, at), then = u;
+    for (; at < stop_at; u = then) {
+        const unsigned stop = stop_at < u.end ? stop_at : u.end;
+        // tiles of the unit
+        const int r0 = at > u.begin + START ? (int)(at - u.begin) - START : 0, r1 = (int)(stop - u.begin) - START;
+        at = stop;
+        if (at < stop_at) then = unit_after(a, plan, u);
+        if (r1 <= r0) continue;
+        const bool full = r0 == 0 && stop == u.end;
+        const Span span = span_of(a, __builtin_amdgcn_readfirstlane(plan[u.b].y));
         const int h = u.pair / a.hblocks, hb = u.pair - h * a.hblocks;
         const int nrows = a.group - 16 * hb < a.rows ? a.group - 16 * hb : a.rows;
-        const int t0 = span.first + (int)(at - u.begin), t1 = span.first + (int)(stop - u.begin);
         const int* table = a.table + (size_t)u.b * a.width;
+        const int t0 = span.first + r0 + (together ? wave : 0), step = together ? NW : 1;
+        const int mine = together ? (r1 - r0 > wave ? (r1 - r0 - wave + NW - 1) / NW : 0) : r1 - r0;
 
-        // q: k-slots of lane (n, j) as the key's loads have them; heads that are not there are zero columns
-        Frag qf[NT];
-        {
-            const _Float16* q = a.q + (size_t)u.b * a.q_stride + (size_t)(h * a.group + 16 * hb + (n < nrows ? n : 0)) * DIM;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int col = BITS == 16 ? 32 * t + 8 * j : 64 * (t / 2) + 16 * j + 8 * (t % 2);
-                const u4 w = *(const u4*)(q + col);
-                qf[t].q = n < nrows ? w : u4{0, 0, 0, 0};
-            }
-        }
-        const float by = a.scale * LOG2E * (BITS == 8 ? a.k_scale[h] : 1.f);
-
-        f4 O[W];
-#pragma unroll
-        for (int b = 0; b < W; ++b) O[b] = f4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
-
-        // Pages of this wavefront's next 32 tiles: lane i has the row of tile i's first half, lane 32 + i of its second (-1: no page)
-        const int mine = t1 - t0 > wave ? (t1 - t0 - wave + NW - 1) / NW : 0;
+        // Pages of the next 32 tiles: lane i has the row of tile i's first half, lane 32 + i of its second (-1: no page)
         long long rows_of = -1;
         auto look = [&](int i0) {
-            const int key = (t0 + wave + NW * (i0 + (lane & 31))) * TILE + 16 * (lane >> 5);
+            const int key = (t0 + step * (i0 + (lane & 31))) * TILE + 16 * (lane >> 5);
             rows_of = -1;
             if (i0 + (lane & 31) < mine && key < span.hi) {
                 const int p = key / a.page, page = table[p];
@@ -221,64 +429,91 @@ __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a)
             const unsigned lo = __builtin_amdgcn_readlane((unsigned)rows_of, from), hi = __builtin_amdgcn_readlane((unsigned)(rows_of >> 32), from);
             return (long long)(((unsigned long long)hi << 32) | lo);
         };
-        u4 kw[2][KL];
-        words vw[8][VL];
-        auto load_k = [&](const long long (&row)[2]) {
+        // AHEAD tiles in registers.  A tile's registers are requested anew (for the tile AHEAD further on) as soon as it has no more use for them; behind the
+        // last tile the requests go on, all lanes to one place: a request behind a branch would make every wait one for all requests.
+        struct Held {
+            u4 k[2][KL];
+            words v[8][VL];
+            long long row[2];
+        } held[AHEAD];
+        auto find = [&](int i, long long (&row)[2]) {
+            row[0] = half_row(i, 0);
+            row[1] = half_row(i, 1);
+        };
+        const unsigned k_at = (unsigned)(n * DIM * BYTES + 16 * j), v_at = (unsigned)(4 * j * DIM * BYTES + n * W * BYTES);
+        auto load_k = [&](Held& t, const long long (&row)[2], unsigned all) {
+            const unsigned off = k_at & all;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const char* base = (const char*)a.pages_k + (size_t)(row[s] < 0 ? 0 : row[s]) * (DIM * BYTES);
 #pragma unroll
-                for (int t = 0; t < KL; ++t) kw[s][t] = *(const u4*)(base + (unsigned)(n * DIM * BYTES + 64 * t + 16 * j));
+                for (int e = 0; e < KL; ++e) t.k[s][e] = *(const u4*)(base + off + 64 * e);
             }
         };
-        auto load_v = [&](const long long (&row)[2]) {
+        auto load_v = [&](Held& t, const long long (&row)[2], unsigned all) {
+            const unsigned off = v_at & all;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const char* base = (const char*)a.pages_v + (size_t)(row[s] < 0 ? 0 : row[s]) * (DIM * BYTES);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int v = 0; v < VL; ++v) vw[4 * s + i][v] = *(const words*)(base + (unsigned)((4 * j + i) * DIM * BYTES + n * W * BYTES + 16 * v));
+                    for (int v = 0; v < VL; ++v) t.v[4 * s + i][v] = *(const words*)(base + off + i * DIM * BYTES + 16 * v);
             }
         };
-        long long row[2], next[2];
-        if (mine > 0) {
-            look(0);
-            row[0] = half_row(0, 0);
-            row[1] = half_row(0, 1);
-            load_k(row);
-            load_v(row);
+        if (mine > 0) look(0);
+        // q: k-slots of lane (n, j) as the key's loads have them; heads that are not there are zero columns
+        Frag qf[NT];
+        {
+            const _Float16* q = a.q + (size_t)u.b * a.q_stride + (size_t)(h * a.group + 16 * hb + (n < nrows ? n : 0)) * DIM;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int col = BITS == 16 ? 32 * t + 8 * j : 64 * (t / 2) + 16 * j + 8 * (t % 2);
+                const u4 w = *(const u4*)(q + col);
+                qf[t].q = n < nrows ? w : u4{0, 0, 0, 0};
+            }
         }
-        for (int i = 0; i < mine; ++i) {
+        const float by = a.scale * LOG2E * (BITS == 8 ? a.k_scale[h] : 1.f), vs = BITS == 8 ? a.v_scale[h] : 1.f;
+        f4 O[W];
+#pragma unroll
+        for (int b = 0; b < W; ++b) O[b] = f4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        if (mine > 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                find(i, held[i].row);
+                load_k(held[i], held[i].row, i < mine ? ~0u : 0u);
+                load_v(held[i], held[i].row, i < mine ? ~0u : 0u);
+            }
+        }
+        auto tile = [&](int i, Held& t) {
             // scores
             f4 S[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 S[s] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                for (int e = 0; e < NT; ++e) {
                     Frag k;
                     if constexpr (BITS == 16) {
-                        k.q = kw[s][t];
+                        k.q = t.k[s][e];
                     } else {
-                        const uint32_t w0 = kw[s][t / 2][2 * (t % 2)], w1 = kw[s][t / 2][2 * (t % 2) + 1];
+                        const uint32_t w0 = t.k[s][e / 2][2 * (e % 2)], w1 = t.k[s][e / 2][2 * (e % 2) + 1];
                         k.u[0] = two_codes<false>(w0);
                         k.u[1] = two_codes<true>(w0);
                         k.u[2] = two_codes<false>(w1);
                         k.u[3] = two_codes<true>(w1);
                     }
-                    S[s] = mfma16(k.v, qf[t].v, S[s]);
+                    S[s] = mfma16(k.v, qf[e].v, S[s]);
                 }
             }
-            const bool more = i + 1 < mine;
-            if (more) {
-                if (((i + 1) & 31) == 0) look(i + 1);
-                next[0] = half_row(i + 1, 0);
-                next[1] = half_row(i + 1, 1);
-                load_k(next);
-            }
-            const int key0 = (t0 + wave + NW * i) * TILE;
-            const bool whole = key0 >= span.lo && key0 + TILE <= span.hi && row[0] >= 0 && row[1] >= 0;
+            if (((i + AHEAD) & 31) == 0) look(i + AHEAD);
+            const unsigned all = i + AHEAD < mine ? ~0u : 0u;
+            long long next[2];
+            find(i + AHEAD, next);
+            load_k(t, next, all);
+            const int key0 = (t0 + step * i) * TILE;
+            const bool whole = key0 >= span.lo && key0 + TILE <= span.hi && t.row[0] >= 0 && t.row[1] >= 0;
             float p[8];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -291,7 +526,7 @@ __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = key0 + 16 * s + 4 * j + e;
-                        if (key < span.lo || key >= span.hi || row[s] < 0) {
+                        if (key < span.lo || key >= span.hi || t.row[s] < 0) {
                             out |= 1u << (4 * s + e);
                             p[4 * s + e] = -INFINITY;
                         }
@@ -317,178 +552,124 @@ __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a)
                 l += p[e];
                 pf.v[e] = (_Float16)p[e];
             }
-            // values: rows of eight keys
-            uint32_t raw[8][W / 2];
+            // values: two columns of eight keys at a time
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int c = 0; c < W / 2; ++c) {
+                uint32_t raw[8];
 #pragma unroll
-                for (int c = 0; c < VW; ++c) {
-                    const uint32_t w = vw[e][c / 4][VW < 4 ? c : c % 4];
-                    if constexpr (BITS == 16) {
-                        raw[e][c] = w;
-                    } else {
-                        raw[e][2 * c] = two_codes<false>(w);
-                        raw[e][2 * c + 1] = two_codes<true>(w);
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const int at_word = BITS == 16 ? c : c / 2;
+                    const uint32_t w = t.v[e][at_word / 4][VW < 4 ? at_word : at_word % 4];
+                    if constexpr (BITS == 16) raw[e] = w;
+                    else raw[e] = c % 2 ? two_codes<true>(w) : two_codes<false>(w);
+                    // what lies in places that do not count may be anything, NaN among it, and 0 NaN is NaN
+                    if (!whole) raw[e] = out >> e & 1 ? 0u : raw[e];
                 }
-                // what lies in places that do not count may be anything, NaN among it, and 0 NaN is NaN
-                if (!whole) {
-#pragma unroll
-                    for (int c = 0; c < W / 2; ++c) raw[e][c] = out >> e & 1 ? 0u : raw[e][c];
-                }
+                Frag v0, v1;
+                transpose_keys(raw, v0, v1);
+                O[2 * c] = mfma16(v0.v, pf.v, O[2 * c]);
+                O[2 * c + 1] = mfma16(v1.v, pf.v, O[2 * c + 1]);
             }
-            if (more) {
-                load_v(next);
-                row[0] = next[0];
-                row[1] = next[1];
+            load_v(t, next, all);
+            t.row[0] = next[0];
+            t.row[1] = next[1];
+        };
+        for (int i = 0; i < mine; i += AHEAD) {
+            tile(i, held[0]);
+            if constexpr (AHEAD == 2) {
+                if (i + 1 >= mine) break;
+                tile(i + 1, held[1]);
             }
-            Frag vf[W];
-            transpose_keys<W>(raw, vf);
-#pragma unroll
-            for (int b = 0; b < W; ++b) O[b] = mfma16(vf[b].v, pf.v, O[b]);
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
 
-        // the four wavefronts' results
+        if (!together) {
+            // This wavefront's result: all of the unit, or a part
+            const float f = l == 0.f ? 0.f : vs / l;
+            if (full) {
+                if (n < nrows) {
+                    const size_t head = head_at(a, u, n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        _Float16 y[W];
+#pragma unroll
+                        for (int b = 0; b < W; ++b) y[b] = (_Float16)(l == 0.f ? 0.f : O[b][i] * f);
+                        __builtin_memcpy((_Float16*)__builtin_assume_aligned(a.out + head * DIM + W * (4 * j + i), 2 * W), y, 2 * W);
+                    }
+                    if (j == 0 && a.lse) a.lse[head] = lse_of(m, l);
+                }
+                continue;
+            }
+            const Parts parts = parts_of(a, runs, plan, u);
+            float* part = part_at(a, 2 * (NW * g + wave) + (r0 == 0));
+            if (n < nrows) {
+                if (j == 0) put2(part + 2 * n, m, l);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int b = 0; b < W; b += 2) put2(part + 2 * a.rows + n * DIM + W * (4 * j + i) + b, O[b][i], O[b + 1][i]);
+            }
+            const unsigned w = NW * g + wave;
+            finish<DIM, 4, 4>(a, parts, u, g == parts.g0 ? w - parts.w0 : parts.first + (parts.g1 - parts.g0 - 1) + (w - NW * parts.g1), nrows, 0, 1, scratch, vs);
+            continue;
+        }
+
+        // The workgroup's results, added up
+        __syncthreads();                       // (the last unit's have been read)
         if (lane < 16) {
             red_m[wave][lane] = m;
             red_l[wave][lane] = l;
         }
         __syncthreads();
-        float M = red_m[0][n];
+        {
+            float M = red_m[0][n];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) M = fmaxf(M, red_m[w][n]);
-        const float mine_f = m == -INFINITY ? 0.f : exp2_(m - M);
-        if (n < nrows) {
-            float* o = red_o + ((size_t)wave * a.rows + n) * DIM;
+            for (int w = 1; w < NW; ++w) M = fmaxf(M, red_m[w][n]);
+            const float f = factor(m, M);
+            if (n < nrows) {
+                float* o = red_o + ((size_t)wave * a.rows + n) * DIM;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int b = 0; b < W; b += 4)
-                    *(f4*)(o + W * (4 * j + i) + b) = f4{O[b][i] * mine_f, O[b + 1][i] * mine_f, O[b + 2][i] * mine_f, O[b + 3][i] * mine_f};
+                    for (int b = 0; b < W; b += 4)
+                        *(f4*)(o + W * (4 * j + i) + b) = f4{O[b][i] * f, O[b + 1][i] * f, O[b + 2][i] * f, O[b + 3][i] * f};
+            }
         }
         __syncthreads();
-        const bool full = at == u.begin && stop == u.end;
-        const float vs = BITS == 8 ? a.v_scale[h] : 1.f;
-        float* part = part_at(a, g, at == u.begin);
-        for (int e = threadIdx.x; e < nrows * (DIM / 8); e += THREADS) {
-            const int r = e / (DIM / 8), c = 8 * (e % (DIM / 8));
-            float Mr = red_m[0][r];
+        float* part = part_at(a, 2 * NW * g + (r0 == 0));
+        for (int e = threadIdx.x; e < nrows * (DIM / 4); e += THREADS) {
+            const int r = e / (DIM / 4), c = 4 * (e % (DIM / 4));
+            float M = red_m[0][r];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) Mr = fmaxf(Mr, red_m[w][r]);
+            for (int w = 1; w < NW; ++w) M = fmaxf(M, red_m[w][r]);
             float sum = 0.f;
-            f4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+            f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float mw = red_m[w][r];
-                sum += mw == -INFINITY ? red_l[w][r] : red_l[w][r] * exp2_(mw - Mr);
-                const float* o = red_o + ((size_t)w * a.rows + r) * DIM + c;
-                x += *(const f4*)o;
-                y += *(const f4*)(o + 4);
+                sum += mw == -INFINITY ? red_l[w][r] : red_l[w][r] * exp2_(mw - M);
+                x += *(const f4*)(red_o + ((size_t)w * a.rows + r) * DIM + c);
             }
             if (full) {
-                const size_t head = (size_t)u.b * a.heads + h * a.group + 16 * hb + r;
+                const size_t head = head_at(a, u, r);
                 const float f = vs / sum;
-                h8 v;
+                typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+                h4 v;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = (_Float16)(sum == 0.f ? 0.f : x[q] * f);         // (every token masked: as without tokens)
-                    v[4 + q] = (_Float16)(sum == 0.f ? 0.f : y[q] * f);
-                }
-                *(h8*)(a.out + head * DIM + c) = v;
-                if (c == 0 && a.lse) a.lse[head] = LN2 * (Mr + __log2f(sum));
+                for (int q = 0; q < 4; ++q) v[q] = (_Float16)(sum == 0.f ? 0.f : x[q] * f);         // (every token masked: as without tokens)
+                *(h4*)(a.out + head * DIM + c) = v;
+                if (c == 0 && a.lse) a.lse[head] = lse_of(M, sum);
             } else {
-                float* o = part + part_head(a.rows) + (size_t)r * DIM + c;
-                *(f4*)o = x;
-                *(f4*)(o + 4) = y;
-                if (c == 0) {
-                    part[2 * r] = Mr;
-                    part[2 * r + 1] = sum;
-                }
+                float* o = part + 2 * a.rows + (size_t)r * DIM + c;
+                put2(o, x[0], x[1]);
+                put2(o + 2, x[2], x[3]);
+                if (c == 0) put2(part + 2 * r, M, sum);
             }
         }
-        __syncthreads();
-        at = stop;
-    }
-}
-
-// Units that several workgroups share, and requests without tokens.  A workgroup takes `per` of a unit's query heads.
-template <int DIM, int BITS>
-__global__ __launch_bounds__(THREADS) void join_kernel(const AttendArgs a, int per)
-{
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ int scratch[NW];
-    constexpr int LPR = DIM / 8, SPAN = THREADS / LPR;    // lanes of a row; partial results read side by side
-    float* red = (float*)smem;                 // SPAN x (DIM + 2)
-    int* ends = (int*)(red + SPAN * (DIM + 2));
-    count_tiles(a, ends, scratch);
-    __syncthreads();
-    const int shares = (a.rows + per - 1) / per;
-    const int share = blockIdx.x % shares, unit = blockIdx.x / shares, pairs = a.kv * a.hblocks, b = unit / pairs, pair = unit - b * pairs;
-    const int h = pair / a.hblocks, hb = pair - h * a.hblocks;
-    const int nrows = a.group - 16 * hb < a.rows ? a.group - 16 * hb : a.rows;
-    const unsigned tiles = (unsigned)(ends[b + 1] - ends[b]), begin = (unsigned)ends[b] * pairs + (unsigned)pair * tiles;
-    const int r0 = share * per, r1 = r0 + per < nrows ? r0 + per : nrows;
-    const size_t head0 = (size_t)b * a.heads + h * a.group + 16 * hb;
-    const int c = 8 * (threadIdx.x % LPR), k = threadIdx.x / LPR;
-    if (tiles == 0) {
-        for (int r = r0 + k; r < r1; r += SPAN) {
-            *(u4*)(a.out + (head0 + r) * DIM + c) = u4{0, 0, 0, 0};
-            if (c == 0 && a.lse) a.lse[head0 + r] = -INFINITY;
-        }
-        return;
-    }
-    const Runs runs = runs_of(a, ends[a.B]);
-    const unsigned g0 = runs.owner(begin), g1 = runs.owner(begin + tiles - 1);
-    if (g0 == g1) return;
-    const float vs = BITS == 8 ? a.v_scale[h] : 1.f;
-    for (int r = r0; r < r1; ++r) {
-        float m = -INFINITY, l = 0.f;
-        f4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-        for (unsigned g = g0 + k; g <= g1; g += SPAN) {
-            const float* part = part_at(a, g, g == g0);
-            const float pm = part[2 * r], pl = part[2 * r + 1];
-            const float* o = part + part_head(a.rows) + (size_t)r * DIM + c;
-            const f4 px = *(const f4*)o, py = *(const f4*)(o + 4);
-            const float up = fmaxf(m, pm), f0 = m == -INFINITY ? 0.f : exp2_(m - up), f1 = pm == -INFINITY ? 0.f : exp2_(pm - up);
-            l = l * f0 + pl * (pm == -INFINITY ? 1.f : f1);
-            x = x * f0 + px * f1;
-            y = y * f0 + py * f1;
-            m = up;
-        }
-        float* mine = red + k * (DIM + 2);
-        if (c == 0) {
-            mine[0] = m;
-            mine[1] = l;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            mine[2 + c + q] = x[q];
-            mine[6 + c + q] = y[q];
-        }
-        __syncthreads();
-        if (k == 0) {
-            float M = red[0];
-#pragma unroll
-            for (int s = 1; s < SPAN; ++s) M = fmaxf(M, red[s * (DIM + 2)]);
-            float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < SPAN; ++s) {
-                const float* p = red + s * (DIM + 2);
-                const float f = p[0] == -INFINITY ? 0.f : exp2_(p[0] - M);
-                sum += p[0] == -INFINITY ? p[1] : p[1] * f;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) o[q] += p[2 + c + q] * f;
-            }
-            const float f = vs / sum;
-            h8 v;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = (_Float16)(sum == 0.f ? 0.f : o[q] * f);
-            *(h8*)(a.out + (head0 + r) * DIM + c) = v;
-            if (c == 0 && a.lse) a.lse[head0 + r] = LN2 * (M + __log2f(sum));
-        }
-        __syncthreads();
+        if (full) continue;
+        const Parts parts = parts_of(a, runs, plan, u);
+        finish<DIM, 2, 8>(a, parts, u, g == parts.g0 ? 0 : parts.first + (g - parts.g0 - 1), nrows, wave, NW, scratch, vs);
     }
 }
 
@@ -500,47 +681,44 @@ void set_blocks(AttendArgs& a)
     a.rows = a.group < 16 ? a.group : 16;
 }
 
-constexpr int MAX_WG = 768;
-
 template <int DIM, int BITS>
-hipError_t start(const AttendArgs& a, hipStream_t stream)
+hipError_t start(AttendArgs& a, hipStream_t stream)
 {
-    const size_t ends = ((size_t)a.B + 1) * sizeof(int), lds = NW * a.rows * DIM * sizeof(float) + ends;
+    const size_t lds = NW * a.rows * DIM * sizeof(float) + ((size_t)a.B + 1) * sizeof(int2);
     const auto kern = attend_kernel<DIM, BITS>;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
+    // as many workgroups as the chip holds at a time (registers, 160 KiB of LDS), and no more than the table's widest requests have work for
+    int each = (int)(159 * 1024 / (lds + 1024));
+    each = each < residents<DIM, BITS>() ? each : residents<DIM, BITS>();
+    const size_t most = (size_t)a.B * a.kv * a.hblocks * (((size_t)a.width * a.page + TILE - 1) / TILE + START + 1) / NW + 1;
+    a.nwg = most < (size_t)256 * each ? (int)most : 256 * each;
     kern<<<a.nwg, THREADS, lds, stream>>>(a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const int units = a.B * a.kv * a.hblocks, per = units >= 512 ? a.rows : 1;
-    join_kernel<DIM, BITS><<<units * ((a.rows + per - 1) / per), THREADS, THREADS / (DIM / 8) * (DIM + 2) * sizeof(float) + ends, stream>>>(a, per);
     return hipGetLastError();
 }
 
 template <int DIM>
-hipError_t start(const AttendArgs& a, hipStream_t stream)
+hipError_t start(AttendArgs& a, hipStream_t stream)
 {
     return a.bits == 8 ? start<DIM, 8>(a, stream) : start<DIM, 16>(a, stream);
 }
 
 }  // namespace
 
-size_t attend_workspace_bytes(int B, int heads, int kv, int dim, int max_tokens)
+size_t attend_workspace_bytes(int heads, int kv, int dim)
 {
     AttendArgs a{};
     a.heads = heads;
     a.kv = kv;
     set_blocks(a);
-    return (size_t)2 * MAX_WG * (part_head(a.rows) + a.rows * dim) * sizeof(float);
+    return ((size_t)COUNTERS + (size_t)2 * NW * MAX_WG * a.rows * (dim + 2)) * sizeof(float);
 }
 
 hipError_t launch_attend(AttendArgs a, hipStream_t stream)
 {
     set_blocks(a);
-    // no more workgroups than the longest requests the table allows have runs
-    const size_t most = (size_t)a.B * a.kv * a.hblocks * (((size_t)a.width * a.page + TILE - 1) / TILE + 1);
-    a.nwg = most / MIN_RUN + 1 < MAX_WG ? (int)(most / MIN_RUN + 1) : MAX_WG;
     return a.dim == 64 ? start<64>(a, stream) : (a.dim == 128 ? start<128>(a, stream) : start<256>(a, stream));
 }
 

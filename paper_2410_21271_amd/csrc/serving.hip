@@ -137,7 +137,7 @@ size_t eora_cache_attention_workspace_bytes(int B, int n_heads, int n_kv_heads, 
 {
     if (B < 0 || B > ATTEND_MAX_B || n_kv_heads <= 0 || n_heads <= 0 || n_heads % n_kv_heads || max_tokens < 0) return 0;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
-    return round256(attend_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens));
+    return round256(attend_workspace_bytes(n_heads, n_kv_heads, head_dim));
 }
 
 int eora_cache_attention(const void* q, const void* pages_k, const void* pages_v, const void* k_scale, const void* v_scale, const void* page_table,

@@ -42,14 +42,14 @@ struct AttendArgs {
     const int* lengths;             // B
     _Float16* out;                  // B x heads x dim
     float* lse;                     // B x heads, or null
-    float* parts;                   // partial results of units that several workgroups share
+    float* parts;                   // arrival counters, partial results of units that several wavefronts share
     int B, heads, kv, dim, q_stride, n_pages, page, bits, width, window;
     float scale;
     int group, hblocks, rows;       // query heads per kv head; blocks of 16 of them; of them in a block (set by the launcher)
     int nwg;                        // workgroups (set by the launcher)
 };
 constexpr int ATTEND_MAX_B = 8192;          // requests per call: their tile counts sit in LDS
-size_t attend_workspace_bytes(int B, int heads, int kv, int dim, int max_tokens);
+size_t attend_workspace_bytes(int heads, int kv, int dim);
 hipError_t launch_attend(AttendArgs a, hipStream_t stream);
 
 struct AdapterArgs {
