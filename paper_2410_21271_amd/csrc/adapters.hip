@@ -8,8 +8,9 @@
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
 // of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight.  With many rows of one pair, y's own traffic bounds it.
 //
-// Rows are grouped without sorting: a window of 64 rows is one adapter index a lane, the rows of a pair are a ballot, and the workgroup whose row
-// comes first among them (the leader) does the work for all.  Prompts have long runs of one pair; a batch of decoding requests has as many leaders as rows.
+// Rows are grouped without sorting: a window of 64 rows is one adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
+// the first row of each pair (its leader) its place among the window's pairs.  Every window has the same number of workgroups, which share its pairs out:
+// a pair's work is cut into as many parts as there are workgroups for it.  So long runs of one pair (prompts) and a pair for each row (a batch of decoding requests) both fill the chip.
 //
 // t is not rounded to fp16: each row's t is scaled by a power of two to a largest value in [256, 512) and split in two fp16 (22 bits, whatever the
 // size of t), both are multiplied with B's tile, and the sum is scaled back in fp32.  y is rounded once.
@@ -22,13 +23,49 @@ namespace {
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int WINDOW = 64;
 
-// the adapter of lane's row of a window (-1: none; -2: no row)
-__device__ __forceinline__ int adapter_of(const AdapterArgs& a, int row0, int lane)
+// A window's rows: lane's adapter (-1: none), the rows of the same one, and the first row of each
+struct Window {
+    int row0, id;
+    unsigned long long same, leaders;
+};
+__device__ __forceinline__ Window window_of(const AdapterArgs& a, int row0, bool with_none)
 {
-    const int row = row0 + lane;
-    if (row >= a.M) return -2;
-    const int id = a.ids[row];
-    return (unsigned)id < (unsigned)a.n ? id : -1;
+    const int lane = threadIdx.x & 63, row = row0 + lane;
+    const bool there = row < a.M;
+    Window w;
+    w.row0 = row0;
+    w.id = there ? a.ids[row] : -1;
+    w.id = (unsigned)w.id < (unsigned)a.n ? w.id : -1;
+    w.same = __ballot(there);
+    const unsigned key = (unsigned)(w.id + 1);             // 0 .. n
+    for (int bit = 0; bit < 32 - __clz(a.n); ++bit) {
+        const unsigned long long ones = __ballot(key >> bit & 1);
+        w.same &= key >> bit & 1 ? ones : ~ones;
+    }
+    w.leaders = __ballot(there && (with_none || w.id >= 0) && !(w.same & ((1ull << lane) - 1)));
+    return w;
+}
+// row of the p-th leader
+__device__ __forceinline__ int leader_at(const Window& w, int p)
+{
+    const int lane = threadIdx.x & 63;
+    return __ffsll(__ballot((w.leaders >> lane & 1) && __popcll(w.leaders & ((1ull << lane) - 1)) == p)) - 1;
+}
+__device__ __forceinline__ unsigned long long rows_at(const Window& w, int first)
+{
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)w.same, first), hi = __builtin_amdgcn_readlane((unsigned)(w.same >> 32), first);
+    return (unsigned long long)hi << 32 | lo;
+}
+
+// Ranges of the contraction in the first launch, for a window with so many pairs: as many as there are workgroups for, of a chunk a wavefront at least, and four at most where
+// pairs have more than a few rows (the second launch reads the parts of t of every row once a slab).
+constexpr int MAX_KSPLIT = 8;
+__device__ __forceinline__ int ranges_of(const AdapterArgs& a, int pairs)
+{
+    const int rows = a.M < WINDOW ? a.M : WINDOW, most = rows > 8 * pairs ? MAX_KSPLIT / 2 : MAX_KSPLIT;
+    int ks = 1;
+    while (2 * ks <= most && 2 * ks * NW <= a.d_in / 128 && 2 * ks * pairs * a.rgroups <= a.down_wgs) ks *= 2;
+    return ks;
 }
 
 // rank of a pair in whole k-tiles of B
@@ -41,26 +78,6 @@ __device__ __forceinline__ int rank_of(const AdapterArgs& a, int id, int step)
     return v > a.r || up > a.r ? a.r : up;
 }
 
-// The pairs of a window, one after the other: calls work(id, rows, first) for those that are `mine`.  With a workgroup for each row that may lead,
-// the one whose row leads; else the leaders are counted.
-template <typename F>
-__device__ __forceinline__ void for_pairs(const AdapterArgs& a, int ids, int mine, F work)
-{
-    if (a.leaders >= WINDOW || a.leaders >= a.M) {
-        const int id = __builtin_amdgcn_readlane(ids, mine);
-        const unsigned long long rows = __ballot(ids == id);
-        if (id != -2 && !(rows & ((1ull << mine) - 1))) work(id, rows);
-        return;
-    }
-    int k = 0;
-    for (unsigned long long left = __ballot(ids != -2); left;) {
-        const int id = __builtin_amdgcn_readlane(ids, __ffsll(left) - 1);
-        const unsigned long long rows = __ballot(ids == id);
-        left &= ~rows;
-        if (k++ % a.leaders == mine) work(id, rows);
-    }
-}
-
 // list[s] = place (in the window) of the s-th of the rows in `rows`; one list a wavefront
 __device__ __forceinline__ void list_rows(unsigned long long rows, int lane, int* list)
 {
@@ -70,7 +87,8 @@ __device__ __forceinline__ void list_rows(unsigned long long rows, int lane, int
 // Wavefronts of a workgroup: `blocks` of them (1, 2 or 4) have a block of 16 rows each, the others share their work
 __device__ __forceinline__ int row_blocks(int count) { return count <= 16 ? 1 : (count <= 32 ? 2 : 4); }
 
-// First launch.  A workgroup: 16 RB ranks of the leaders' pairs x one range of the contraction, in chunks of 128 columns.
+// First launch.  A workgroup: 16 RB ranks of the rows of a pair x one range of the contraction, in chunks of 128 columns.  x passes through LDS (a part of its own for each
+// wavefront) so that its rows are read 256 bytes at a time.
 template <int FA, int RB>
 struct Chunk {
     static constexpr int WORDS = Fmt<FA>::WORDS, TPC = 128 / Fmt<FA>::KT;        // tiles of a chunk
@@ -80,32 +98,38 @@ struct Chunk {
 };
 
 template <int FA, int RB>
-__global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, int step)
+__global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, int step)
 {
-    constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT;
+    constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT, XLD = 128 + 8;
     __shared__ int lists[NW][WINDOW];
+    __shared__ __attribute__((aligned(16))) _Float16 xs[NW][16 * XLD];
     __shared__ __attribute__((aligned(16))) float red[NW * RB * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    int at = blockIdx.x;
-    const int rg = at % a.rgroups;
-    at /= a.rgroups;
-    const int ks = at % a.ksplit;
-    at /= a.ksplit;
-    const int row0 = at / a.leaders * WINDOW;
+    const int window = blockIdx.x / a.down_wgs, g = blockIdx.x - window * a.down_wgs;
     int* list = lists[wave];
-    const int chunks = a.d_in / 128, c0 = chunks * ks / a.ksplit, c1 = chunks * (ks + 1) / a.ksplit, rb0 = rg * RB;
-    const int ids = adapter_of(a, row0, lane);
-    for_pairs(a, ids, at % a.leaders, [&](int id, unsigned long long rows) {
-        if (id < 0) return;
-        const int rank = rank_of(a, id, step), count = __popcll(rows);
-        if (16 * rb0 >= rank) return;
+    _Float16* xw = xs[wave];
+    const Window win = window_of(a, window * WINDOW, false);
+    const int pairs = __popcll(win.leaders), kss = ranges_of(a, pairs), chunks = a.d_in / 128;
+    for (int unit = g; unit < pairs * a.rgroups * kss; unit += a.down_wgs) {
+        const int rg = unit % a.rgroups, ks = unit / a.rgroups % kss, first_row = leader_at(win, unit / (a.rgroups * kss));
+        const int id = __builtin_amdgcn_readlane(win.id, first_row), c0 = chunks * ks / kss, c1 = chunks * (ks + 1) / kss, rb0 = rg * RB;
+        const unsigned long long rows = rows_at(win, first_row);
+        const int rank = rank_of(a, id, step), count = __popcll(rows), row0 = win.row0;
+        if (16 * rb0 >= rank) continue;
         const int blocks = rank / 16 - rb0 < RB ? rank / 16 - rb0 : RB;
         const int tbs = row_blocks(count), phases = NW / tbs, tb = wave % tbs, phase = wave / tbs;
         list_rows(rows, lane, list);
-        const int s = 16 * tb + n;
-        const _Float16* px = a.x + (size_t)(row0 + list[s < count ? s : 0]) * a.d_in;
+        // the rows of x that this lane moves, 16 bytes of each
+        const _Float16* px[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = 16 * tb + 4 * i + lane / 16;
+            px[i] = a.x + (size_t)(row0 + list[s < count ? s : 0]) * a.d_in + 8 * n;
+        }
         const uint32_t* tiles = (const uint32_t*)a.A + (size_t)id * a.r * a.d_in / KT * (64 * WORDS / 16) + (size_t)lane * WORDS;
         auto load = [&](Chunk<FA, RB>& k, int c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k.x[i] = *(const h8*)(px[i] + 128 * c);
 #pragma unroll
             for (int q = 0; q < RB; ++q) {
                 const int rb = rb0 + (q < blocks ? q : 0);               // (blocks beyond the rank read the first one again and are not stored)
@@ -113,13 +137,16 @@ __global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, i
                 for (int t = 0; t < TPC; ++t) load_words<WORDS>(k.w[q][t], tiles + ((size_t)rb * (a.d_in / KT) + (size_t)c * TPC + t) * (64 * WORDS));
                 if constexpr (FA != S_F16) k.sc[q] = a.A_scales[((size_t)id * a.r + 16 * rb + n) * chunks + c];
             }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) k.x[t] = *(const h8*)(px + 128 * c + (FA == S_F16 ? 32 * t + 8 * j : 32 * j + 8 * t));
         };
         f4 acc[RB];
 #pragma unroll
         for (int q = 0; q < RB; ++q) acc[q] = f4{0.f, 0.f, 0.f, 0.f};
         auto add = [&](const Chunk<FA, RB>& k) {
+            h8 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *(h8*)(xw + (4 * i + lane / 16) * XLD + 8 * n) = k.x[i];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[t] = *(const h8*)(xw + n * XLD + (FA == S_F16 ? 32 * t + 8 * j : 32 * j + 8 * t));
 #pragma unroll
             for (int q = 0; q < RB; ++q) {
                 h8 f[4];
@@ -132,12 +159,12 @@ __global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, i
                         f[t] = g.v;
                     }
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[q] = mfma16(k.x[t], f[t], acc[q]);
+                    for (int t = 0; t < 4; ++t) acc[q] = mfma16(x[t], f[t], acc[q]);
                 } else {
                     decode_tile<FA>(k.w[q][0], 8u, f);
                     f4 part = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) part = mfma16(k.x[t], f[t], part);
+                    for (int t = 0; t < 4; ++t) part = mfma16(x[t], f[t], part);
                     acc[q] += (float)k.sc[q] * part;
                 }
             }
@@ -148,14 +175,18 @@ __global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, i
             Chunk<FA, RB> even, odd;
             load(even, first);
             int i = 0;
+            // (fences: the compiler would otherwise multiply first and request afterwards)
             for (; i + 2 < mine; i += 2) {
                 load(odd, first + (i + 1) * phases);
+                __builtin_amdgcn_sched_barrier(0);
                 add(even);
                 load(even, first + (i + 2) * phases);
+                __builtin_amdgcn_sched_barrier(0);
                 add(odd);
             }
             if (i + 1 < mine) {
                 load(odd, first + (i + 1) * phases);
+                __builtin_amdgcn_sched_barrier(0);
                 add(even);
                 add(odd);
             } else {
@@ -170,10 +201,10 @@ __global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, i
                     const int slot = 16 * tb + 4 * j + i;
                     if (slot < count && q < blocks) a.t[((size_t)ks * a.M + row0 + list[slot]) * a.r + 16 * (rb0 + q) + n] = acc[q][i];
                 }
-            return;
+            continue;
         }
         // sum over the wavefronts of a block of rows, in order
-        __syncthreads();                                  // (the last pair's sums have been read)
+        __syncthreads();                                  // (the last unit's sums have been read)
 #pragma unroll
         for (int q = 0; q < RB; ++q) *(f4*)(red + ((wave * RB + q) * 64 + lane) * 4) = acc[q];
         __syncthreads();
@@ -185,41 +216,34 @@ __global__ __launch_bounds__(THREADS, 2) void down_kernel(const AdapterArgs a, i
             for (int p = 0; p < phases; ++p) sum += red[(((p * tbs + b) * RB + q) * 64 + l) * 4 + i];
             a.t[((size_t)ks * a.M + row0 + list[slot]) * a.r + 16 * (rb0 + q) + col] = sum;
         }
-    });
+    }
 }
 
-// Second launch.  A workgroup: the leaders' rows x a slab of outputs.  A wavefront keeps t of its 16 rows in registers, as the second operand (NK fragments of 32 ranks, high
-// and low halves), and takes 16 PB outputs at a time: B's tiles are the first operand.  The products pass through LDS (a part of its own for each
-// wavefront, no barrier) so that base and y are moved 16 bytes a lane, consecutive lanes along a row: straight from the products' registers they are 16 rows an instruction, 64
-// accesses of the L1 instead of 16 (2048 rows, 4096 -> 14336, rank 128: 131 us this launch, 38 now).
-template <int FE, int NK>
-__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const AdapterArgs a, int slabs)
-{
-    constexpr int WORDS = Fmt<FE>::WORDS, KT = Fmt<FE>::KT, NF = KT / 32, TILES = NK / NF;
-    constexpr int PB = NK <= 4 || (FE != S_F16 && NK <= 8) ? 4 : 2;       // blocks of 16 outputs at a time
-    constexpr int LPR = 2 * PB, RPI = 64 / LPR, INS = (16 + RPI - 1) / RPI;      // lanes of a row, rows of an instruction, instructions
-    constexpr int LD = 16 * PB + 4;
+// Second launch.  A workgroup: the leaders' rows x a slab of outputs.  A wavefront keeps t of its 16 rows in registers, as the second operand (NK fragments of 32
+// ranks, high and low halves), and takes 16 PB outputs at a time: B's tiles are the first operand.  What is row-major (t on its way in, base and y) passes through LDS, a part of
+// its own for each wavefront and no barrier, so that it is moved 16 bytes a lane, consecutive lanes along a row: straight to and from the operands' places it is
+// 16 rows an instruction, 64 accesses of the L1 instead of 16.
+// SHARE (many rows): the wavefronts have a block of rows each and all outputs of the slab, so that B's tiles are requested once a workgroup, a quarter by each, and pass through LDS
+// too, two steps of them (requested by every wavefront they are 470 MB from L2 for 2048 rows, 4096 -> 14336, rank 128).
+template <int FE, int NK, bool SHARE>
+struct Up {
+    static constexpr int WORDS = Fmt<FE>::WORDS, KT = Fmt<FE>::KT, NF = KT / 32, TILES = NK / NF;
+    static constexpr int PB = NK <= 4 || (FE != S_F16 && NK <= 8) ? 4 : 2;       // blocks of 16 outputs at a time
+    static constexpr int LPR = 2 * PB, RPI = 64 / LPR, INS = (16 + RPI - 1) / RPI;       // lanes of a row, rows of an instruction, instructions of a block of rows
+    static constexpr int LD = 16 * PB + 4, COLS = NK * 32 < 128 ? NK * 32 : 128, TLD = COLS + 4;
+    static constexpr int LDS = 16 * (LD > TLD ? LD : TLD);                       // floats of a wavefront
+    static constexpr int STEP = PB * TILES, HELD = SHARE ? (STEP + NW - 1) / NW : STEP;      // tiles of a step, of them in this wavefront's registers
+    static constexpr int STAGE = SHARE ? 2 * STEP * 64 * WORDS : 1;                          // words of the workgroup
     typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-    __shared__ int lists[NW][WINDOW];
-    __shared__ __attribute__((aligned(16))) float turn[NW][16 * LD];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    int at = blockIdx.x;
-    const int slab = at % slabs;
-    at /= slabs;
-    const int row0 = at / a.leaders * WINDOW;
-    int* list = lists[wave];
-    float* mine = turn[wave];
-    const int ids = adapter_of(a, row0, lane);
-    for_pairs(a, ids, at % a.leaders, [&](int id, unsigned long long rows) {
-        const int rank = rank_of(a, id, KT), count = __popcll(rows), ntk = a.r / KT, nt = rank / KT;
-        if (rank == 0 && a.base == a.y) return;           // nothing to add
-        const int tbs = row_blocks(count), phases = NW / tbs, tb = wave % tbs, phase = wave / tbs, here = count - 16 * tb < 16 ? count - 16 * tb : 16;
-        list_rows(rows, lane, list);
-        const bool live = n < here;
-        const size_t row = (size_t)(row0 + list[live ? 16 * tb + n : 0]);
-        const int blocks = a.d_out / 16, end = (slab + 1) * a.slab < blocks ? (slab + 1) * a.slab : blocks;
-        int rb = slab * a.slab + PB * phase;
-        if (rb >= end || here <= 0) return;
+
+    // tb: this wavefront's first block of rows; it takes every `phases`-th step of 16 PB outputs from `phase` on
+    static __device__ __forceinline__ void run(const AdapterArgs& a, int id, int rank, int row0, const int* list, int count, int tb, int phase, int phases, int first_block, int end, int kss, float* mine, uint32_t* stage)
+    {
+        const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+        const int ntk = a.r / KT, nt = rank / KT, here = count - 16 * tb;
+        int rb = first_block + PB * phase;
+        if (!SHARE && (rb >= end || here <= 0)) return;
+        const int wave = SHARE ? tb : 0;
         // the rows that this lane moves
         const int piece = lane % LPR;
         size_t moved[INS];
@@ -229,21 +253,24 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
             moved[i] = (size_t)(row0 + list[r < here ? 16 * tb + r : 0]) * a.d_out;
         }
 
-        uint32_t w[PB][TILES][WORDS];
+        uint32_t w[HELD][WORDS];
         h4 sc[PB][TILES];                                 // of rows 4 j .. 4 j + 3, TILES tiles each
         h8 base[INS];
         const _Float16* from = a.base ? a.base : a.y;     // (requested either way: no branch around a request)
         const uint32_t* tiles = (const uint32_t*)a.B + (id < 0 ? 0 : (size_t)id * a.d_out * a.r / KT * (64 * WORDS / 16)) + (size_t)lane * WORDS;
-        auto load = [&](int first) {
+        auto load_tiles = [&](int first) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int k = SHARE ? wave + NW * i : i, p = k / TILES, t = k % TILES, R = first + p < end ? first + p : end - 1;
+                const size_t tile = (size_t)R * ntk + (t < nt ? t : (nt ? nt - 1 : 0));      // (beyond the rank: the last tile again, times zeros)
+                load_words<WORDS>(w[i], tiles + tile * (64 * WORDS));
+            }
+        };
+        auto load_rest = [&](int first) {
 #pragma unroll
             for (int p = 0; p < PB; ++p) {
-                const int R = first + p < end ? first + p : end - 1;
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    const size_t tile = (size_t)R * ntk + (t < nt ? t : (nt ? nt - 1 : 0));     // (beyond the rank: the last tile again, times zeros)
-                    load_words<WORDS>(w[p][t], tiles + tile * (64 * WORDS));
-                }
                 if constexpr (FE != S_F16) {
+                    const int R = first + p < end ? first + p : end - 1;
                     const _Float16* src = a.B_scales + ((size_t)(id < 0 ? 0 : id) * a.d_out + 16 * R + 4 * j) * TILES;
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) sc[p][t] = *(const h4*)(src + 4 * t);
@@ -253,52 +280,63 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
 #pragma unroll
             for (int i = 0; i < INS; ++i) base[i] = *(const h8*)(from + moved[i] + (c < last ? c : last));
         };
-        load(rb);
-
-        // t of this lane's row, its k-slots: sums of the ranges in order
-        float t[NK][8];
-        float big = 0.f;
+        auto put_tiles = [&](int buffer) {
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+            for (int i = 0; i < HELD; ++i) {
+                if (STEP % NW && wave + NW * i >= STEP) break;
+                uint32_t* dst = stage + ((size_t)(buffer * STEP + wave + NW * i) * 64 + lane) * WORDS;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) t[k][e] = 0.f;
-        constexpr int ROUND = NK <= 4 ? 2 : 1;            // ranges requested at a time
-#pragma clang loop unroll(disable)
-        for (int k0 = 0; k0 < a.ksplit; k0 += ROUND) {
-            f4 in[ROUND][NK][2];
-#pragma unroll
-            for (int q = 0; q < ROUND; ++q) {
-                const float* src = a.t + ((size_t)(k0 + q < a.ksplit ? k0 + q : k0) * a.M + row) * a.r + KT / 4 * j;
-#pragma unroll
-                for (int k = 0; k < NK; ++k) {
-                    const float* at = src + (k / NF < nt ? k / NF * KT : 0) + 8 * (k % NF);
-                    in[q][k][0] = *(const f4*)at;
-                    in[q][k][1] = *(const f4*)(at + 4);
-                }
+                for (int v = 0; v < WORDS; ++v) dst[v] = w[i][v];
             }
-#pragma unroll
-            for (int q = 0; q < ROUND; ++q)
-#pragma unroll
-                for (int k = 0; k < NK; ++k) {
-                    const bool there = live && k / NF < nt && k0 + q < a.ksplit;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) t[k][e] += there ? in[q][k][e / 4][e % 4] : 0.f;
-                }
-        }
+        };
+        load_tiles(rb);
+        load_rest(rb);
+        __builtin_amdgcn_sched_barrier(0);
+
+        // t of the rows, summed over the ranges in order, COLS columns at a time
+        h8 high[NK], low[NK];
+        float t[NK][8], big = 0.f;
+        constexpr int TL = COLS / 4, TRI = 64 / TL, TIN = 16 / TRI;              // lanes of a row, rows of an instruction, instructions
         const float scaling = a.scalings && id >= 0 ? a.scalings[id] : 1.f;
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+        for (int c = 0; c < NK * 32 / COLS; ++c) {
+            f4 sum[TIN];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                t[k][e] *= scaling;
-                big = fmaxf(big, fabsf(t[k][e]));
+            for (int i = 0; i < TIN; ++i) sum[i] = f4{0.f, 0.f, 0.f, 0.f};
+            const int col = c * COLS + 4 * (lane % TL);
+#pragma clang loop unroll(disable)
+            for (int ks = 0; ks < kss; ++ks) {
+                f4 in[TIN];
+#pragma unroll
+                for (int i = 0; i < TIN; ++i) {
+                    const int r = lane / TL + TRI * i;
+                    in[i] = *(const f4*)(a.t + ((size_t)ks * a.M + row0 + list[r < here ? 16 * tb + r : 0]) * a.r + (col < rank ? col : 0));
+                }
+#pragma unroll
+                for (int i = 0; i < TIN; ++i) sum[i] += in[i];
             }
+#pragma unroll
+            for (int i = 0; i < TIN; ++i) {
+                const int r = lane / TL + TRI * i;
+                *(f4*)(mine + r * TLD + 4 * (lane % TL)) = r < here && col < rank ? sum[i] * scaling : f4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int k = 0; k < COLS / 32; ++k) {
+                const float* src = mine + n * TLD + k / NF * KT + KT / 4 * j + 8 * (k % NF);
+                const f4 lo = *(const f4*)src, hi = *(const f4*)(src + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = e < 4 ? lo[e] : hi[e - 4];
+                    t[c * (COLS / 32) + k][e] = v;
+                    big = fmaxf(big, fabsf(v));
+                }
+            }
+        }
         big = fmaxf(big, __shfl_xor(big, 16, 64));
         big = fmaxf(big, __shfl_xor(big, 32, 64));
-        int ex = (int)(__float_as_uint(big) >> 23) - 127; // exponent of the row's largest value
+        int ex = (int)(__float_as_uint(big) >> 23) - 127;  // exponent of the row's largest value
         ex = big == 0.f ? 8 : (ex < -110 ? -110 : (ex > 127 ? 127 : ex));
         const float to = __uint_as_float((unsigned)(127 + 8 - ex) << 23), back = rank ? __uint_as_float((unsigned)(127 - 8 + ex) << 23) : 0.f;
-        h8 high[NK], low[NK];
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
@@ -308,16 +346,33 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
                 low[k][e] = (_Float16)(fabsf(v) == INFINITY ? 0.f : v - (float)high[k][e]);
             }
 
-        for (;;) {
+        if constexpr (SHARE) {
+            __syncthreads();                              // (the last unit's tiles have been read)
+            put_tiles(0);
+            load_tiles(rb + PB < end ? rb + PB : rb);
+            __syncthreads();
+        }
+        for (int buffer = 0;; buffer ^= 1) {
+            f4 acc[PB];
 #pragma unroll
-            for (int p = 0; p < PB; ++p) {
-                f4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < PB; ++p) acc[p] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int q = 0; q < TILES; ++q) {
+            for (int q = 0; q < TILES; ++q)
+#pragma unroll
+                for (int p = 0; p < PB; ++p) {
+                    uint32_t now[WORDS];
+                    if constexpr (SHARE) {
+                        const uint32_t* src = stage + ((size_t)(buffer * STEP + p * TILES + q) * 64 + lane) * WORDS;
+#pragma unroll
+                        for (int v = 0; v < WORDS; ++v) now[v] = src[v];
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < WORDS; ++v) now[v] = w[p * TILES + q][v];
+                    }
                     h8 f[NF];
-                    decode_tile<FE>(w[p][q], 8u, f);
+                    decode_tile<FE>(now, 8u, f);
                     f4 part = {0.f, 0.f, 0.f, 0.f};
-                    f4& sum = FE == S_F16 ? acc : part;
+                    f4& sum = FE == S_F16 ? acc[p] : part;
 #pragma unroll
                     for (int i = 0; i < NF; ++i) {
                         sum = mfma16(f[i], high[q * NF + i], sum);
@@ -325,12 +380,13 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
                     }
                     if constexpr (FE != S_F16) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[i] += (float)sc[p][(i * TILES + q) / 4][(i * TILES + q) % 4] * part[i];
+                        for (int i = 0; i < 4; ++i) acc[p][i] += (float)sc[p][(i * TILES + q) / 4][(i * TILES + q) % 4] * part[i];
                     }
                 }
-                // (without a pair the tiles are another's: whatever they give, nothing is added)
-                *(f4*)(mine + n * LD + 16 * p + 4 * j) = rank ? acc * back : f4{0.f, 0.f, 0.f, 0.f};
-            }
+            const int col = 16 * rb + 8 * piece;
+            // (without a pair the tiles are another's: whatever they give, nothing is added)
+#pragma unroll
+            for (int p = 0; p < PB; ++p) *(f4*)(mine + n * LD + 16 * p + 4 * j) = rank ? acc[p] * back : f4{0.f, 0.f, 0.f, 0.f};
             h8 y[INS];
 #pragma unroll
             for (int i = 0; i < INS; ++i) {
@@ -339,19 +395,59 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[i][e] = (_Float16)((a.base ? (float)base[i][e] : 0.f) + (e < 4 ? lo[e] : hi[e - 4]));
             }
-            const int col = 16 * rb + 8 * piece;
             rb += PB * phases;
             const bool more = rb < end;
-            if (more) load(rb);
+            if (more) {
+                if constexpr (SHARE) {
+                    put_tiles(buffer ^ 1);
+                    load_tiles(rb + PB < end ? rb + PB : rb);
+                } else {
+                    load_tiles(rb);
+                }
+                load_rest(rb);
+            }
 #pragma unroll
             for (int i = 0; i < INS; ++i)
                 if (lane / LPR + RPI * i < here && col < 16 * end) *(h8*)(a.y + moved[i] + col) = y[i];
             if (!more) break;
+            if constexpr (SHARE) __syncthreads();
         }
-    });
+    }
+};
+
+template <int FE, int NK, bool SHARE>
+__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const AdapterArgs a)
+{
+    typedef Up<FE, NK, SHARE> Rows;
+    __shared__ int lists[NW][WINDOW];
+    __shared__ __attribute__((aligned(16))) float space[NW][Rows::LDS];
+    __shared__ __attribute__((aligned(16))) uint32_t stage[Rows::STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int window = blockIdx.x / a.up_wgs, g = blockIdx.x - window * a.up_wgs;
+    int* list = lists[wave];
+    // (rows without a pair have nothing to add; with y apart from base they are copied)
+    const Window win = window_of(a, window * WINDOW, a.base != a.y);
+    const int pairs = __popcll(win.leaders), kss = ranges_of(a, __popcll(win.leaders & __ballot(win.id >= 0)));
+    // slabs of outputs: as many as there are workgroups for, a step of each wavefront at least
+    const int blocks = a.d_out / 16, unit_blocks = NW * Rows::PB, least = (blocks + unit_blocks - 1) / unit_blocks;
+    const int each = pairs ? a.up_wgs / pairs : 1, slabs = each < 1 ? 1 : (each < least ? each : least), size = (blocks + slabs - 1) / slabs;
+    for (int unit = g; unit < pairs * slabs; unit += a.up_wgs) {
+        const int slab = unit % slabs, first_row = leader_at(win, unit / slabs);
+        const int id = __builtin_amdgcn_readlane(win.id, first_row);
+        const unsigned long long rows = rows_at(win, first_row);
+        const int rank = rank_of(a, id, Fmt<FE>::KT), count = __popcll(rows), first = slab * size, end = first + size < blocks ? first + size : blocks;
+        if ((rank == 0 && a.base == a.y) || first >= end) continue;
+        list_rows(rows, lane, list);
+        if (SHARE && count > 16) {
+            Up<FE, NK, SHARE>::run(a, id, rank, win.row0, list, count, wave, 0, 1, first, end, kss, space[wave], stage);
+        } else {
+            const int tbs = row_blocks(count);
+            Up<FE, NK, false>::run(a, id, rank, win.row0, list, count, wave % tbs, wave / tbs, NW / tbs, first, end, kss, space[wave], stage);
+        }
+    }
 }
 
-constexpr int MAX_KSPLIT = 8;
+constexpr int MANY = 512;                      // rows
 
 template <int FA, int RB>
 hipError_t start_down(const AdapterArgs& a, unsigned grid, int step, hipStream_t stream)
@@ -369,8 +465,9 @@ hipError_t start_down(const AdapterArgs& a, unsigned grid, int rblocks, int step
 template <int FE, int NK>
 hipError_t start_up(const AdapterArgs& a, int windows, hipStream_t stream)
 {
-    const int slabs = (a.d_out / 16 + a.slab - 1) / a.slab;
-    up_kernel<FE, NK><<<(unsigned)(windows * a.leaders) * slabs, THREADS, 0, stream>>>(a, slabs);
+    // (the kernel that can share has less LDS left for others)
+    if (a.M >= MANY) up_kernel<FE, NK, true><<<(unsigned)windows * a.up_wgs, THREADS, 0, stream>>>(a);
+    else up_kernel<FE, NK, false><<<(unsigned)windows * a.up_wgs, THREADS, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -400,25 +497,21 @@ hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
         a.ids += m0;
         a.y += (size_t)m0 * a.d_out;
         if (a.base) a.base += (size_t)m0 * a.d_out;
-        const int windows = (a.M + WINDOW - 1) / WINDOW, chunks = a.d_in / 128, nr = a.r / 16;
-        // a workgroup for each row that may lead; where there are many windows (prompts) few rows lead
-        a.leaders = windows == 1 ? a.M : (windows <= 8 ? WINDOW : 2);
-        const int groups = windows * (windows <= 8 ? a.leaders : 1);
-        int rblocks = groups * ((nr + 3) / 4) * (chunks < 16 ? 1 : 4) >= 256 && nr >= 4 ? 4 : 1;
+        const int windows = (a.M + WINDOW - 1) / WINDOW, nr = a.r / 16, rblocks = nr < 4 || (a.M == 1 && nr <= 8) ? 1 : 4;
         a.rgroups = (nr + rblocks - 1) / rblocks;
-        a.ksplit = 1;
-        while (a.ksplit < MAX_KSPLIT && a.ksplit * 2 * NW <= chunks && groups * a.rgroups * a.ksplit < 512) a.ksplit *= 2;
+        // one workgroup a compute unit with two chunks in its registers; two
+        a.down_wgs = windows < 256 ? 256 / windows : 1;
+        a.up_wgs = windows < 512 ? 512 / windows : 1;
+        if (a.M < WINDOW) {                               // no more than its rows have work for
+            const int down = a.M * a.rgroups * MAX_KSPLIT, up = a.M * ((a.d_out / 16 + 7) / 8);
+            a.down_wgs = down < a.down_wgs ? down : a.down_wgs;
+            a.up_wgs = up < a.up_wgs ? up : a.up_wgs;
+        }
         const int step = fe == S_F16 ? 32 : (fe == S_Q4S64 ? 64 : 128);
-        const unsigned grid = (unsigned)(windows * a.leaders) * a.rgroups * a.ksplit;
+        const unsigned grid = (unsigned)windows * a.down_wgs;
         hipError_t e = fa == S_F16 ? start_down<S_F16>(a, grid, rblocks, step, stream)
                                    : (fa == S_Q4S128 ? start_down<S_Q4S128>(a, grid, rblocks, step, stream) : start_down<S_Q3S128>(a, grid, rblocks, step, stream));
         if (e != hipSuccess) return e;
-        // slabs of outputs: enough workgroups to fill the chip, a step of each wavefront at least
-        const int blocks = a.d_out / 16, least = (a.r <= 128 || (fe != S_F16 && a.r <= 256) ? 4 : 2) * NW;
-        int slabs = (512 + groups - 1) / groups;
-        if (windows > 8) slabs = (slabs + 7) / 8 * 8;     // slab s of every window then runs on the same XCD, whose L2 keeps its tiles
-        a.slab = (blocks + slabs - 1) / slabs;
-        a.slab = windows > 8 ? (a.slab + 3) / 4 * 4 : (a.slab + least - 1) / least * least;
         e = fe == S_F16 ? start_up<S_F16>(a, windows, stream)
                         : (fe == S_Q4S64 ? start_up<S_Q4S64>(a, windows, stream)
                                          : (fe == S_Q4S128 ? start_up<S_Q4S128>(a, windows, stream) : start_up<S_Q3S128>(a, windows, stream)));

@@ -63,9 +63,9 @@ struct AdapterArgs {
     const int* ids;                 // M
     const _Float16* base;           // M x d_out, or null: zeros
     _Float16* y;                    // M x d_out
-    float* t;                       // ksplit x M x r partial sums of x A^T
+    float* t;                       // ranges x M x r partial sums of x A^T
     int M, d_in, d_out, r, n;
-    int ksplit, leaders, rgroups, slab;     // set by the launcher
+    int rgroups, down_wgs, up_wgs;          // groups of ranks; workgroups of a window in either launch (set by the launcher)
 };
 size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r);
 hipError_t launch_adapters(AdapterArgs a, int fa, int fe, hipStream_t stream);

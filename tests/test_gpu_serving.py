@@ -136,6 +136,23 @@ def test_adapters_shapes(gpu, M, d_in, d_out, r, n, bits, mixed):
     check_adapters(gpu, pool, x, ids, None, None)
 
 
+@pytest.mark.parametrize("bits,r", [(16, 96), (16, 256), (16, 384), (16, 512), (4, 64), (4, 256), (3, 128), (3, 384)])
+def test_adapters_many_rows(gpu, bits, r):
+    """From 512 rows on, blocks of rows of one pair share its tiles; pairs of few rows and rows without one lie between them."""
+    rng = np.random.default_rng(r + bits)
+    pool = Pool(gpu, 60 + r, 256, 336, r, 4, bits, [r, r // 2 if bits == 16 else r, r, 0])
+    ids = np.concatenate([np.repeat([1, 0, -1, 2, 3], [130, 200, 5, 190, 3]), rng.integers(-1, 4, 30)])
+    x, base = rng.normal(0, 1, (len(ids), 256)).astype(np.float16), rng.normal(0, 1, (len(ids), 336)).astype(np.float16)
+    step = 32 if bits == 16 else min(128, r)
+    for a, k in enumerate([r, r // 2 if bits == 16 else r, r, 0]):       # ranks go up to whole tiles
+        up = -(-k // step) * step
+        if up != k:
+            pool.pairs[a] = tuple(t.astype(np.float64) for t in _first(pool, gpu, 60 + r, 256, 336, r, 4, a, up))
+    y = check_adapters(gpu, pool, x, ids, [1.0, -0.5, 2.0, 1.0], base)
+    again = run_adapters(gpu, pool, x, ids, [1.0, -0.5, 2.0, 1.0], base, in_place=True)
+    assert np.array_equal(y.view(np.uint16), again.view(np.uint16))
+
+
 def test_adapters_runs_of_prompts(gpu):
     """300 rows of four prompts, one without a pair: runs that begin and end inside windows."""
     rng = np.random.default_rng(5)
