@@ -28,7 +28,7 @@ namespace {
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int TILE = 32;
 constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs)
-constexpr int MIN_RUN = 16, FEW = 8;           // cost of a workgroup's run at least: requests of one length, of several
+constexpr int MIN_RUN = 20, FEW = 8;           // cost of a workgroup's run at least: requests of one length, of several
 constexpr int MAX_WG = 1024;
 constexpr int SLOTS = 2 * NW * MAX_WG;
 constexpr int COUNTERS = SLOTS + NW * MAX_WG;  // words before the partial results: a counter for each group of them, and for each unit
@@ -87,35 +87,50 @@ __device__ __forceinline__ void add_costs(const AttendArgs& a, int2* plan, int* 
     }
 }
 
-// The units in one row, each START + tiles long (the first START places stand for what a unit costs beside its tiles), cut into equal runs:
-// wavefront w of n workgroups has [cut(w), cut(w + 1)).
+// The units in one row, each START + tiles long (the first START places stand for what a unit costs beside its tiles), cut into runs that differ by one at
+// most: wavefront w of n workgroups has [cut(w), cut(w + 1)).  With requests of one length, and workgroups for all of them, each unit is cut for itself, into `each` runs.
 struct Runs {
-    unsigned total, n;                         // total >= 4 n, unless there is one unit of one or two tiles: no run is empty
-    __device__ unsigned cut(unsigned w) const { return (unsigned)((unsigned long long)w * total / (n * NW)); }
+    unsigned n, each, length, q, r;            // a stretch of `length` = q each + r places has `each` runs, at most 4 MAX_WG
+    __device__ unsigned cut(unsigned w) const
+    {
+        const unsigned stretch = w / each, i = w - stretch * each;
+        return stretch * length + i * q + i * r / each;       // floor(i length / each), without 64 bits
+    }
     // the wavefront whose run holds a place
     __device__ unsigned owner(unsigned at) const
     {
-        unsigned w = (unsigned)((unsigned long long)at * (n * NW) / total);
-        while (cut(w + 1) <= at) ++w;
+        const unsigned stretch = at / length;
+        unsigned w = stretch * each + (unsigned)((float)(at - stretch * length) * ((float)each / (float)length));     // one off at most
+        w = w < n * NW ? w : n * NW - 1;
         while (cut(w) > at) --w;
+        while (cut(w + 1) <= at) ++w;
         return w;
     }
 };
 __device__ __forceinline__ Runs runs_of(const AttendArgs& a, const int2* plan)
 {
-    const unsigned pairs = (unsigned)(a.kv * a.hblocks), units = (unsigned)a.B * pairs;
+    const unsigned pairs = (unsigned)(a.kv * a.hblocks), units = (unsigned)a.B * pairs, total = (unsigned)plan[a.B].x * pairs, cost = (unsigned)plan[1].x;
     Runs r;
-    r.total = (unsigned)plan[a.B].x * pairs;
     r.n = (unsigned)a.nwg;
-    if (units < r.n && (unsigned)plan[1].x * (unsigned)a.B == (unsigned)plan[a.B].x) {
-        // requests of one length: a whole number of workgroups a unit
-        const unsigned k = (r.total + units * MIN_RUN - 1) / (units * MIN_RUN), most = r.n / units;
-        r.n = units * (k > most ? most : (k < 1 ? 1 : k));
-    } else if (r.n > r.total / FEW + 1) {
-        r.n = r.total / FEW + 1;
+    r.each = 0;
+    if (units <= r.n && cost * (unsigned)a.B == (unsigned)plan[a.B].x) {
+        const unsigned k = (cost + MIN_RUN - 1) / MIN_RUN, most = r.n / units;
+        r.each = NW * (k > most ? most : (k < 1 ? 1 : k));
+        r.length = cost;
+        r.n = units * r.each / NW;
     }
-    if (r.n > r.total / NW) r.n = r.total / NW;
-    if (r.n == 0 && r.total) r.n = 1;
+    if (r.each == 0 || r.each > r.length) {    // (runs are not empty: at least NW places a workgroup, unless there are fewer in all)
+        if (r.n > total / FEW + 1) r.n = total / FEW + 1;
+        if (r.n > total / NW) r.n = total / NW;
+        if (r.n == 0 && total) r.n = 1;
+        r.each = NW * r.n;
+        r.length = total;
+    }
+    r.each = __builtin_amdgcn_readfirstlane(r.each);
+    r.length = __builtin_amdgcn_readfirstlane(r.length);
+    r.n = __builtin_amdgcn_readfirstlane(r.n);
+    r.q = r.each ? r.length / r.each : 0;
+    r.r = r.length - r.q * r.each;
     return r;
 }
 
@@ -126,11 +141,14 @@ struct Unit {
 __device__ __forceinline__ Unit unit_at(const AttendArgs& a, const int2* plan, unsigned at)
 {
     const unsigned pairs = (unsigned)(a.kv * a.hblocks);
-    int lo = 0, hi = a.B;                      // plan[lo].x * pairs <= at < plan[hi].x * pairs
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if ((unsigned)plan[mid].x * pairs <= at) lo = mid;
-        else hi = mid;
+    // the last request that begins at or before `at`: 64 places a look
+    int lo = 0;
+    for (int range = a.B; range > 1;) {
+        const int stride = (range + 63) / 64, mine = lo + (int)(threadIdx.x & 63) * stride;
+        const bool before = mine < lo + range && (unsigned)plan[mine < a.B ? mine : a.B].x * pairs <= at;
+        const int past = lo + range;
+        lo += (__popcll(__ballot(before)) - 1) * stride;
+        range = past - lo < stride ? past - lo : stride;
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     Unit u;
