@@ -334,7 +334,7 @@ int eora_linear_sp24_group(const void* x, const eora_sp_member* members, int n_m
  * written `base`):
  *      y[m] = base[m] + s_a * (x[m].A_a^T).B_a^T,      a = adapter_of_row[m]
  * Only the pairs that rows select are read, so the pool may hold any number of them; eora_linear_q_multi() streams all of
- * its pairs (ranks together <= 512) and needs no second launch.
+ * its pairs (ranks together <= 512).
  * A_pool, B_pool: n_adapters slots, one after the other; slot a holds A_a (r x d_in) and B_a (d_out x r) as
  *      eora_pack_factor_*() or eora_factors_store_*() write them (ab_bits 16, 4 or 3), its scales (ab_bits 4 and 3) lie
  *      at slot a of A_scales and B_scales.
@@ -344,6 +344,9 @@ int eora_linear_sp24_group(const void* x, const eora_sp_member* members, int n_m
  * scalings: n_adapters fp32 or NULL (all 1).
  * adapter_of_row: M int32; values outside [0, n_adapters): y[m] = base[m].
  * base: fp16 M x d_out, or NULL (zeros); may be y itself, and must not overlap it otherwise.
+ * workspace: eora_adapters_workspace_bytes() of the largest call.  Its bytes are ZERO before the first call (hipMemset, say); every call leaves it
+ * usable for the next, of whatever sizes.  Up to 64 rows are one launch, in which a bounded wait (eora_debug_set_spin_limit()) hands t over:
+ * eora_workspace_error() reports one that expired (y is then invalid, and the workspace to be zeroed again).
  * t = x.A^T is held in fp32 (multiplied with B's tiles as two fp16 of 22 bits together, whatever its magnitude); the sum with
  * base is rounded once.  Equal inputs give bit-equal outputs; a row's sums do not depend on the other rows'
  * contents, but may be split differently when M changes.

@@ -405,7 +405,7 @@ def adapters_workspace_bytes(M, d_in, d_out, r):
 
 
 def new_adapters_workspace(M, d_in, d_out, r):
-    return _torch.empty(adapters_workspace_bytes(M, d_in, d_out, r), dtype=_torch.uint8, device="cuda")
+    return _torch.zeros(adapters_workspace_bytes(M, d_in, d_out, r), dtype=_torch.uint8, device="cuda")
 
 
 def linear_adapters(x, A_pool, B_pool, A_scales, B_scales, ranks, scalings, adapter_of_row, base, y, M, d_in, d_out, r,

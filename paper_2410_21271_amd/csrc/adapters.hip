@@ -68,6 +68,22 @@ __device__ __forceinline__ int ranges_of(const AdapterArgs& a, int pairs)
     return ks;
 }
 
+// The two launches as one, for up to a window of rows: the workgroups of the second part request their first tiles of B and then wait for t, which the first part
+// (lower indices, and it never waits) hands over past the caches of an XCD, eight bytes at a time (relaxed, agent scope), with a count of its finished units for each pair (at the
+// pair's first row).  The last wavefront to have read a pair's t clears its counts.
+constexpr int READY = 64, TAKEN = 1, LINE = 32, HEADER = READY + LINE * WINDOW;       // words before t (word HDR_ERROR: a wait expired); a pair's two counts in a line of their own
+__device__ __forceinline__ void put_t(float* p, float x, float y)
+{
+    const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
+    __hip_atomic_store((unsigned long long*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_t(const float* p)
+{
+    const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+__device__ __forceinline__ unsigned add_one(unsigned* p) { return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 // rank of a pair in whole k-tiles of B
 __device__ __forceinline__ int rank_of(const AdapterArgs& a, int id, int step)
 {
@@ -97,17 +113,23 @@ struct Chunk {
     h8 x[4];
 };
 
-template <int FA, int RB>
-__global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, int step)
+template <int RB>
+struct DownSpace {
+    static constexpr int XLD = 128 + 8;
+    int lists[NW][WINDOW];
+    __attribute__((aligned(16))) _Float16 xs[NW][16 * XLD];
+    __attribute__((aligned(16))) float red[NW * RB * 256];
+};
+
+// workgroup g of the a.down_wgs that a window has
+template <int FA, int RB, bool ONE>
+__device__ __forceinline__ void down(const AdapterArgs& a, int step, int window, int g, DownSpace<RB>& space)
 {
-    constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT, XLD = 128 + 8;
-    __shared__ int lists[NW][WINDOW];
-    __shared__ __attribute__((aligned(16))) _Float16 xs[NW][16 * XLD];
-    __shared__ __attribute__((aligned(16))) float red[NW * RB * 256];
+    constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT, XLD = DownSpace<RB>::XLD;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    const int window = blockIdx.x / a.down_wgs, g = blockIdx.x - window * a.down_wgs;
-    int* list = lists[wave];
-    _Float16* xw = xs[wave];
+    int* list = space.lists[wave];
+    _Float16* xw = space.xs[wave];
+    float* red = space.red;
     const Window win = window_of(a, window * WINDOW, false);
     const int pairs = __popcll(win.leaders), kss = ranges_of(a, pairs), chunks = a.d_in / 128;
     for (int unit = g; unit < pairs * a.rgroups * kss; unit += a.down_wgs) {
@@ -193,7 +215,7 @@ __global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, i
                 add(even);
             }
         }
-        if (phases == 1) {
+        if (!ONE && phases == 1) {
 #pragma unroll
             for (int q = 0; q < RB; ++q)
 #pragma unroll
@@ -208,24 +230,70 @@ __global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, i
 #pragma unroll
         for (int q = 0; q < RB; ++q) *(f4*)(red + ((wave * RB + q) * 64 + lane) * 4) = acc[q];
         __syncthreads();
-        for (int e = threadIdx.x; e < tbs * RB * 256; e += THREADS) {
-            // consecutive threads: consecutive ranks of one row
-            const int col = e % 16, q = e / 16 % RB, slot = e / (16 * RB), b = slot / 16, l = 16 * (slot % 16 / 4) + col, i = slot % 4;
+        for (int e = threadIdx.x; e < tbs * RB * 128; e += THREADS) {
+            // consecutive threads: consecutive pairs of ranks of one row
+            const int col = 2 * (e % 8), q = e / 8 % RB, slot = e / (8 * RB), b = slot / 16, l = 16 * (slot % 16 / 4) + col, i = slot % 4;
             if (slot >= count || q >= blocks) continue;
-            float sum = 0.f;
-            for (int p = 0; p < phases; ++p) sum += red[(((p * tbs + b) * RB + q) * 64 + l) * 4 + i];
-            a.t[((size_t)ks * a.M + row0 + list[slot]) * a.r + 16 * (rb0 + q) + col] = sum;
+            float sum = 0.f, sum1 = 0.f;
+            for (int p = 0; p < phases; ++p) {
+                const float* src = red + (((p * tbs + b) * RB + q) * 64 + l) * 4 + i;
+                sum += src[0];
+                sum1 += src[4];
+            }
+            float* dst = a.t + ((size_t)ks * a.M + row0 + list[slot]) * a.r + 16 * (rb0 + q) + col;
+            if constexpr (ONE) put_t(dst, sum, sum1);
+            else *(float2*)dst = make_float2(sum, sum1);
+        }
+        if constexpr (ONE) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) add_one(a.header + READY + LINE * first_row);
         }
     }
+}
+
+template <int FA, int RB>
+__global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, int step)
+{
+    __shared__ DownSpace<RB> space;
+    const int window = blockIdx.x / a.down_wgs;
+    down<FA, RB, false>(a, step, window, blockIdx.x - window * a.down_wgs, space);
 }
 
 // Second launch.  A workgroup: the leaders' rows x a slab of outputs.  A wavefront keeps t of its 16 rows in registers, as the second operand (NK fragments of 32
 // ranks, high and low halves), and takes 16 PB outputs at a time: B's tiles are the first operand.  What is row-major (t on its way in, base and y) passes through LDS, a part of
 // its own for each wavefront and no barrier, so that it is moved 16 bytes a lane, consecutive lanes along a row: straight to and from the operands' places it is
 // 16 rows an instruction, 64 accesses of the L1 instead of 16.
+// Waits for, and gives up, t of the pair that row `first` leads; need: the units that make it up, readers: the wavefronts that read it
+struct Wait {
+    int first;
+    unsigned need, readers;
+    __device__ __forceinline__ void ready(const AdapterArgs& a) const
+    {
+        bool there = need == 0;
+        for (int spins = 0; !there && spins <= a.spin_limit; ++spins) {
+            unsigned v = 0;
+            if ((threadIdx.x & 63) == 0) v = ld_relaxed(a.header + READY + LINE * first);
+            there = (unsigned)__builtin_amdgcn_readfirstlane(v) >= need;
+            if (!there) __builtin_amdgcn_s_sleep(20);        // (looking more often delays the counting: 1 row 4096 -> 14336 13.9 us with 2, 10.9)
+        }
+        if (!there && (threadIdx.x & 63) == 0) __hip_atomic_store(a.header + HDR_ERROR, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("" ::: "memory");                    // nothing of t is requested before
+    }
+    __device__ __forceinline__ void taken(const AdapterArgs& a) const
+    {
+        if (need == 0 || (threadIdx.x & 63) != 0) return;
+        asm volatile("" ::: "memory");
+        unsigned* counts = a.header + READY + LINE * first;
+        if (add_one(counts + TAKEN) + 1 < readers) return;
+        __hip_atomic_store(counts, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(counts + TAKEN, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+};
+
 // SHARE (many rows): the wavefronts have a block of rows each and all outputs of the slab, so that B's tiles are requested once a workgroup, a quarter by each, and pass through LDS
 // too, two steps of them (requested by every wavefront they are 470 MB from L2 for 2048 rows, 4096 -> 14336, rank 128).
-template <int FE, int NK, bool SHARE>
+template <int FE, int NK, bool SHARE, bool ONE>
 struct Up {
     static constexpr int WORDS = Fmt<FE>::WORDS, KT = Fmt<FE>::KT, NF = KT / 32, TILES = NK / NF;
     static constexpr int PB = NK <= 4 || (FE != S_F16 && NK <= 8) ? 4 : 2;       // blocks of 16 outputs at a time
@@ -237,12 +305,15 @@ struct Up {
     typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
     // tb: this wavefront's first block of rows; it takes every `phases`-th step of 16 PB outputs from `phase` on
-    static __device__ __forceinline__ void run(const AdapterArgs& a, int id, int rank, int row0, const int* list, int count, int tb, int phase, int phases, int first_block, int end, int kss, float* mine, uint32_t* stage)
+    static __device__ __forceinline__ void run(const AdapterArgs& a, int id, int rank, int row0, const int* list, int count, int tb, int phase, int phases, int first_block, int end, int kss, float* mine, uint32_t* stage, const Wait& wait)
     {
         const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
         const int ntk = a.r / KT, nt = rank / KT, here = count - 16 * tb;
         int rb = first_block + PB * phase;
-        if (!SHARE && (rb >= end || here <= 0)) return;
+        if (!SHARE && (rb >= end || here <= 0)) {
+            if constexpr (ONE) wait.taken(a);
+            return;
+        }
         const int wave = SHARE ? tb : 0;
         // the rows that this lane moves
         const int piece = lane % LPR;
@@ -293,6 +364,7 @@ struct Up {
         load_rest(rb);
         __builtin_amdgcn_sched_barrier(0);
 
+        if constexpr (ONE) wait.ready(a);
         // t of the rows, summed over the ranges in order, COLS columns at a time
         h8 high[NK], low[NK];
         float t[NK][8], big = 0.f;
@@ -304,16 +376,31 @@ struct Up {
 #pragma unroll
             for (int i = 0; i < TIN; ++i) sum[i] = f4{0.f, 0.f, 0.f, 0.f};
             const int col = c * COLS + 4 * (lane % TL);
-#pragma clang loop unroll(disable)
-            for (int ks = 0; ks < kss; ++ks) {
-                f4 in[TIN];
-#pragma unroll
-                for (int i = 0; i < TIN; ++i) {
-                    const int r = lane / TL + TRI * i;
-                    in[i] = *(const f4*)(a.t + ((size_t)ks * a.M + row0 + list[r < here ? 16 * tb + r : 0]) * a.r + (col < rank ? col : 0));
+            auto fetch = [&](int ks, int r) {
+                const float* src = a.t + ((size_t)ks * a.M + row0 + list[r < here ? 16 * tb + r : 0]) * a.r + (col < rank ? col : 0);
+                if constexpr (ONE) {
+                    const float2 lo = get_t(src), hi = get_t(src + 2);
+                    return f4{lo.x, lo.y, hi.x, hi.y};
+                } else {
+                    return *(const f4*)src;
                 }
+            };
+            if (ONE && here <= TRI) {
+                // one instruction a range: all of them at a time
+                f4 in[MAX_KSPLIT];
 #pragma unroll
-                for (int i = 0; i < TIN; ++i) sum[i] += in[i];
+                for (int ks = 0; ks < MAX_KSPLIT; ++ks) in[ks] = fetch(ks < kss ? ks : 0, lane / TL);
+#pragma unroll
+                for (int ks = 0; ks < MAX_KSPLIT; ++ks) sum[0] += ks < kss ? in[ks] : f4{0.f, 0.f, 0.f, 0.f};
+            } else {
+#pragma clang loop unroll(disable)
+                for (int ks = 0; ks < kss; ++ks) {
+                    f4 in[TIN];
+#pragma unroll
+                    for (int i = 0; i < TIN; ++i) in[i] = fetch(ks, lane / TL + TRI * i);
+#pragma unroll
+                    for (int i = 0; i < TIN; ++i) sum[i] += in[i];
+                }
             }
 #pragma unroll
             for (int i = 0; i < TIN; ++i) {
@@ -332,6 +419,7 @@ struct Up {
                 }
             }
         }
+        if constexpr (ONE) wait.taken(a);                 // (t is in LDS)
         big = fmaxf(big, __shfl_xor(big, 16, 64));
         big = fmaxf(big, __shfl_xor(big, 32, 64));
         int ex = (int)(__float_as_uint(big) >> 23) - 127;  // exponent of the row's largest value
@@ -384,9 +472,9 @@ struct Up {
                     }
                 }
             const int col = 16 * rb + 8 * piece;
-            // (without a pair the tiles are another's: whatever they give, nothing is added)
+            // (without a pair the tiles are another's: whatever they give, -0 is added, which leaves base as it is)
 #pragma unroll
-            for (int p = 0; p < PB; ++p) *(f4*)(mine + n * LD + 16 * p + 4 * j) = rank ? acc[p] * back : f4{0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < PB; ++p) *(f4*)(mine + n * LD + 16 * p + 4 * j) = rank ? acc[p] * back : f4{-0.f, -0.f, -0.f, -0.f};
             h8 y[INS];
 #pragma unroll
             for (int i = 0; i < INS; ++i) {
@@ -416,15 +504,19 @@ struct Up {
 };
 
 template <int FE, int NK, bool SHARE>
-__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const AdapterArgs a)
+struct UpSpace {
+    int lists[NW][WINDOW];
+    __attribute__((aligned(16))) float space[NW][Up<FE, NK, SHARE, false>::LDS];
+    __attribute__((aligned(16))) uint32_t stage[Up<FE, NK, SHARE, false>::STAGE];
+};
+
+// workgroup g of the a.up_wgs that a window has; rb_ranks: ranks of a unit of the first part (ONE)
+template <int FE, int NK, bool SHARE, bool ONE>
+__device__ __forceinline__ void up(const AdapterArgs& a, int window, int g, int rb_ranks, UpSpace<FE, NK, SHARE>& s)
 {
-    typedef Up<FE, NK, SHARE> Rows;
-    __shared__ int lists[NW][WINDOW];
-    __shared__ __attribute__((aligned(16))) float space[NW][Rows::LDS];
-    __shared__ __attribute__((aligned(16))) uint32_t stage[Rows::STAGE];
+    typedef Up<FE, NK, false, ONE> Rows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int window = blockIdx.x / a.up_wgs, g = blockIdx.x - window * a.up_wgs;
-    int* list = lists[wave];
+    int* list = s.lists[wave];
     // (rows without a pair have nothing to add; with y apart from base they are copied)
     const Window win = window_of(a, window * WINDOW, a.base != a.y);
     const int pairs = __popcll(win.leaders), kss = ranges_of(a, __popcll(win.leaders & __ballot(win.id >= 0)));
@@ -436,15 +528,37 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const Adap
         const int id = __builtin_amdgcn_readlane(win.id, first_row);
         const unsigned long long rows = rows_at(win, first_row);
         const int rank = rank_of(a, id, Fmt<FE>::KT), count = __popcll(rows), first = slab * size, end = first + size < blocks ? first + size : blocks;
-        if ((rank == 0 && a.base == a.y) || first >= end) continue;
+        const Wait wait{first_row, (unsigned)((rank + rb_ranks - 1) / rb_ranks * kss), (unsigned)(slabs * NW)};
+        if ((rank == 0 && a.base == a.y) || (!ONE && first >= end)) continue;      // (ONE: every wavefront of a pair's units gives its t up)
         list_rows(rows, lane, list);
         if (SHARE && count > 16) {
-            Up<FE, NK, SHARE>::run(a, id, rank, win.row0, list, count, wave, 0, 1, first, end, kss, space[wave], stage);
+            Up<FE, NK, SHARE, false>::run(a, id, rank, win.row0, list, count, wave, 0, 1, first, end, kss, s.space[wave], s.stage, wait);
         } else {
             const int tbs = row_blocks(count);
-            Up<FE, NK, false>::run(a, id, rank, win.row0, list, count, wave % tbs, wave / tbs, NW / tbs, first, end, kss, space[wave], stage);
+            Rows::run(a, id, rank, win.row0, list, count, wave % tbs, wave / tbs, NW / tbs, first, end, kss, s.space[wave], s.stage, wait);
         }
     }
+}
+
+template <int FE, int NK, bool SHARE>
+__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const AdapterArgs a)
+{
+    __shared__ UpSpace<FE, NK, SHARE> space;
+    const int window = blockIdx.x / a.up_wgs;
+    up<FE, NK, SHARE, false>(a, window, blockIdx.x - window * a.up_wgs, 1, space);
+}
+
+template <int FA, int RB, int FE, int NK>
+__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void adapters_kernel(const AdapterArgs a, int step)
+{
+    __shared__ union Space {
+        DownSpace<RB> first;
+        UpSpace<FE, NK, false> second;
+        __device__ Space() {}
+    } space;
+    const int g = blockIdx.x;
+    if (g < a.down_wgs) down<FA, RB, true>(a, step, 0, g, space.first);
+    else up<FE, NK, false, true>(a, 0, g - a.down_wgs, 16 * RB, space.second);
 }
 
 constexpr int MANY = 512;                      // rows
@@ -463,35 +577,44 @@ hipError_t start_down(const AdapterArgs& a, unsigned grid, int rblocks, int step
 }
 
 template <int FE, int NK>
-hipError_t start_up(const AdapterArgs& a, int windows, hipStream_t stream)
+hipError_t start_up(const AdapterArgs& a, int windows, int rblocks, int step, hipStream_t stream)
 {
-    // (the kernel that can share has less LDS left for others)
-    if (a.M >= MANY) up_kernel<FE, NK, true><<<(unsigned)windows * a.up_wgs, THREADS, 0, stream>>>(a);
-    else up_kernel<FE, NK, false><<<(unsigned)windows * a.up_wgs, THREADS, 0, stream>>>(a);
+    if (windows == 1) {
+        constexpr int FA = FE == S_Q4S64 ? S_Q4S128 : FE;
+        const unsigned grid = (unsigned)(a.down_wgs + a.up_wgs);
+        if (rblocks == 1) adapters_kernel<FA, 1, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+        else adapters_kernel<FA, 4, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+    } else {
+        const unsigned grid = (unsigned)windows * a.up_wgs;
+        // (the kernel that can share has less LDS left for others)
+        if (a.M >= MANY) up_kernel<FE, NK, true><<<grid, THREADS, 0, stream>>>(a);
+        else up_kernel<FE, NK, false><<<grid, THREADS, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
 template <int FE>
-hipError_t start_up(const AdapterArgs& a, int windows, hipStream_t stream)
+hipError_t start_up(const AdapterArgs& a, int windows, int rblocks, int step, hipStream_t stream)
 {
     if constexpr (FE == S_Q4S64) {
-        return start_up<FE, 2>(a, windows, stream);
+        return start_up<FE, 2>(a, windows, rblocks, step, stream);
     } else {
-        if (a.r <= 128) return start_up<FE, 4>(a, windows, stream);
-        if (a.r <= 256) return start_up<FE, 8>(a, windows, stream);
-        return a.r <= 384 ? start_up<FE, 12>(a, windows, stream) : start_up<FE, 16>(a, windows, stream);
+        if (a.r <= 128) return start_up<FE, 4>(a, windows, rblocks, step, stream);
+        if (a.r <= 256) return start_up<FE, 8>(a, windows, rblocks, step, stream);
+        return a.r <= 384 ? start_up<FE, 12>(a, windows, rblocks, step, stream) : start_up<FE, 16>(a, windows, rblocks, step, stream);
     }
 }
 
 }  // namespace
 
-size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r) { return (size_t)MAX_KSPLIT * M * r * sizeof(float); }
+size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r) { return HEADER * sizeof(uint32_t) + (size_t)MAX_KSPLIT * M * r * sizeof(float); }
 
 hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
 {
     constexpr int LAUNCH = 1 << 16;                       // rows of a launch
     for (int m0 = 0; m0 < args.M; m0 += LAUNCH) {
         AdapterArgs a = args;
+        a.t = (float*)(a.header + HEADER);
         a.M = args.M - m0 < LAUNCH ? args.M - m0 : LAUNCH;
         a.x += (size_t)m0 * a.d_in;
         a.ids += m0;
@@ -499,22 +622,24 @@ hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
         if (a.base) a.base += (size_t)m0 * a.d_out;
         const int windows = (a.M + WINDOW - 1) / WINDOW, nr = a.r / 16, rblocks = nr < 4 || (a.M == 1 && nr <= 8) ? 1 : 4;
         a.rgroups = (nr + rblocks - 1) / rblocks;
-        // one workgroup a compute unit with two chunks in its registers; two
+        // First part: one workgroup a compute unit, with two chunks in its registers.  Second: two, or one beside those of the first
         a.down_wgs = windows < 256 ? 256 / windows : 1;
-        a.up_wgs = windows < 512 ? 512 / windows : 1;
+        a.up_wgs = windows == 1 ? 256 : (windows < 512 ? 512 / windows : 1);
         if (a.M < WINDOW) {                               // no more than its rows have work for
             const int down = a.M * a.rgroups * MAX_KSPLIT, up = a.M * ((a.d_out / 16 + 7) / 8);
             a.down_wgs = down < a.down_wgs ? down : a.down_wgs;
             a.up_wgs = up < a.up_wgs ? up : a.up_wgs;
         }
         const int step = fe == S_F16 ? 32 : (fe == S_Q4S64 ? 64 : 128);
-        const unsigned grid = (unsigned)windows * a.down_wgs;
-        hipError_t e = fa == S_F16 ? start_down<S_F16>(a, grid, rblocks, step, stream)
-                                   : (fa == S_Q4S128 ? start_down<S_Q4S128>(a, grid, rblocks, step, stream) : start_down<S_Q3S128>(a, grid, rblocks, step, stream));
-        if (e != hipSuccess) return e;
-        e = fe == S_F16 ? start_up<S_F16>(a, windows, stream)
-                        : (fe == S_Q4S64 ? start_up<S_Q4S64>(a, windows, stream)
-                                         : (fe == S_Q4S128 ? start_up<S_Q4S128>(a, windows, stream) : start_up<S_Q3S128>(a, windows, stream)));
+        if (windows > 1) {
+            const unsigned grid = (unsigned)windows * a.down_wgs;
+            const hipError_t e = fa == S_F16 ? start_down<S_F16>(a, grid, rblocks, step, stream)
+                                             : (fa == S_Q4S128 ? start_down<S_Q4S128>(a, grid, rblocks, step, stream) : start_down<S_Q3S128>(a, grid, rblocks, step, stream));
+            if (e != hipSuccess) return e;
+        }
+        const hipError_t e = fe == S_F16 ? start_up<S_F16>(a, windows, rblocks, step, stream)
+                                         : (fe == S_Q4S64 ? start_up<S_Q4S64>(a, windows, rblocks, step, stream)
+                                                          : (fe == S_Q4S128 ? start_up<S_Q4S128>(a, windows, rblocks, step, stream) : start_up<S_Q3S128>(a, windows, rblocks, step, stream)));
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

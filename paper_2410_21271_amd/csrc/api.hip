@@ -475,6 +475,10 @@ size_t workspace_room(int M, int d_in, int r)
 
 }  // namespace
 
+namespace eora {
+int spin_limit() { return g_spin_limit; }
+}  // namespace eora
+
 extern "C" {
 
 size_t eora_workspace_bytes(int M, int d_in, int d_out, int r)

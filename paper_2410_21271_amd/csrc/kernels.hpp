@@ -32,6 +32,7 @@ constexpr int MAX_KCN = 8;                      // k-ranges of the down-projecti
 // back through eora_debug_last_launch() (tests assert that a shape reaches the instantiation it is meant to
 // cover).  `fmt` is a printf format for up to eight ints and must be a string literal.  Not synchronised.
 void note_launch(const char* fmt, int a = 0, int b = 0, int c = 0, int d = 0, int e = 0, int f = 0, int g = 0, int h = 0);
+int spin_limit();                                    // iterations of a bounded wait in a kernel (eora_debug_set_spin_limit)
 void note_prefill(const char* fmt, int tokens);      // which of the kernels for many tokens, and its tokens per workgroup
 
 // General kernel of the quantised backbone (wideq.hip): 5 and more tokens, and the shapes the decode kernel does not take.

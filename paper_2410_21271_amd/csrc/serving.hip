@@ -70,7 +70,8 @@ int eora_linear_adapters(const void* x, const void* A_pool, const void* B_pool, 
     a.ids = (const int*)adapter_of_row;
     a.base = (const _Float16*)base;
     a.y = (_Float16*)y;
-    a.t = (float*)workspace;
+    a.header = (uint32_t*)workspace;
+    a.spin_limit = spin_limit();
     a.M = M;
     a.d_in = d_in;
     a.d_out = d_out;

@@ -63,7 +63,9 @@ struct AdapterArgs {
     const int* ids;                 // M
     const _Float16* base;           // M x d_out, or null: zeros
     _Float16* y;                    // M x d_out
-    float* t;                       // ranges x M x r partial sums of x A^T
+    uint32_t* header;               // counts of the one-launch form
+    int spin_limit;
+    float* t;                       // (behind the header; set by the launcher) ranges x M x r partial sums of x A^T
     int M, d_in, d_out, r, n;
     int rgroups, down_wgs, up_wgs;          // groups of ranks; workgroups of a window in either launch (set by the launcher)
 };

@@ -194,6 +194,42 @@ def test_adapters_large_and_small_t(gpu, bits):
     check_adapters(gpu, pool, x[[1, 2, 3, 4]], np.zeros(4, int), [1024.0], base[:4])
 
 
+def test_adapters_expired_wait(gpu):
+    """With every wait counted as expired the call ends and says so; a workspace zeroed again works as before."""
+    import torch
+    rng = np.random.default_rng(15)
+    pool = Pool(gpu, 16, 512, 256, 64, 3, 16)
+    x, base, ids = rng.normal(0, 1, (9, 512)).astype(np.float16), rng.normal(0, 1, (9, 256)).astype(np.float16), rng.integers(-1, 3, 9)
+    ws = gpu.new_adapters_workspace(9, 512, 256, 64)
+    want = run_adapters(gpu, pool, x, ids, None, base, ws=ws)
+    assert gpu.workspace_error(ws) == 0
+    gpu.debug_set_spin_limit(-1)
+    try:
+        run_adapters(gpu, pool, x, ids, None, base, ws=ws)
+        assert gpu.workspace_error(ws) == -8
+    finally:
+        gpu.debug_set_spin_limit(1 << 22)
+    ws.zero_()
+    for _ in range(3):
+        assert np.array_equal(run_adapters(gpu, pool, x, ids, None, base, ws=ws).view(np.uint16), want.view(np.uint16))
+    assert gpu.workspace_error(ws) == 0
+    assert not ws.view(torch.int32)[:64 + 32 * 64].any()     # the counts are left at zero
+
+
+def test_adapters_one_workspace_for_calls_of_all_sizes(gpu):
+    rng = np.random.default_rng(17)
+    pool = Pool(gpu, 18, 384, 272, 128, 5, 16, [128, 0, 32, 96, 64])
+    ws = gpu.new_adapters_workspace(600, 384, 272, 128)
+    x, base = rng.normal(0, 1, (600, 384)).astype(np.float16), rng.normal(0, 1, (600, 272)).astype(np.float16)
+    base[:, 3] = -0.0
+    for M in (1, 64, 600, 17, 65, 2, 64):
+        ids = rng.integers(-1, 5, M)
+        y = check_adapters(gpu, pool, x[:M], ids, None, base[:M], ws=ws)
+        none = (ids < 0) | (ids == 1)
+        assert np.array_equal(y[none].view(np.uint16), base[:M][none].view(np.uint16))
+    assert gpu.workspace_error(ws) == 0
+
+
 def test_adapters_infinities_stay_in_their_row(gpu):
     rng = np.random.default_rng(11)
     pool = Pool(gpu, 12, 256, 32, 32, 2, 16)
