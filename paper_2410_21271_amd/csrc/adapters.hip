@@ -2,8 +2,9 @@
 //
 //      y[m] = base[m] + s_a (x[m] A_a^T) B_a^T            a = adapter of row m, from a pool of any size
 //
-// Two launches: t = x A^T (fp32 partial sums of ranges of the contraction), then y from t and B.  Only the pairs that rows select are read,
-// each once per window of 64 rows, in the stored tiles of the layer kernels.
+// Two parts: t = x A^T (fp32 partial sums of ranges of the contraction), then y from t and B.  One launch for up to 64 rows, where each launch would be half the time or more
+// (1 row 4096 -> 4096, rank 16: 7.5 us in one, 10.1 in two), two beyond.  Only the pairs that rows select are read, each once per window of 64 rows, in the stored
+// tiles of the layer kernels.
 //
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
 // of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight.  With many rows of one pair, y's own traffic bounds it.
@@ -57,8 +58,8 @@ __device__ __forceinline__ unsigned long long rows_at(const Window& w, int first
     return (unsigned long long)hi << 32 | lo;
 }
 
-// Ranges of the contraction in the first launch, for a window with so many pairs: as many as there are workgroups for, of a chunk a wavefront at least, and four at most where
-// pairs have more than a few rows (the second launch reads the parts of t of every row once a slab).
+// Ranges of the contraction in the first part, for a window with so many pairs: as many as there are workgroups for, of a chunk a wavefront at least, and four at most where
+// pairs have more than a few rows (the second part reads the parts of t of every row once a slab).
 constexpr int MAX_KSPLIT = 8;
 __device__ __forceinline__ int ranges_of(const AdapterArgs& a, int pairs)
 {
@@ -68,7 +69,7 @@ __device__ __forceinline__ int ranges_of(const AdapterArgs& a, int pairs)
     return ks;
 }
 
-// The two launches as one, for up to a window of rows: the workgroups of the second part request their first tiles of B and then wait for t, which the first part
+// Both parts in one launch, for up to a window of rows: the workgroups of the second part request their first tiles of B and then wait for t, which the first part
 // (lower indices, and it never waits) hands over past the caches of an XCD, eight bytes at a time (relaxed, agent scope), with a count of its finished units for each pair (at the
 // pair's first row).  The last wavefront to have read a pair's t clears its counts.
 constexpr int READY = 64, TAKEN = 1, LINE = 32, HEADER = READY + LINE * WINDOW;       // words before t (word HDR_ERROR: a wait expired); a pair's two counts in a line of their own
@@ -103,7 +104,7 @@ __device__ __forceinline__ void list_rows(unsigned long long rows, int lane, int
 // Wavefronts of a workgroup: `blocks` of them (1, 2 or 4) have a block of 16 rows each, the others share their work
 __device__ __forceinline__ int row_blocks(int count) { return count <= 16 ? 1 : (count <= 32 ? 2 : 4); }
 
-// First launch.  A workgroup: 16 RB ranks of the rows of a pair x one range of the contraction, in chunks of 128 columns.  x passes through LDS (a part of its own for each
+// First part.  A workgroup: 16 RB ranks of the rows of a pair x one range of the contraction, in chunks of 128 columns.  x passes through LDS (a part of its own for each
 // wavefront) so that its rows are read 256 bytes at a time.
 template <int FA, int RB>
 struct Chunk {
@@ -260,10 +261,6 @@ __global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, i
     down<FA, RB, false>(a, step, window, blockIdx.x - window * a.down_wgs, space);
 }
 
-// Second launch.  A workgroup: the leaders' rows x a slab of outputs.  A wavefront keeps t of its 16 rows in registers, as the second operand (NK fragments of 32
-// ranks, high and low halves), and takes 16 PB outputs at a time: B's tiles are the first operand.  What is row-major (t on its way in, base and y) passes through LDS, a part of
-// its own for each wavefront and no barrier, so that it is moved 16 bytes a lane, consecutive lanes along a row: straight to and from the operands' places it is
-// 16 rows an instruction, 64 accesses of the L1 instead of 16.
 // Waits for, and gives up, t of the pair that row `first` leads; need: the units that make it up, readers: the wavefronts that read it
 struct Wait {
     int first;
@@ -291,6 +288,11 @@ struct Wait {
     }
 };
 
+// Second part.  A workgroup: the leaders' rows x a slab of outputs.  A wavefront keeps t of its 16 rows in registers, as the second operand (NK fragments of 32
+// ranks, high and low halves), and takes 16 PB outputs at a time: B's tiles are the first operand.  What is row-major (t on its way in, base and y) passes through LDS, a part of
+// its own for each wavefront and no barrier, so that it is moved 16 bytes a lane, consecutive lanes along a row: straight to and from the operands' places it is
+// 16 rows an instruction, 64 accesses of the L1 instead of 16.
+//
 // SHARE (many rows): the wavefronts have a block of rows each and all outputs of the slab, so that B's tiles are requested once a workgroup, a quarter by each, and pass through LDS
 // too, two steps of them (requested by every wavefront they are 470 MB from L2 for 2048 rows, 4096 -> 14336, rank 128).
 template <int FE, int NK, bool SHARE, bool ONE>
@@ -573,7 +575,9 @@ hipError_t start_down(const AdapterArgs& a, unsigned grid, int step, hipStream_t
 template <int FA>
 hipError_t start_down(const AdapterArgs& a, unsigned grid, int rblocks, int step, hipStream_t stream)
 {
-    return rblocks == 1 ? start_down<FA, 1>(a, grid, step, stream) : start_down<FA, 4>(a, grid, step, stream);
+    if constexpr (FA == S_F16)                            // (codes have ranks of 64 or more)
+        if (rblocks == 1) return start_down<FA, 1>(a, grid, step, stream);
+    return start_down<FA, 4>(a, grid, step, stream);
 }
 
 template <int FE, int NK>
@@ -582,8 +586,12 @@ hipError_t start_up(const AdapterArgs& a, int windows, int rblocks, int step, hi
     if (windows == 1) {
         constexpr int FA = FE == S_Q4S64 ? S_Q4S128 : FE;
         const unsigned grid = (unsigned)(a.down_wgs + a.up_wgs);
-        if (rblocks == 1) adapters_kernel<FA, 1, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
-        else adapters_kernel<FA, 4, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+        if constexpr (NK <= 4)
+            if (rblocks == 1) {
+                adapters_kernel<FA, 1, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+                return hipGetLastError();
+            }
+        adapters_kernel<FA, 4, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
     } else {
         const unsigned grid = (unsigned)windows * a.up_wgs;
         // (the kernel that can share has less LDS left for others)

@@ -372,16 +372,13 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
-// Tiles of 8 KiB two at a time in registers, larger ones one: eight wavefronts a compute unit have 64 to 128 KiB in flight.
-template <int DIM, int BITS>
-constexpr int tiles_ahead() { return 1; }
-
-// wavefronts a SIMD: what the registers of an instantiation leave room for
-template <int DIM, int BITS>
+// Wavefronts a SIMD: what the registers leave room for, which hold one tile and, at D = 256, 64 words of O.  Eight wavefronts a compute unit have 64 to 128 KiB
+// in flight; a second tile in registers, for half the wavefronts, measured 3 to 8 % more.
+template <int DIM>
 constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
 
 template <int DIM, int BITS>
-__global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kernel(const AttendArgs a)
+__global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const AttendArgs a)
 {
     constexpr int NT = DIM / 32;               // k-steps of the first product
     constexpr int W = DIM / 16;                // columns of V a lane holds, blocks of O^T
@@ -390,7 +387,6 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
     constexpr int VW = W * BYTES / 4;          // words of a value row a lane holds
     typedef uint32_t words __attribute__((ext_vector_type(VW < 4 ? VW : 4)));
     constexpr int VL = VW < 4 ? 1 : VW / 4;    // loads of a value row
-    constexpr int AHEAD = tiles_ahead<DIM, BITS>();
 
     __shared__ int scratch[NW];
     __shared__ float red_m[NW][16], red_l[NW][16];
@@ -447,28 +443,26 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
             const unsigned lo = __builtin_amdgcn_readlane((unsigned)rows_of, from), hi = __builtin_amdgcn_readlane((unsigned)(rows_of >> 32), from);
             return (long long)(((unsigned long long)hi << 32) | lo);
         };
-        // AHEAD tiles in registers.  A tile's registers are requested anew (for the tile AHEAD further on) as soon as it has no more use for them; behind the
+        // One tile in registers.  Its keys' are requested anew, for the next tile, as soon as the scores are there, its values' behind the second product; behind the
         // last tile the requests go on, all lanes to one place: a request behind a branch would make every wait one for all requests.
-        struct Held {
-            u4 k[2][KL];
-            words v[8][VL];
-            long long row[2];
-        } held[AHEAD];
+        u4 tk[2][KL];
+        words tv[8][VL];
+        long long rows[2];
         auto find = [&](int i, long long (&row)[2]) {
             row[0] = half_row(i, 0);
             row[1] = half_row(i, 1);
         };
         const unsigned k_at = (unsigned)(n * DIM * BYTES + 16 * j), v_at = (unsigned)(4 * j * DIM * BYTES + n * W * BYTES);
-        auto load_k = [&](Held& t, const long long (&row)[2], unsigned all) {
+        auto load_k = [&](const long long (&row)[2], unsigned all) {
             const unsigned off = k_at & all;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const char* base = (const char*)a.pages_k + (size_t)(row[s] < 0 ? 0 : row[s]) * (DIM * BYTES);
 #pragma unroll
-                for (int e = 0; e < KL; ++e) t.k[s][e] = *(const u4*)(base + off + 64 * e);
+                for (int e = 0; e < KL; ++e) tk[s][e] = *(const u4*)(base + off + 64 * e);
             }
         };
-        auto load_v = [&](Held& t, const long long (&row)[2], unsigned all) {
+        auto load_v = [&](const long long (&row)[2], unsigned all) {
             const unsigned off = v_at & all;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -476,7 +470,7 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int v = 0; v < VL; ++v) t.v[4 * s + i][v] = *(const words*)(base + off + i * DIM * BYTES + 16 * v);
+                    for (int v = 0; v < VL; ++v) tv[4 * s + i][v] = *(const words*)(base + off + i * DIM * BYTES + 16 * v);
             }
         };
         if (mine > 0) look(0);
@@ -497,14 +491,11 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
         for (int b = 0; b < W; ++b) O[b] = f4{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
         if (mine > 0) {
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                find(i, held[i].row);
-                load_k(held[i], held[i].row, i < mine ? ~0u : 0u);
-                load_v(held[i], held[i].row, i < mine ? ~0u : 0u);
-            }
+            find(0, rows);
+            load_k(rows, ~0u);
+            load_v(rows, ~0u);
         }
-        auto tile = [&](int i, Held& t) {
+        for (int i = 0; i < mine; ++i) {
             // scores
             f4 S[2];
 #pragma unroll
@@ -514,9 +505,9 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
                 for (int e = 0; e < NT; ++e) {
                     Frag k;
                     if constexpr (BITS == 16) {
-                        k.q = t.k[s][e];
+                        k.q = tk[s][e];
                     } else {
-                        const uint32_t w0 = t.k[s][e / 2][2 * (e % 2)], w1 = t.k[s][e / 2][2 * (e % 2) + 1];
+                        const uint32_t w0 = tk[s][e / 2][2 * (e % 2)], w1 = tk[s][e / 2][2 * (e % 2) + 1];
                         k.u[0] = two_codes<false>(w0);
                         k.u[1] = two_codes<true>(w0);
                         k.u[2] = two_codes<false>(w1);
@@ -525,13 +516,13 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
                     S[s] = mfma16(k.v, qf[e].v, S[s]);
                 }
             }
-            if (((i + AHEAD) & 31) == 0) look(i + AHEAD);
-            const unsigned all = i + AHEAD < mine ? ~0u : 0u;
+            if (((i + 1) & 31) == 0) look(i + 1);
+            const unsigned all = i + 1 < mine ? ~0u : 0u;
             long long next[2];
-            find(i + AHEAD, next);
-            load_k(t, next, all);
+            find(i + 1, next);
+            load_k(next, all);
             const int key0 = (t0 + step * i) * TILE;
-            const bool whole = key0 >= span.lo && key0 + TILE <= span.hi && t.row[0] >= 0 && t.row[1] >= 0;
+            const bool whole = key0 >= span.lo && key0 + TILE <= span.hi && rows[0] >= 0 && rows[1] >= 0;
             float p[8];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -544,7 +535,7 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = key0 + 16 * s + 4 * j + e;
-                        if (key < span.lo || key >= span.hi || t.row[s] < 0) {
+                        if (key < span.lo || key >= span.hi || rows[s] < 0) {
                             out |= 1u << (4 * s + e);
                             p[4 * s + e] = -INFINITY;
                         }
@@ -577,7 +568,7 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int at_word = BITS == 16 ? c : c / 2;
-                    const uint32_t w = t.v[e][at_word / 4][VW < 4 ? at_word : at_word % 4];
+                    const uint32_t w = tv[e][at_word / 4][VW < 4 ? at_word : at_word % 4];
                     if constexpr (BITS == 16) raw[e] = w;
                     else raw[e] = c % 2 ? two_codes<true>(w) : two_codes<false>(w);
                     // what lies in places that do not count may be anything, NaN among it, and 0 NaN is NaN
@@ -588,16 +579,9 @@ __global__ __launch_bounds__(THREADS, (residents<DIM, BITS>())) void attend_kern
                 O[2 * c] = mfma16(v0.v, pf.v, O[2 * c]);
                 O[2 * c + 1] = mfma16(v1.v, pf.v, O[2 * c + 1]);
             }
-            load_v(t, next, all);
-            t.row[0] = next[0];
-            t.row[1] = next[1];
-        };
-        for (int i = 0; i < mine; i += AHEAD) {
-            tile(i, held[0]);
-            if constexpr (AHEAD == 2) {
-                if (i + 1 >= mine) break;
-                tile(i + 1, held[1]);
-            }
+            load_v(next, all);
+            rows[0] = next[0];
+            rows[1] = next[1];
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
@@ -710,7 +694,7 @@ hipError_t start(AttendArgs& a, hipStream_t stream)
     }
     // as many workgroups as the chip holds at a time (registers, 160 KiB of LDS), and no more than the table's widest requests have work for
     int each = (int)(159 * 1024 / (lds + 1024));
-    each = each < residents<DIM, BITS>() ? each : residents<DIM, BITS>();
+    each = each < residents<DIM>() ? each : residents<DIM>();
     const size_t most = (size_t)a.B * a.kv * a.hblocks * (((size_t)a.width * a.page + TILE - 1) / TILE + START + 1) / NW + 1;
     a.nwg = most < (size_t)256 * each ? (int)most : 256 * each;
     kern<<<a.nwg, THREADS, lds, stream>>>(a);
