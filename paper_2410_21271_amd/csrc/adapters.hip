@@ -522,9 +522,12 @@ __device__ __forceinline__ void up(const AdapterArgs& a, int window, int g, int 
     // (rows without a pair have nothing to add; with y apart from base they are copied)
     const Window win = window_of(a, window * WINDOW, a.base != a.y);
     const int pairs = __popcll(win.leaders), kss = ranges_of(a, __popcll(win.leaders & __ballot(win.id >= 0)));
-    // slabs of outputs: as many as there are workgroups for, a step of each wavefront at least
-    const int blocks = a.d_out / 16, unit_blocks = NW * Rows::PB, least = (blocks + unit_blocks - 1) / unit_blocks;
-    const int each = pairs ? a.up_wgs / pairs : 1, slabs = each < 1 ? 1 : (each < least ? each : least), size = (blocks + slabs - 1) / slabs;
+    // slabs of outputs: as many as there are workgroups for, a step of each wavefront at least for the largest pair (with no more than a small pair has steps for: 256 rows of one
+    // pair, 4096 -> 4096, 22 us, 18)
+    const int rows_here = __popcll(win.same);
+    const bool four = __ballot(rows_here > (SHARE ? 16 : 32)) & win.leaders, two = __ballot(rows_here > 16) & win.leaders;
+    const int blocks = a.d_out / 16, steps = (blocks + Rows::PB - 1) / Rows::PB, most = four ? steps : (two ? (steps + 1) / 2 : (steps + 3) / 4);
+    const int each = pairs ? a.up_wgs / pairs : 1, slabs = each < 1 ? 1 : (each < most ? each : most), size = (blocks + slabs - 1) / slabs;
     for (int unit = g; unit < pairs * slabs; unit += a.up_wgs) {
         const int slab = unit % slabs, first_row = leader_at(win, unit / slabs);
         const int id = __builtin_amdgcn_readlane(win.id, first_row);
@@ -630,8 +633,9 @@ hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
         if (a.base) a.base += (size_t)m0 * a.d_out;
         const int windows = (a.M + WINDOW - 1) / WINDOW, nr = a.r / 16, rblocks = nr < 4 || (a.M == 1 && nr <= 8) ? 1 : 4;
         a.rgroups = (nr + rblocks - 1) / rblocks;
-        // First part: one workgroup a compute unit, with two chunks in its registers.  Second: two, or one beside those of the first
-        a.down_wgs = windows < 256 ? 256 / windows : 1;
+        // First part: one workgroup a compute unit, with two chunks in its registers (two: 2048 rows 44 us, 48), but four a window while that is no more than
+        // four a compute unit (8192 rows of one pair, 4096 -> 4096, with two 71 us, 62).  Second: two, or one beside those of the first
+        a.down_wgs = windows < 64 ? 256 / windows : (windows < 256 ? 4 : (windows < 1024 ? 1024 / windows : 1));
         a.up_wgs = windows == 1 ? 256 : (windows < 512 ? 512 / windows : 1);
         if (a.M < WINDOW) {                               // no more than its rows have work for
             const int down = a.M * a.rgroups * MAX_KSPLIT, up = a.M * ((a.d_out / 16 + 7) / 8);
