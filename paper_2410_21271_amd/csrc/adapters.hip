@@ -122,26 +122,18 @@ struct DownSpace {
     __attribute__((aligned(16))) float red[NW * RB * 256];
 };
 
-// workgroup g of the a.down_wgs that a window has
+// One unit: `count` rows (row0 + list[..]) of pair id, group rg of its ranks, range ks of kss.  first_row: the pair's counts (ONE)
 template <int FA, int RB, bool ONE>
-__device__ __forceinline__ void down(const AdapterArgs& a, int step, int window, int g, DownSpace<RB>& space)
-{
-    constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT, XLD = DownSpace<RB>::XLD;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    int* list = space.lists[wave];
-    _Float16* xw = space.xs[wave];
-    float* red = space.red;
-    const Window win = window_of(a, window * WINDOW, false);
-    const int pairs = __popcll(win.leaders), kss = ranges_of(a, pairs), chunks = a.d_in / 128;
-    for (int unit = g; unit < pairs * a.rgroups * kss; unit += a.down_wgs) {
-        const int rg = unit % a.rgroups, ks = unit / a.rgroups % kss, first_row = leader_at(win, unit / (a.rgroups * kss));
-        const int id = __builtin_amdgcn_readlane(win.id, first_row), c0 = chunks * ks / kss, c1 = chunks * (ks + 1) / kss, rb0 = rg * RB;
-        const unsigned long long rows = rows_at(win, first_row);
-        const int rank = rank_of(a, id, step), count = __popcll(rows), row0 = win.row0;
-        if (16 * rb0 >= rank) continue;
+struct Down {
+    static constexpr int WORDS = Fmt<FA>::WORDS, KT = Fmt<FA>::KT, TPC = 128 / KT, XLD = DownSpace<RB>::XLD;
+    static __device__ __forceinline__ void run(const AdapterArgs& a, int id, int rank, int row0, const int* list, int count, int rg, int ks, int kss, int first_row, DownSpace<RB>& space)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
+        _Float16* xw = space.xs[wave];
+        float* red = space.red;
+        const int chunks = a.d_in / 128, c0 = chunks * ks / kss, c1 = chunks * (ks + 1) / kss, rb0 = rg * RB;
         const int blocks = rank / 16 - rb0 < RB ? rank / 16 - rb0 : RB;
         const int tbs = row_blocks(count), phases = NW / tbs, tb = wave % tbs, phase = wave / tbs;
-        list_rows(rows, lane, list);
         // the rows of x that this lane moves, 16 bytes of each
         const _Float16* px[4];
 #pragma unroll
@@ -224,7 +216,7 @@ __device__ __forceinline__ void down(const AdapterArgs& a, int step, int window,
                     const int slot = 16 * tb + 4 * j + i;
                     if (slot < count && q < blocks) a.t[((size_t)ks * a.M + row0 + list[slot]) * a.r + 16 * (rb0 + q) + n] = acc[q][i];
                 }
-            continue;
+            return;
         }
         // sum over the wavefronts of a block of rows, in order
         __syncthreads();                                  // (the last unit's sums have been read)
@@ -251,6 +243,218 @@ __device__ __forceinline__ void down(const AdapterArgs& a, int step, int window,
             if (threadIdx.x == 0) add_one(a.header + READY + LINE * first_row);
         }
     }
+};
+
+// More than 64 rows: batches of up to 2048 of them in the order of their pairs (stable), cut into units of up to 64 rows of one pair.  Rows without one come first.  In the order of
+// the calling program B is read again in each 64 rows that hold one of a pair's: 2048 rows 4096 -> 14336 with their 16 pairs one after the other 112 us, in order ORDERED_MIXED; in runs of
+// 60 62 us, ORDERED_60.  Each workgroup of the first launch finds the order itself (some 2 us), and one of a batch leaves it for the second.
+constexpr int BATCH = 2048, ORDER = 4 + 4 * (BATCH + 1) + BATCH + 28;        // words of a batch in the workspace
+struct Order {
+    int keys[BATCH];                           // pair + 1, 0: none
+    unsigned short rows[2][BATCH], starts[BATCH + 1];
+    int digits[64 * NW];
+    int sums[NW];
+    int units, none;                           // units in all, without a pair
+};
+
+// sum (maximum) of v over the threads before this one; all: over all
+template <bool MAX>
+__device__ __forceinline__ int before_me(int v, int* sums, int& all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto join = [](int x, int y) { return MAX ? (x > y ? x : y) : x + y; };
+    const int none = MAX ? -1 : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int w = __shfl_up(v, o, 64);
+        v = join(v, lane >= o ? w : none);
+    }
+    if (lane == 63) sums[wave] = v;
+    int mine = __shfl_up(v, 1, 64);
+    if (lane == 0) mine = none;
+    __syncthreads();
+    all = none;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < wave) mine = join(mine, sums[w]);
+        all = join(all, sums[w]);
+    }
+    __syncthreads();
+    return mine;
+}
+
+// All threads; returns the rows in order.  By up to six bits of the key at a time, lowest first.
+__device__ __forceinline__ const unsigned short* order_rows(const AdapterArgs& a, int row0, int m, Order& o)
+{
+    static_assert(64 * NW == THREADS, "a digit's counts by wavefronts: one a thread");
+    constexpr int EACH = BATCH / THREADS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per = (m + THREADS - 1) / THREADS, place = wave * 64 * per + lane;         // places of a wavefront: `per` times 64
+    int row[EACH], key[EACH], from = 0;
+#pragma unroll
+    for (int c = 0; c < EACH; ++c) {
+        row[c] = place + 64 * c;
+        key[c] = a.ids[row0 + (row[c] < m ? row[c] : 0)];
+    }
+#pragma unroll
+    for (int c = 0; c < EACH; ++c) {
+        key[c] = (unsigned)key[c] < (unsigned)a.n ? key[c] + 1 : 0;
+        if (c < per && row[c] < m) o.keys[row[c]] = key[c];
+    }
+    const int bits = 32 - __clz(a.n);
+    for (int shift = 0; shift < bits; shift += 6, from ^= 1) {
+        const int width = bits - shift < 6 ? bits - shift : 6;
+        o.digits[threadIdx.x] = 0;
+        __syncthreads();
+        if (shift > 0) {
+#pragma unroll
+            for (int c = 0; c < EACH; ++c) {
+                const int p = place + 64 * c;
+                row[c] = o.rows[from][p < m ? p : 0];
+            }
+#pragma unroll
+            for (int c = 0; c < EACH; ++c) key[c] = o.keys[row[c]];
+        }
+        // how many of each digit; then where they go: a wavefront's counts in the order of its places
+        unsigned long long same[EACH];
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+            if (c >= per) break;
+            const bool there = place + 64 * c < m;
+            same[c] = __ballot(there);
+            for (int bit = shift; bit < shift + width; ++bit) {
+                const unsigned long long ones = __ballot(key[c] >> bit & 1);
+                same[c] &= key[c] >> bit & 1 ? ones : ~ones;
+            }
+            if (there && !(same[c] & ((1ull << lane) - 1))) atomicAdd(&o.digits[(key[c] >> shift & 63) * NW + wave], __popcll(same[c]));
+        }
+        __syncthreads();
+        int all;
+        const int before = before_me<false>(o.digits[threadIdx.x], o.sums, all);
+        o.digits[threadIdx.x] = before;
+        __syncthreads();
+        int to[EACH];
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+            to[c] = 0;
+            if (c < per && place + 64 * c < m && !(same[c] & ((1ull << lane) - 1))) to[c] = atomicAdd(&o.digits[(key[c] >> shift & 63) * NW + wave], __popcll(same[c]));
+        }
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+            if (c >= per) break;
+            const int first = __shfl(to[c], __ffsll(same[c]) - 1, 64);
+            if (place + 64 * c < m) o.rows[from ^ 1][first + __popcll(same[c] & ((1ull << lane) - 1))] = (unsigned short)row[c];
+        }
+        __syncthreads();
+    }
+    const unsigned short* rows = o.rows[from];
+    // units: every 64 places of a run of equal keys
+    int start[EACH], last = -1, all;
+    const int p0 = EACH * (int)threadIdx.x, previous = o.keys[rows[p0 > 0 && p0 <= m ? p0 - 1 : 0]];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) row[e] = rows[p0 + e < m ? p0 + e : 0];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) key[e] = o.keys[row[e]];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int p = p0 + e;
+        if (p < m && (p == 0 || key[e] != (e ? key[e ? e - 1 : 0] : previous))) last = p;
+        start[e] = last;
+    }
+    const int run = before_me<true>(last, o.sums, all);
+    int count = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int p = p0 + e;
+        start[e] = p < m && ((p - (start[e] < 0 ? run : start[e])) & 63) == 0;
+        count += start[e] ? (key[e] ? 1 : 1 + (1 << 16)) : 0;
+    }
+    int at = before_me<false>(count, o.sums, all) & 0xffff;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if (start[e]) o.starts[at++] = (unsigned short)(p0 + e);
+    if (threadIdx.x == 0) {
+        o.units = all & 0xffff;
+        o.none = all >> 16;
+        o.starts[all & 0xffff] = (unsigned short)m;
+    }
+    __syncthreads();
+    return rows;
+}
+
+// Work of a unit in the second launch: up to 16 rows, which all wavefronts have, or a block for each
+__device__ __forceinline__ int weight_of(int count) { return count > 16 ? 4 : 1; }
+
+// For the second launch: units and units without a pair, then of each unit its first place, the weights before it and its pair, then the rows in order
+__device__ __forceinline__ void leave_order(const AdapterArgs& a, int batch, int m, const Order& order, const unsigned short* rows, int* sums)
+{
+    int* to = a.order + (size_t)batch * ORDER;
+    constexpr int EACH = BATCH / THREADS;
+    int weight = 0, all;
+    for (int e = 0; e < EACH; ++e) {
+        const int u = EACH * (int)threadIdx.x + e;
+        if (u < order.units) weight += weight_of(order.starts[u + 1] - order.starts[u]);
+    }
+    int before = before_me<false>(weight, sums, all);
+    for (int e = 0; e < EACH; ++e) {
+        const int u = EACH * (int)threadIdx.x + e;
+        if (u >= order.units) break;
+        const int first = order.starts[u];
+        ((int4*)to)[1 + u] = make_int4(first, before, order.keys[rows[first]] - 1, 0);
+        before += weight_of(order.starts[u + 1] - first);
+    }
+    if (threadIdx.x == 0) {
+        ((int4*)to)[0] = make_int4(order.units, order.none, 0, 0);
+        ((int4*)to)[1 + order.units] = make_int4(m, all, -1, 0);
+    }
+    for (int e = threadIdx.x; e < m; e += THREADS) to[4 + 4 * (BATCH + 1) + e] = rows[e];
+}
+// ranges of the contraction where a batch has so many units with a pair
+__device__ __forceinline__ int ranges_of_batch(const AdapterArgs& a, int m, int units)
+{
+    const int most = m > 8 * units ? MAX_KSPLIT / 2 : MAX_KSPLIT, fair = units ? a.down_wgs / (units * a.rgroups) : 1, chunks = a.d_in / 128 / NW;
+    const int ks = fair < most ? fair : most;
+    return ks <= 1 ? 1 : (ks < chunks ? ks : (chunks < 1 ? 1 : chunks));
+}
+
+template <int FA, int RB>
+__global__ __launch_bounds__(THREADS, 1) void down_ordered_kernel(const AdapterArgs a, int step)
+{
+    __shared__ DownSpace<RB> space;
+    __shared__ Order order;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int batch = blockIdx.x / a.down_wgs, g = blockIdx.x - batch * a.down_wgs, row0 = batch * BATCH, m = a.M - row0 < BATCH ? a.M - row0 : BATCH;
+    int* list = space.lists[wave];
+    const unsigned short* rows = order_rows(a, row0, m, order);
+    if (g == a.down_wgs - 1) leave_order(a, batch, m, order, rows, order.sums);        // (often one without a unit)
+    const int none = order.none, kss = ranges_of_batch(a, m, order.units - none), slices = a.rgroups * kss;
+    for (int unit = g; unit < (order.units - none) * slices; unit += a.down_wgs) {
+        const int u = none + unit / slices, slice = unit % slices, rg = slice % a.rgroups;
+        const int first = __builtin_amdgcn_readfirstlane(order.starts[u]), count = __builtin_amdgcn_readfirstlane(order.starts[u + 1]) - first;
+        const int id = __builtin_amdgcn_readfirstlane(order.keys[rows[first]]) - 1, rank = rank_of(a, id, step);
+        if (16 * RB * rg >= rank) continue;
+        list[lane] = rows[first + (lane < count ? lane : 0)];
+        Down<FA, RB, false>::run(a, id, rank, row0, list, count, rg, slice / a.rgroups, kss, 0, space);
+    }
+}
+
+// Rows in the caller's order: workgroup g of the a.down_wgs of a window
+template <int FA, int RB, bool ONE>
+__device__ __forceinline__ void down_window(const AdapterArgs& a, int step, int window, int g, DownSpace<RB>& space)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int* list = space.lists[wave];
+    const Window win = window_of(a, window * WINDOW, false);
+    const int pairs = __popcll(win.leaders), kss = ranges_of(a, pairs);
+    for (int unit = g; unit < pairs * a.rgroups * kss; unit += a.down_wgs) {
+        const int rg = unit % a.rgroups, ks = unit / a.rgroups % kss, first_row = leader_at(win, unit / (a.rgroups * kss));
+        const int id = __builtin_amdgcn_readlane(win.id, first_row);
+        const unsigned long long rows = rows_at(win, first_row);
+        const int rank = rank_of(a, id, step);
+        if (16 * RB * rg >= rank) continue;
+        list_rows(rows, lane, list);
+        Down<FA, RB, ONE>::run(a, id, rank, win.row0, list, __popcll(rows), rg, ks, kss, first_row, space);
+    }
 }
 
 template <int FA, int RB>
@@ -258,7 +462,7 @@ __global__ __launch_bounds__(THREADS, 1) void down_kernel(const AdapterArgs a, i
 {
     __shared__ DownSpace<RB> space;
     const int window = blockIdx.x / a.down_wgs;
-    down<FA, RB, false>(a, step, window, blockIdx.x - window * a.down_wgs, space);
+    down_window<FA, RB, false>(a, step, window, blockIdx.x - window * a.down_wgs, space);
 }
 
 // Waits for, and gives up, t of the pair that row `first` leads; need: the units that make it up, readers: the wavefronts that read it
@@ -512,9 +716,9 @@ struct UpSpace {
     __attribute__((aligned(16))) uint32_t stage[Up<FE, NK, SHARE, false>::STAGE];
 };
 
-// workgroup g of the a.up_wgs that a window has; rb_ranks: ranks of a unit of the first part (ONE)
-template <int FE, int NK, bool SHARE, bool ONE>
-__device__ __forceinline__ void up(const AdapterArgs& a, int window, int g, int rb_ranks, UpSpace<FE, NK, SHARE>& s)
+// Rows in the caller's order: workgroup g of the a.up_wgs of a window; rb_ranks: ranks of a unit of the first part (ONE)
+template <int FE, int NK, bool ONE>
+__device__ __forceinline__ void up_window(const AdapterArgs& a, int window, int g, int rb_ranks, UpSpace<FE, NK, false>& s)
 {
     typedef Up<FE, NK, false, ONE> Rows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -525,7 +729,7 @@ __device__ __forceinline__ void up(const AdapterArgs& a, int window, int g, int 
     // slabs of outputs: as many as there are workgroups for, a step of each wavefront at least for the largest pair (with no more than a small pair has steps for: 256 rows of one
     // pair, 4096 -> 4096, 22 us, 18)
     const int rows_here = __popcll(win.same);
-    const bool four = __ballot(rows_here > (SHARE ? 16 : 32)) & win.leaders, two = __ballot(rows_here > 16) & win.leaders;
+    const bool four = __ballot(rows_here > 32) & win.leaders, two = __ballot(rows_here > 16) & win.leaders;
     const int blocks = a.d_out / 16, steps = (blocks + Rows::PB - 1) / Rows::PB, most = four ? steps : (two ? (steps + 1) / 2 : (steps + 3) / 4);
     const int each = pairs ? a.up_wgs / pairs : 1, slabs = each < 1 ? 1 : (each < most ? each : most), size = (blocks + slabs - 1) / slabs;
     for (int unit = g; unit < pairs * slabs; unit += a.up_wgs) {
@@ -536,21 +740,65 @@ __device__ __forceinline__ void up(const AdapterArgs& a, int window, int g, int 
         const Wait wait{first_row, (unsigned)((rank + rb_ranks - 1) / rb_ranks * kss), (unsigned)(slabs * NW)};
         if ((rank == 0 && a.base == a.y) || (!ONE && first >= end)) continue;      // (ONE: every wavefront of a pair's units gives its t up)
         list_rows(rows, lane, list);
-        if (SHARE && count > 16) {
-            Up<FE, NK, SHARE, false>::run(a, id, rank, win.row0, list, count, wave, 0, 1, first, end, kss, s.space[wave], s.stage, wait);
-        } else {
-            const int tbs = row_blocks(count);
-            Rows::run(a, id, rank, win.row0, list, count, wave % tbs, wave / tbs, NW / tbs, first, end, kss, s.space[wave], s.stage, wait);
-        }
+        const int tbs = row_blocks(count);
+        Rows::run(a, id, rank, win.row0, list, count, wave % tbs, wave / tbs, NW / tbs, first, end, kss, s.space[wave], s.stage, wait);
     }
 }
 
-template <int FE, int NK, bool SHARE>
+template <int FE, int NK>
 __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_kernel(const AdapterArgs a)
 {
-    __shared__ UpSpace<FE, NK, SHARE> space;
+    __shared__ UpSpace<FE, NK, false> space;
     const int window = blockIdx.x / a.up_wgs;
-    up<FE, NK, SHARE, false>(a, window, blockIdx.x - window * a.up_wgs, 1, space);
+    up_window<FE, NK, false>(a, window, blockIdx.x - window * a.up_wgs, 1, space);
+}
+
+// Rows in order: the outputs are cut into up to eight column groups, one for the workgroups of each XCD (whose L2 then holds its columns of B once), and the units of a batch, as
+// they follow one another, for each group into runs of equal weight: a workgroup ends one unit and begins another.
+template <int FE, int NK>
+__global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void up_ordered_kernel(const AdapterArgs a)
+{
+    __shared__ UpSpace<FE, NK, true> s;
+    typedef Up<FE, NK, false, false> Rows;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int batch = blockIdx.x / a.up_wgs, g = blockIdx.x - batch * a.up_wgs, row0 = batch * BATCH, m = a.M - row0 < BATCH ? a.M - row0 : BATCH;
+    const int4* units = (const int4*)(a.order + (size_t)batch * ORDER) + 1;
+    const int* rows = (const int*)(units + BATCH + 1);
+    int* list = s.lists[wave];
+    const int n_units = __builtin_amdgcn_readfirstlane(units[-1].x), none = __builtin_amdgcn_readfirstlane(units[-1].y);
+    const int u0 = a.base == a.y ? none : 0;              // (rows without a pair have nothing to add; with y apart from base they are copied)
+    const int kss = ranges_of_batch(a, m, n_units - none), blocks = a.d_out / 16;
+    int groups = 8;
+    while (groups > 1 && (groups > a.up_wgs || blocks < groups * 4 * NW * Rows::PB)) groups /= 2;
+    const int per = (blocks + groups - 1) / groups, group = g % groups, first = group * per, end = first + per < blocks ? first + per : blocks;
+    // a unit of weight w has w q places, of NW / w steps of PB blocks
+    const int q = (per + NW * Rows::PB - 1) / (NW * Rows::PB), before = __builtin_amdgcn_readfirstlane(units[u0].y);
+    const unsigned total = (unsigned)(__builtin_amdgcn_readfirstlane(units[n_units].y) - before) * (unsigned)q, n = (unsigned)(a.up_wgs / groups), i = (unsigned)(g / groups);
+    if (i >= n) return;
+    unsigned at = (unsigned)((unsigned long long)total * i / n);
+    const unsigned stop = (unsigned)((unsigned long long)total * (i + 1) / n);
+    if (at >= stop) return;
+    int u = u0;
+    for (int range = n_units - u0; range > 1;) {          // the last unit that begins at or before `at`
+        const int stride = (range + 63) / 64, mine = u + lane * stride, past = u + range;
+        const bool here = mine < past && (unsigned)(units[mine < past ? mine : past - 1].y - before) * (unsigned)q <= at;
+        u += (__popcll(__ballot(here)) - 1) * stride;
+        range = past - u < stride ? past - u : stride;
+    }
+    u = __builtin_amdgcn_readfirstlane(u);
+    for (; at < stop; ++u) {
+        const int4 unit = units[u], after = units[u + 1];
+        const int start = __builtin_amdgcn_readfirstlane(unit.x), count = __builtin_amdgcn_readfirstlane(after.x) - start, id = __builtin_amdgcn_readfirstlane(unit.z);
+        const unsigned begins = (unsigned)(__builtin_amdgcn_readfirstlane(unit.y) - before) * (unsigned)q, ends = (unsigned)(__builtin_amdgcn_readfirstlane(after.y) - before) * (unsigned)q;
+        const int weight = weight_of(count), place = NW / weight * Rows::PB, from = first + (int)(at - begins) * place, to = first + (int)((stop < ends ? stop : ends) - begins) * place;
+        at = ends;
+        const int rank = rank_of(a, id, Fmt<FE>::KT), last = to < end ? to : end;
+        if (from >= last || (rank == 0 && a.base == a.y)) continue;
+        list[lane] = rows[start + (lane < count ? lane : 0)];
+        const Wait wait{0, 0, 0};
+        if (weight == 4) Up<FE, NK, true, false>::run(a, id, rank, row0, list, count, wave, 0, 1, from, last, kss, s.space[wave], s.stage, wait);
+        else Rows::run(a, id, rank, row0, list, count, 0, wave, NW, from, last, kss, s.space[wave], s.stage, wait);
+    }
 }
 
 template <int FA, int RB, int FE, int NK>
@@ -562,96 +810,104 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void adapters_kernel(cons
         __device__ Space() {}
     } space;
     const int g = blockIdx.x;
-    if (g < a.down_wgs) down<FA, RB, true>(a, step, 0, g, space.first);
-    else up<FE, NK, false, true>(a, 0, g - a.down_wgs, 16 * RB, space.second);
+    if (g < a.down_wgs) down_window<FA, RB, true>(a, step, 0, g, space.first);
+    else up_window<FE, NK, true>(a, 0, g - a.down_wgs, 16 * RB, space.second);
 }
 
-constexpr int MANY = 512;                      // rows
+// How a call goes: in one launch, in two by windows of 64 rows, in two by batches of 2048 in order.  Ordering costs 3 to 6 us and saves B's being read in every window: 1024 rows
+// of 64 pairs, 4096 -> 4096, rank 64, 100 us by windows, 40 in order; 512 rows of 16, rank 128, 22 and 23.5; 256 rows 17 and 22; 2048 rows of one 28 and 34.
+enum Form { ONE_LAUNCH, WINDOWS, ORDERED };
+constexpr int MANY = 512;                      // rows from which they are put in order
 
 template <int FA, int RB>
-hipError_t start_down(const AdapterArgs& a, unsigned grid, int step, hipStream_t stream)
+hipError_t start_down(const AdapterArgs& a, Form form, unsigned grid, int step, hipStream_t stream)
 {
-    down_kernel<FA, RB><<<grid, THREADS, 0, stream>>>(a, step);
+    if (form == ORDERED) down_ordered_kernel<FA, RB><<<grid, THREADS, 0, stream>>>(a, step);
+    else down_kernel<FA, RB><<<grid, THREADS, 0, stream>>>(a, step);
     return hipGetLastError();
 }
 
 template <int FA>
-hipError_t start_down(const AdapterArgs& a, unsigned grid, int rblocks, int step, hipStream_t stream)
+hipError_t start_down(const AdapterArgs& a, Form form, unsigned grid, int rblocks, int step, hipStream_t stream)
 {
     if constexpr (FA == S_F16)                            // (codes have ranks of 64 or more)
-        if (rblocks == 1) return start_down<FA, 1>(a, grid, step, stream);
-    return start_down<FA, 4>(a, grid, step, stream);
+        if (rblocks == 1) return start_down<FA, 1>(a, form, grid, step, stream);
+    return start_down<FA, 4>(a, form, grid, step, stream);
 }
 
 template <int FE, int NK>
-hipError_t start_up(const AdapterArgs& a, int windows, int rblocks, int step, hipStream_t stream)
+hipError_t start_up(const AdapterArgs& a, Form form, unsigned grid, int rblocks, int step, hipStream_t stream)
 {
-    if (windows == 1) {
+    if (form == ONE_LAUNCH) {
         constexpr int FA = FE == S_Q4S64 ? S_Q4S128 : FE;
-        const unsigned grid = (unsigned)(a.down_wgs + a.up_wgs);
         if constexpr (NK <= 4)
             if (rblocks == 1) {
-                adapters_kernel<FA, 1, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+                adapters_kernel<FA, 1, FE, NK><<<a.down_wgs + a.up_wgs, THREADS, 0, stream>>>(a, step);
                 return hipGetLastError();
             }
-        adapters_kernel<FA, 4, FE, NK><<<grid, THREADS, 0, stream>>>(a, step);
+        adapters_kernel<FA, 4, FE, NK><<<a.down_wgs + a.up_wgs, THREADS, 0, stream>>>(a, step);
+    } else if (form == WINDOWS) {
+        up_kernel<FE, NK><<<grid, THREADS, 0, stream>>>(a);
     } else {
-        const unsigned grid = (unsigned)windows * a.up_wgs;
-        // (the kernel that can share has less LDS left for others)
-        if (a.M >= MANY) up_kernel<FE, NK, true><<<grid, THREADS, 0, stream>>>(a);
-        else up_kernel<FE, NK, false><<<grid, THREADS, 0, stream>>>(a);
+        up_ordered_kernel<FE, NK><<<grid, THREADS, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
 
 template <int FE>
-hipError_t start_up(const AdapterArgs& a, int windows, int rblocks, int step, hipStream_t stream)
+hipError_t start_up(const AdapterArgs& a, Form form, unsigned grid, int rblocks, int step, hipStream_t stream)
 {
     if constexpr (FE == S_Q4S64) {
-        return start_up<FE, 2>(a, windows, rblocks, step, stream);
+        return start_up<FE, 2>(a, form, grid, rblocks, step, stream);
     } else {
-        if (a.r <= 128) return start_up<FE, 4>(a, windows, rblocks, step, stream);
-        if (a.r <= 256) return start_up<FE, 8>(a, windows, rblocks, step, stream);
-        return a.r <= 384 ? start_up<FE, 12>(a, windows, rblocks, step, stream) : start_up<FE, 16>(a, windows, rblocks, step, stream);
+        if (a.r <= 128) return start_up<FE, 4>(a, form, grid, rblocks, step, stream);
+        if (a.r <= 256) return start_up<FE, 8>(a, form, grid, rblocks, step, stream);
+        return a.r <= 384 ? start_up<FE, 12>(a, form, grid, rblocks, step, stream) : start_up<FE, 16>(a, form, grid, rblocks, step, stream);
     }
 }
 
 }  // namespace
 
-size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r) { return HEADER * sizeof(uint32_t) + (size_t)MAX_KSPLIT * M * r * sizeof(float); }
+size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r)
+{
+    return (HEADER + (size_t)((M + BATCH - 1) / BATCH) * ORDER) * sizeof(uint32_t) + (size_t)MAX_KSPLIT * M * r * sizeof(float);
+}
 
 hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
 {
     constexpr int LAUNCH = 1 << 16;                       // rows of a launch
     for (int m0 = 0; m0 < args.M; m0 += LAUNCH) {
         AdapterArgs a = args;
-        a.t = (float*)(a.header + HEADER);
         a.M = args.M - m0 < LAUNCH ? args.M - m0 : LAUNCH;
+        const Form form = a.M <= WINDOW ? ONE_LAUNCH : (a.M < MANY ? WINDOWS : ORDERED);
+        const int of = form == ORDERED ? BATCH : WINDOW, parts = (a.M + of - 1) / of, nr = a.r / 16, rblocks = nr < 4 || (a.M == 1 && nr <= 8) ? 1 : 4;
+        a.order = (int*)(a.header + HEADER);
+        a.t = (float*)(a.order + (form == ORDERED ? (size_t)parts * ORDER : 0));
         a.x += (size_t)m0 * a.d_in;
         a.ids += m0;
         a.y += (size_t)m0 * a.d_out;
         if (a.base) a.base += (size_t)m0 * a.d_out;
-        const int windows = (a.M + WINDOW - 1) / WINDOW, nr = a.r / 16, rblocks = nr < 4 || (a.M == 1 && nr <= 8) ? 1 : 4;
         a.rgroups = (nr + rblocks - 1) / rblocks;
-        // First part: one workgroup a compute unit, with two chunks in its registers (two: 2048 rows 44 us, 48), but four a window while that is no more than
-        // four a compute unit (8192 rows of one pair, 4096 -> 4096, with two 71 us, 62).  Second: two, or one beside those of the first
-        a.down_wgs = windows < 64 ? 256 / windows : (windows < 256 ? 4 : (windows < 1024 ? 1024 / windows : 1));
-        a.up_wgs = windows == 1 ? 256 : (windows < 512 ? 512 / windows : 1);
-        if (a.M < WINDOW) {                               // no more than its rows have work for
-            const int down = a.M * a.rgroups * MAX_KSPLIT, up = a.M * ((a.d_out / 16 + 7) / 8);
-            a.down_wgs = down < a.down_wgs ? down : a.down_wgs;
-            a.up_wgs = up < a.up_wgs ? up : a.up_wgs;
-        }
         const int step = fe == S_F16 ? 32 : (fe == S_Q4S64 ? 64 : 128);
-        if (windows > 1) {
-            const unsigned grid = (unsigned)windows * a.down_wgs;
-            const hipError_t e = fa == S_F16 ? start_down<S_F16>(a, grid, rblocks, step, stream)
-                                             : (fa == S_Q4S128 ? start_down<S_Q4S128>(a, grid, rblocks, step, stream) : start_down<S_Q3S128>(a, grid, rblocks, step, stream));
+        if (form == ONE_LAUNCH) {
+            // one workgroup a compute unit for either part, and no more than the rows have work for
+            const int down = a.M * a.rgroups * MAX_KSPLIT, up = a.M * ((a.d_out / 16 + 7) / 8);
+            a.down_wgs = down < 256 ? down : 256;
+            a.up_wgs = up < 256 ? up : 256;
+        } else {
+            // First: one workgroup a compute unit, with two chunks in its registers (two: 2048 rows 44 us, 48), but with more batches 128 each while that is no more than four a
+            // compute unit (8192 rows of one pair, 4096 -> 4096, with 64 each 71 us, 62).  Second: two.
+            a.down_wgs = form == WINDOWS || parts == 1 ? 256 / parts : (parts < 8 ? 128 : 1024 / parts);
+            a.up_wgs = 512 / parts;
+            const unsigned grid = (unsigned)parts * a.down_wgs;
+            const hipError_t e = fa == S_F16 ? start_down<S_F16>(a, form, grid, rblocks, step, stream)
+                                             : (fa == S_Q4S128 ? start_down<S_Q4S128>(a, form, grid, rblocks, step, stream) : start_down<S_Q3S128>(a, form, grid, rblocks, step, stream));
             if (e != hipSuccess) return e;
         }
-        const hipError_t e = fe == S_F16 ? start_up<S_F16>(a, windows, rblocks, step, stream)
-                                         : (fe == S_Q4S64 ? start_up<S_Q4S64>(a, windows, rblocks, step, stream)
-                                                          : (fe == S_Q4S128 ? start_up<S_Q4S128>(a, windows, rblocks, step, stream) : start_up<S_Q3S128>(a, windows, rblocks, step, stream)));
+        const unsigned grid = (unsigned)parts * a.up_wgs;
+        const hipError_t e = fe == S_F16 ? start_up<S_F16>(a, form, grid, rblocks, step, stream)
+                                         : (fe == S_Q4S64 ? start_up<S_Q4S64>(a, form, grid, rblocks, step, stream)
+                                                          : (fe == S_Q4S128 ? start_up<S_Q4S128>(a, form, grid, rblocks, step, stream) : start_up<S_Q3S128>(a, form, grid, rblocks, step, stream)));
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -65,9 +65,10 @@ struct AdapterArgs {
     _Float16* y;                    // M x d_out
     uint32_t* header;               // counts of the one-launch form
     int spin_limit;
-    float* t;                       // (behind the header; set by the launcher) ranges x M x r partial sums of x A^T
+    int* order;                     // (behind the header; these set by the launcher) of the two-launch form: rows of each batch in the order of their pairs
+    float* t;                       // (behind those) ranges x M x r partial sums of x A^T
     int M, d_in, d_out, r, n;
-    int rgroups, down_wgs, up_wgs;          // groups of ranks; workgroups of a window in either launch (set by the launcher)
+    int rgroups, down_wgs, up_wgs;          // groups of ranks; workgroups of either part (of a batch in either launch)
 };
 size_t adapters_workspace_bytes(int M, int d_in, int d_out, int r);
 hipError_t launch_adapters(AdapterArgs a, int fa, int fe, hipStream_t stream);
