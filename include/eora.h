@@ -349,7 +349,7 @@ int eora_linear_sp24_group(const void* x, const eora_sp_member* members, int n_m
  * eora_workspace_error() reports one that expired (y is then invalid, and the workspace to be zeroed again).
  * t = x.A^T is held in fp32 (multiplied with B's tiles as two fp16 of 22 bits together, whatever its magnitude); the sum with
  * base is rounded once.  Equal inputs give bit-equal outputs; a row's sums do not depend on the other rows'
- * contents, but may be split differently when M changes.
+ * contents, but may be split differently when M or the other rows' adapters change.
  * Constraints: M >= 0 (0: no-op), d_in % 128 == 0, d_out % 16 == 0, 1 <= n_adapters, r as for eora_linear_q (> 0).
  * Errors: EORA_ERR_NULL / UNSUPPORTED (ab_bits) / SHAPE / ALIGN / WORKSPACE / LAUNCH. */
 size_t eora_adapters_workspace_bytes(int M, int d_in, int d_out, int r);      /* never shrinks as M or r grows; 0: invalid */

@@ -2,16 +2,17 @@
 //
 //      y[m] = base[m] + s_a (x[m] A_a^T) B_a^T            a = adapter of row m, from a pool of any size
 //
-// Two parts: t = x A^T (fp32 partial sums of ranges of the contraction), then y from t and B.  One launch for up to 64 rows, where each launch would be half the time or more
-// (1 row 4096 -> 4096, rank 16: 7.5 us in one, 10.1 in two), two beyond.  Only the pairs that rows select are read, each once per window of 64 rows, in the stored
-// tiles of the layer kernels.
+// Two parts: t = x A^T (fp32 partial sums of ranges of the contraction), then y from t and B.  One launch for up to 64 rows, where each of two would be half the time
+// (1 row 1024 -> 1024, rank 64: 7.5 us in one, 10.1 in two), two beyond.  Only the pairs that rows select are read, in the stored tiles of the layer kernels.
 //
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
-// of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight.  With many rows of one pair, y's own traffic bounds it.
+// of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight (64 requests, 4096 -> 4096, rank 128: 76 MB in 20.6 us).  With many rows of one pair, y's
+// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 74 us).
 //
-// Rows are grouped without sorting: a window of 64 rows is one adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
+// Rows by pairs: below 512 rows without sorting, in windows of 64 rows, an adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
 // the first row of each pair (its leader) its place among the window's pairs.  Every window has the same number of workgroups, which share its pairs out:
 // a pair's work is cut into as many parts as there are workgroups for it.  So long runs of one pair (prompts) and a pair for each row (a batch of decoding requests) both fill the chip.
+// From 512 rows on they are put in the order of their pairs first (see Order).
 //
 // t is not rounded to fp16: each row's t is scaled by a power of two to a largest value in [256, 512) and split in two fp16 (22 bits, whatever the
 // size of t), both are multiplied with B's tile, and the sum is scaled back in fp32.  y is rounded once.
@@ -245,9 +246,9 @@ struct Down {
     }
 };
 
-// More than 64 rows: batches of up to 2048 of them in the order of their pairs (stable), cut into units of up to 64 rows of one pair.  Rows without one come first.  In the order of
-// the calling program B is read again in each 64 rows that hold one of a pair's: 2048 rows 4096 -> 14336 with their 16 pairs one after the other 112 us, in order ORDERED_MIXED; in runs of
-// 60 62 us, ORDERED_60.  Each workgroup of the first launch finds the order itself (some 2 us), and one of a batch leaves it for the second.
+// Many rows: batches of up to 2048 of them in the order of their pairs (stable), cut into units of up to 64 rows of one pair.  Rows without one come first.  In the
+// caller's order B is read again for each 64 rows that hold one of a pair's.  Each workgroup of the first launch finds the order itself (5 us of 256 threads; a launch of its own would
+// cost as much), and one of a batch leaves it for the second.
 constexpr int BATCH = 2048, ORDER = 4 + 4 * (BATCH + 1) + BATCH + 28;        // words of a batch in the workspace
 struct Order {
     int keys[BATCH];                           // pair + 1, 0: none
@@ -497,7 +498,7 @@ struct Wait {
 // its own for each wavefront and no barrier, so that it is moved 16 bytes a lane, consecutive lanes along a row: straight to and from the operands' places it is
 // 16 rows an instruction, 64 accesses of the L1 instead of 16.
 //
-// SHARE (many rows): the wavefronts have a block of rows each and all outputs of the slab, so that B's tiles are requested once a workgroup, a quarter by each, and pass through LDS
+// SHARE (rows in order): the wavefronts have a block of rows each and all outputs of the slab, so that B's tiles are requested once a workgroup, a quarter by each, and pass through LDS
 // too, two steps of them (requested by every wavefront they are 470 MB from L2 for 2048 rows, 4096 -> 14336, rank 128).
 template <int FE, int NK, bool SHARE, bool ONE>
 struct Up {
@@ -814,8 +815,9 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void adapters_kernel(cons
     else up_window<FE, NK, true>(a, 0, g - a.down_wgs, 16 * RB, space.second);
 }
 
-// How a call goes: in one launch, in two by windows of 64 rows, in two by batches of 2048 in order.  Ordering costs 3 to 6 us and saves B's being read in every window: 1024 rows
-// of 64 pairs, 4096 -> 4096, rank 64, 100 us by windows, 40 in order; 512 rows of 16, rank 128, 22 and 23.5; 256 rows 17 and 22; 2048 rows of one 28 and 34.
+// How a call goes: in one launch, in two by windows of 64 rows, in two by batches of 2048 in order.  Ordering costs 4 to 6 us and saves B's being read in every window (4096 -> 4096,
+// by windows and in order: 1024 rows of 64 pairs in turn, rank 64, 100 and 40 us; rank 128, 512 rows of 16 pairs in turn 22 and 23.5, 256 rows 17 and 22; 8192 rows of 16 pairs in turn 195
+// and 74, in runs of 60 99 and 97, of one pair 63 and 68).
 enum Form { ONE_LAUNCH, WINDOWS, ORDERED };
 constexpr int MANY = 512;                      // rows from which they are put in order
 
