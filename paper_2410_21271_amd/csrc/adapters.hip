@@ -249,7 +249,7 @@ struct Down {
 // Many rows: batches of up to 2048 of them in the order of their pairs (stable), cut into units of up to 64 rows of one pair.  Rows without one come first.  In the
 // caller's order B is read again for each 64 rows that hold one of a pair's.  Each workgroup of the first launch finds the order itself (5 us of 256 threads; a launch of its own would
 // cost as much), and one of a batch leaves it for the second.
-constexpr int BATCH = 2048, ORDER = 4 + 4 * (BATCH + 1) + BATCH + 28;        // words of a batch in the workspace
+constexpr int BATCH = 2048, NOWHERE = 4 * 64, ORDER = 4 + 4 * (BATCH + 1) + BATCH + NOWHERE;       // words of a batch in the workspace; the last are for stores of no use
 struct Order {
     int keys[BATCH];                           // pair + 1, 0: none
     unsigned short rows[2][BATCH], starts[BATCH + 1];
@@ -522,13 +522,14 @@ struct Up {
             return;
         }
         const int wave = SHARE ? tb : 0;
-        // the rows that this lane moves
-        const int piece = lane % LPR;
+        // The rows that this lane moves.  Lanes beyond the last row or column have the last one's, and store the same there; a wavefront without rows (SHARE) stores to where nothing
+        // reads: a store behind a branch would make the next step's wait for its requests one for the stores too (2048 rows STORES).
+        const int piece = lane % LPR, last_row = here > 0 ? here - 1 : 0;
         size_t moved[INS];
 #pragma unroll
         for (int i = 0; i < INS; ++i) {
             const int r = lane / LPR + RPI * i;
-            moved[i] = (size_t)(row0 + list[r < here ? 16 * tb + r : 0]) * a.d_out;
+            moved[i] = (size_t)(row0 + list[here > 0 ? 16 * tb + (r < last_row ? r : last_row) : 0]) * a.d_out;
         }
 
         uint32_t w[HELD][WORDS];
@@ -678,33 +679,40 @@ struct Up {
                         for (int i = 0; i < 4; ++i) acc[p][i] += (float)sc[p][(i * TILES + q) / 4][(i * TILES + q) % 4] * part[i];
                     }
                 }
-            const int col = 16 * rb + 8 * piece;
+            const int most = 2 * (end - rb) - 1, at = piece < most ? piece : most, col = 16 * rb + 8 * at;
             // (without a pair the tiles are another's: whatever they give, -0 is added, which leaves base as it is)
 #pragma unroll
             for (int p = 0; p < PB; ++p) *(f4*)(mine + n * LD + 16 * p + 4 * j) = rank ? acc[p] * back : f4{-0.f, -0.f, -0.f, -0.f};
             h8 y[INS];
 #pragma unroll
             for (int i = 0; i < INS; ++i) {
-                const float* src = mine + (lane / LPR + RPI * i) * LD + 8 * piece;
+                const int r = lane / LPR + RPI * i;
+                const float* src = mine + (r < last_row ? r : last_row) * LD + 8 * at;
                 const f4 lo = *(const f4*)src, hi = *(const f4*)(src + 4);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[i][e] = (_Float16)((a.base ? (float)base[i][e] : 0.f) + (e < 4 ? lo[e] : hi[e - 4]));
             }
-            rb += PB * phases;
-            const bool more = rb < end;
-            if (more) {
-                if constexpr (SHARE) {
-                    put_tiles(buffer ^ 1);
-                    load_tiles(rb + PB < end ? rb + PB : rb);
-                } else {
-                    load_tiles(rb);
-                }
-                load_rest(rb);
-            }
+            auto store = [&] {
 #pragma unroll
-            for (int i = 0; i < INS; ++i)
-                if (lane / LPR + RPI * i < here && col < 16 * end) *(h8*)(a.y + moved[i] + col) = y[i];
-            if (!more) break;
+                for (int i = 0; i < INS; ++i) {
+                    _Float16* to = a.y + moved[i] + col;
+                    if constexpr (SHARE) to = here > 0 ? to : (_Float16*)(a.order + ORDER - NOWHERE) + 8 * lane;
+                    *(h8*)to = y[i];
+                }
+            };
+            rb += PB * phases;
+            if (rb >= end) {
+                store();
+                break;
+            }
+            if constexpr (SHARE) {
+                put_tiles(buffer ^ 1);
+                load_tiles(rb + PB < end ? rb + PB : rb);
+            } else {
+                load_tiles(rb);
+            }
+            load_rest(rb);
+            store();
             if constexpr (SHARE) __syncthreads();
         }
     }
