@@ -7,7 +7,7 @@
 //
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
 // of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight (64 requests, 4096 -> 4096, rank 128: 76 MB in 20.6 us).  With many rows of one pair, y's
-// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 74 us).
+// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 71 us).
 //
 // Rows by pairs: below 512 rows without sorting, in windows of 64 rows, an adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
 // the first row of each pair (its leader) its place among the window's pairs.  Every window has the same number of workgroups, which share its pairs out:
@@ -249,7 +249,7 @@ struct Down {
 // Many rows: batches of up to 2048 of them in the order of their pairs (stable), cut into units of up to 64 rows of one pair.  Rows without one come first.  In the
 // caller's order B is read again for each 64 rows that hold one of a pair's.  Each workgroup of the first launch finds the order itself (5 us of 256 threads; a launch of its own would
 // cost as much), and one of a batch leaves it for the second.
-constexpr int BATCH = 2048, NOWHERE = 4 * 64, ORDER = 4 + 4 * (BATCH + 1) + BATCH + NOWHERE;       // words of a batch in the workspace; the last are for stores of no use
+constexpr int BATCH = 2048, NOWHERE = 2 * 4 * 64, ORDER = 4 + 4 * (BATCH + 1) + BATCH + NOWHERE;       // words of a batch in the workspace; the last are for stores of no use
 struct Order {
     int keys[BATCH];                           // pair + 1, 0: none
     unsigned short rows[2][BATCH], starts[BATCH + 1];
@@ -523,7 +523,7 @@ struct Up {
         }
         const int wave = SHARE ? tb : 0;
         // The rows that this lane moves.  Lanes beyond the last row or column have the last one's, and store the same there; a wavefront without rows (SHARE) stores to where nothing
-        // reads: a store behind a branch would make the next step's wait for its requests one for the stores too (2048 rows STORES).
+        // reads: a store behind a branch would make the next step's wait for its requests one for the stores too (2048 rows, 4096 -> 14336, 74.7 us, 72.3).
         const int piece = lane % LPR, last_row = here > 0 ? here - 1 : 0;
         size_t moved[INS];
 #pragma unroll
@@ -532,6 +532,8 @@ struct Up {
             moved[i] = (size_t)(row0 + list[here > 0 ? 16 * tb + (r < last_row ? r : last_row) : 0]) * a.d_out;
         }
 
+        static_assert(INS <= 2, "what NOWHERE has room for");
+        _Float16* const nowhere = (_Float16*)(a.order + ORDER - NOWHERE) + 8 * lane;
         uint32_t w[HELD][WORDS];
         h4 sc[PB][TILES];                                 // of rows 4 j .. 4 j + 3, TILES tiles each
         h8 base[INS];
@@ -545,7 +547,7 @@ struct Up {
                 load_words<WORDS>(w[i], tiles + tile * (64 * WORDS));
             }
         };
-        auto load_rest = [&](int first) {
+        auto load_scales = [&](int first) {
 #pragma unroll
             for (int p = 0; p < PB; ++p) {
                 if constexpr (FE != S_F16) {
@@ -555,6 +557,8 @@ struct Up {
                     for (int t = 0; t < TILES; ++t) sc[p][t] = *(const h4*)(src + 4 * t);
                 }
             }
+        };
+        auto load_base = [&](int first) {
             const int c = 16 * first + 8 * piece, last = 16 * end - 8;
 #pragma unroll
             for (int i = 0; i < INS; ++i) base[i] = *(const h8*)(from + moved[i] + (c < last ? c : last));
@@ -569,7 +573,8 @@ struct Up {
             }
         };
         load_tiles(rb);
-        load_rest(rb);
+        load_scales(rb);
+        if constexpr (!SHARE) load_base(rb);
         __builtin_amdgcn_sched_barrier(0);
 
         if constexpr (ONE) wait.ready(a);
@@ -645,7 +650,13 @@ struct Up {
         if constexpr (SHARE) {
             __syncthreads();                              // (the last unit's tiles have been read)
             put_tiles(0);
+            // as in every step, stores among it: what is under way at the loop's beginning in whatever order decides how little its waits may leave (72.3, 71.3)
             load_tiles(rb + PB < end ? rb + PB : rb);
+            load_base(rb);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < INS; ++i) *(h8*)(nowhere + 512 * i) = h8{};
+            __builtin_amdgcn_sched_barrier(0);
             __syncthreads();
         }
         for (int buffer = 0;; buffer ^= 1) {
@@ -696,7 +707,7 @@ struct Up {
 #pragma unroll
                 for (int i = 0; i < INS; ++i) {
                     _Float16* to = a.y + moved[i] + col;
-                    if constexpr (SHARE) to = here > 0 ? to : (_Float16*)(a.order + ORDER - NOWHERE) + 8 * lane;
+                    if constexpr (SHARE) to = here > 0 ? to : nowhere + 512 * i;
                     *(h8*)to = y[i];
                 }
             };
@@ -711,7 +722,9 @@ struct Up {
             } else {
                 load_tiles(rb);
             }
-            load_rest(rb);
+            load_scales(rb);
+            load_base(rb);
+            __builtin_amdgcn_sched_barrier(0);
             store();
             if constexpr (SHARE) __syncthreads();
         }

@@ -27,8 +27,10 @@ namespace {
 
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int TILE = 32;
-constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs)
-constexpr int MIN_RUN = 20, FEW = 8;           // cost of a workgroup's run at least: requests of one length, of several
+constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs; with 2, 64 requests of 1 to 4096 tokens 40.6 -> 41.4 us)
+// Cost of a workgroup's run at least, where a join costs more than a longer run.  Requests of one length (1 of 8192 tokens, 4 of 4096 in 8 bits: 10: 17.0, 18.8 us; 20: 17.4, 15.7;
+// 40: 20.8, 17.0), of several (37 of up to 1000 tokens, 13 heads of 64: 4: 20.6; 8: 20.1; 16: 23.1)
+constexpr int MIN_RUN = 20, FEW = 8;
 constexpr int MAX_WG = 1024;
 constexpr int SLOTS = 2 * NW * MAX_WG;
 constexpr int COUNTERS = SLOTS + NW * MAX_WG;  // words before the partial results: a counter for each group of them, and for each unit
@@ -182,7 +184,8 @@ __device__ __forceinline__ Unit unit_after(const AttendArgs& a, const int2* plan
 
 // Whether the wavefronts of a workgroup go through its run together, tile by tile in turn, with their results added up in LDS at each unit's end: in one unit,
 // or where units are long.  Otherwise each has a quarter of the run for itself (short units would leave three of four idle).
-constexpr unsigned LONG = 8;                   // tiles
+// From so many tiles a unit on (64 requests of 1 to 4096 tokens, 37 of up to 1000: 4: 42.2, 23.4 us; 8: 40.6, 20.1; 16: 43.7, 20.1)
+constexpr unsigned LONG = 8;
 __device__ __forceinline__ bool together_at(const AttendArgs& a, const Runs& r, const int2* plan, unsigned g)
 {
     const unsigned pairs = (unsigned)(a.kv * a.hblocks), at = r.cut(NW * g), to = r.cut(NW * g + NW);
@@ -373,7 +376,8 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w)
 }
 
 // Wavefronts a SIMD: what the registers leave room for, which hold one tile and, at D = 256, 64 words of O.  Eight wavefronts a compute unit have 64 to 128 KiB
-// in flight; a second tile in registers, for half the wavefronts, measured 3 to 8 % more.
+// in flight; with a second tile in registers, for half the wavefronts, 64 requests of 1 to 4096 tokens go from 40.6 us to 44.5, 160 to 8192 in 8 bits from 215 to 229, one of 131072 from
+// 59.6 to 58.8.
 template <int DIM>
 constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
 
