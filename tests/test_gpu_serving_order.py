@@ -85,3 +85,68 @@ def test_rows_in_order(gpu, M, n, kind, bits):
     without = (ids < 0) | (ids >= n)
     assert np.array_equal(results[0][without].view(np.uint16), base[without].view(np.uint16))
     assert all(np.array_equal(results[0].view(np.uint16), t.view(np.uint16)) for t in results[1:]), "in place, or a second time, other bits"
+
+
+def small_pool(gpu, rng, n, d_in, d_out, r):
+    import torch
+    pairs = [((rng.normal(0, d_in ** -0.5, (r, d_in))).astype(np.float16), (rng.normal(0, r ** -0.5, (d_out, r))).astype(np.float16)) for _ in range(n)]
+    pools = [torch.from_numpy(np.concatenate([gpu.pack_factor_f16(p[i]) for p in pairs])).cuda() for i in range(2)]
+    return [(A.astype(np.float64), B.astype(np.float64)) for A, B in pairs], pools
+
+
+def check(got, x, base, ids, pairs, scalings):
+    want, size = base.astype(np.float64), np.abs(base.astype(np.float64))
+    for a, (A, B) in enumerate(pairs):
+        rows = ids == a
+        want[rows] += scalings[a] * (x[rows].astype(np.float64) @ A.T @ B.T)
+        size[rows] += abs(scalings[a]) * (np.abs(x[rows].astype(np.float64)) @ np.abs(A).T @ np.abs(B).T)
+    bad = ~(np.abs(got.astype(np.float64) - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -16 * size + 2.0 ** -25)
+    assert not bad.any(), "%d of %d off, first at %s" % (bad.sum(), bad.size, tuple(np.argwhere(bad)[0]))
+
+
+def test_more_rows_than_a_launch(gpu):
+    """65536 + 70 rows: 32 batches in order, then two windows."""
+    import torch
+    rng = np.random.default_rng(9)
+    M, n, d_in, d_out, r = 65536 + 70, 5, 128, 48, 32
+    pairs, pools = small_pool(gpu, rng, n, d_in, d_out, r)
+    scalings = np.array([1.0, -0.5, 2.0, 0.0, 3.0], np.float32)
+    ids = rng.integers(-1, n, M).astype(np.int32)
+    x, base = rng.normal(0, 1, (M, d_in)).astype(np.float16), rng.normal(0, 1, (M, d_out)).astype(np.float16)
+    dev = [torch.from_numpy(t).cuda() for t in (x, base, ids, scalings)]
+    gpu.linear_adapters(dev[0], pools[0], pools[1], None, None, None, dev[3], dev[2], dev[1], dev[1], M, d_in, d_out, r, n, 16, gpu.new_adapters_workspace(M, d_in, d_out, r))
+    torch.cuda.synchronize()
+    check(dev[1].cpu().numpy(), x, base, ids, pairs, scalings)
+
+
+def test_order_changes_between_replays_of_a_graph(gpu):
+    """The rows' pairs are read when the graph runs: other indices, other order, the eager bits each time; small calls between use the same workspace."""
+    import torch
+    rng = np.random.default_rng(10)
+    M, n, d_in, d_out, r = 900, 70, 256, 80, 64
+    pairs, pools = small_pool(gpu, rng, n, d_in, d_out, r)
+    x, base = rng.normal(0, 1, (M, d_in)).astype(np.float16), rng.normal(0, 1, (M, d_out)).astype(np.float16)
+    dx, dbase, ids = torch.from_numpy(x).cuda(), torch.from_numpy(base).cuda(), torch.zeros(M, dtype=torch.int32, device="cuda")
+    y, ws = torch.empty_like(dbase), gpu.new_adapters_workspace(M, d_in, d_out, r)
+
+    def step(rows):
+        gpu.linear_adapters(dx, pools[0], pools[1], None, None, None, None, ids, dbase, y, rows, d_in, d_out, r, n, 16, ws)
+
+    step(M)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(M)
+    for draw in ("random", "in turn", "falling", "none", "random"):
+        host = draw_ids(draw, M, n, rng).astype(np.int32)
+        ids.copy_(torch.from_numpy(host))
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = y.cpu().numpy()
+        check(got, x, base, host, pairs, np.ones(n))
+        for rows in (64, 100, M):
+            y.zero_()
+            step(rows)
+            torch.cuda.synchronize()
+        assert np.array_equal(got.view(np.uint16), y.cpu().numpy().view(np.uint16))
