@@ -7,7 +7,7 @@
 //
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
 // of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight (64 requests, 4096 -> 4096, rank 128: 76 MB in 20.6 us).  With many rows of one pair, y's
-// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 71 us).
+// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 69 us).
 //
 // Rows by pairs: below 512 rows without sorting, in windows of 64 rows, an adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
 // the first row of each pair (its leader) its place among the window's pairs.  Every window has the same number of workgroups, which share its pairs out:
@@ -708,7 +708,10 @@ struct Up {
                 for (int i = 0; i < INS; ++i) {
                     _Float16* to = a.y + moved[i] + col;
                     if constexpr (SHARE) to = here > 0 ? to : nowhere + 512 * i;
-                    *(h8*)to = y[i];
+                    // (many rows: past L2, which has B's tiles and base to hold: 2048 rows, 4096 -> 14336, 72.4 us, 69.1; 30000 rows 1024 -> 2048 110, 92; followed by a reader of y the
+                    // same as without)
+                    if constexpr (SHARE) __builtin_nontemporal_store(y[i], (h8*)to);
+                    else *(h8*)to = y[i];
                 }
             };
             rb += PB * phases;
