@@ -27,6 +27,7 @@ namespace {
 
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int TILE = 32;
+// (Measured sides below: loads through the caches throughout.)
 constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs; with 2, 64 requests of 1 to 4096 tokens 40.6 -> 41.4 us)
 // Cost of a workgroup's run at least, where a join costs more than a longer run.  Requests of one length (1 of 8192 tokens, 4 of 4096 in 8 bits: 10: 17.0, 18.8 us; 20: 17.4, 15.7;
 // 40: 20.8, 17.0), of several (37 of up to 1000 tokens, 13 heads of 64: 4: 20.6; 8: 20.1; 16: 23.1)
@@ -381,7 +382,15 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w)
 template <int DIM>
 constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
 
-template <int DIM, int BITS>
+// Keys and values past the caches (once read, of no more use), or through them
+template <bool PAST, typename T>
+__device__ __forceinline__ T fetch(const char* p)
+{
+    if constexpr (PAST) return __builtin_nontemporal_load((const T*)p);
+    else return *(const T*)p;
+}
+
+template <int DIM, int BITS, bool PAST>
 __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const AttendArgs a)
 {
     constexpr int NT = DIM / 32;               // k-steps of the first product
@@ -463,7 +472,7 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
             for (int s = 0; s < 2; ++s) {
                 const char* base = (const char*)a.pages_k + (size_t)(row[s] < 0 ? 0 : row[s]) * (DIM * BYTES);
 #pragma unroll
-                for (int e = 0; e < KL; ++e) tk[s][e] = *(const u4*)(base + off + 64 * e);
+                for (int e = 0; e < KL; ++e) tk[s][e] = fetch<PAST, u4>(base + off + 64 * e);
             }
         };
         auto load_v = [&](const long long (&row)[2], unsigned all) {
@@ -474,7 +483,7 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int v = 0; v < VL; ++v) tv[4 * s + i][v] = *(const words*)(base + off + i * DIM * BYTES + 16 * v);
+                    for (int v = 0; v < VL; ++v) tv[4 * s + i][v] = fetch<PAST, words>(base + off + i * DIM * BYTES + 16 * v);
             }
         };
         if (mine > 0) look(0);
@@ -687,11 +696,11 @@ void set_blocks(AttendArgs& a)
     a.rows = a.group < 16 ? a.group : 16;
 }
 
-template <int DIM, int BITS>
+template <int DIM, int BITS, bool PAST>
 hipError_t start(AttendArgs& a, hipStream_t stream)
 {
     const size_t lds = NW * a.rows * DIM * sizeof(float) + ((size_t)a.B + 1) * sizeof(int2);
-    const auto kern = attend_kernel<DIM, BITS>;
+    const auto kern = attend_kernel<DIM, BITS, PAST>;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
@@ -703,6 +712,15 @@ hipError_t start(AttendArgs& a, hipStream_t stream)
     a.nwg = most < (size_t)256 * each ? (int)most : 256 * each;
     kern<<<a.nwg, THREADS, lds, stream>>>(a);
     return hipGetLastError();
+}
+
+// Past the caches where what the widest requests hold is half of the last-level cache or more (64 requests of 2048 tokens, 538 MB, 94.5 us through, 83.8 past; 64 of 527, 139 MB, 29.9,
+// 27.3; 160 to 8192 in 8 bits 214, 198); less may be there still from the call before (1 of 8192, 34 MB, 17.4, 20.0; 37 of up to 1000, 20.6, 22.1).
+template <int DIM, int BITS>
+hipError_t start(AttendArgs& a, hipStream_t stream)
+{
+    const size_t tokens = (size_t)a.width * a.page, seen = a.window > 0 && (size_t)a.window < tokens ? (size_t)a.window : tokens;
+    return a.B * seen * a.kv * DIM * (BITS / 8) * 2 >= ((size_t)128 << 20) ? start<DIM, BITS, true>(a, stream) : start<DIM, BITS, false>(a, stream);
 }
 
 template <int DIM>

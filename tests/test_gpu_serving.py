@@ -638,3 +638,15 @@ def test_on_another_stream_and_in_a_graph(gpu):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
         x.mul_(1.0)
+
+
+@pytest.mark.parametrize("heads,kv,dim,bits,page,window", [(8, 2, 64, 16, 16, 0), (6, 3, 128, 16, 48, 0), (8, 8, 128, 8, 16, 70), (4, 2, 256, 16, 32, 0), (16, 1, 64, 8, 64, 0), (5, 5, 256, 8, 16, 33)])
+def test_attention_tables_wider_than_the_requests(gpu, heads, kv, dim, bits, page, window):
+    """Tables with room for caches that are read past the last-level cache: 128 MiB and more, of which the requests have little."""
+    c = Cache(61 + dim + bits, [700, 0, 1, 333, page, 4 * page + 1], heads, kv, dim, bits, page)
+    each = 6 * kv * dim * (bits // 8) * 2
+    tokens = -(-2 ** 27 // each) if not window else 0
+    more = max(0, -(-tokens // page) - c.width) + 3
+    c.table = np.ascontiguousarray(np.pad(c.table, ((0, 0), (0, more)), constant_values=-1))
+    c.width += more
+    c.check(gpu, window)
