@@ -394,7 +394,7 @@ int eora_cache_append(const void* q, const void* k, const void* v, const void* q
  * never used, NaN included.
  * out: fp16 B x n_heads x head_dim; lse: fp32 B x n_heads or NULL (natural logarithm: with it results over parts of a cache
  * can be joined).  Several tokens of one request (a short prompt): one row each, with the lengths that each may see.
- * Scores, sums and out are fp32 until the end; a weight is rounded to fp16 for its product with v.  Equal inputs give
+ * Scores, sums and out are fp32 until the end; a weight meets v with 20 bits (as two fp16).  Equal inputs give
  * bit-equal outputs; how the tokens are split between workgroups, and so the last bits, depends on the lengths of all requests.
  * workspace: eora_cache_attention_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its bytes are ZERO before the
  * first call (hipMemset, say); every call leaves it usable for the next, of whatever sizes.

@@ -13,8 +13,9 @@
 // has column dim / 16 * n + b as its row n, and a lane's operand is a transposition of 16-bit values in its own registers.  No LDS, no exchange between lanes in the loop.
 //
 // Softmax: m is a reference, common to the lanes of a head, not the exact maximum: it is raised, and O and the sum rescaled, only when a score
-// exceeds it by 8 or more (weights up to 256 are as exact in fp16 as weights up to 1).  Scores, sums and O are fp32; a weight is
-// rounded to fp16 (nearest-even) for the product with V, the sum takes it unrounded.
+// exceeds it by 8 or more.  Scores, sums and O are fp32.  A weight meets V as two fp16, the second what the first leaves of it: 20.7 bits together, beside which the
+// rounding of the result is all that shows (one fp16 put out off by up to 2^-12 of sum p |v|).  The first is cut off from a little
+// below the weight, so that the second is positive as well: an infinite value then gives an infinity, which halves of zero or of two signs would make a NaN.
 //
 // Split: all units (a request's kv head, or block of 16 of its query heads) in one row are cut into equal runs, whatever the lengths are: a request of 100 000
 // tokens is spread over the whole chip, and one of 10 costs a tile.  A workgroup whose run lies in one unit works on it together and adds up in
@@ -41,6 +42,10 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 static_assert(START < NW, "the run of a workgroup holds a tile of each unit that it touches alone");
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// what the first half of a weight is cut off from
+constexpr float BELOW = 1.f - 0x1p-12f;
+__device__ __forceinline__ h2 toward_zero(float x, float y) { return __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y)); }
 
 // tokens and tiles of a request of n tokens
 struct Span {
@@ -568,13 +573,16 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
                 for (int b = 0; b < W; ++b) O[b] *= f;
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            Frag pf;
+            Frag high, low;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 p[e] = exp2_(p[e] - ref);
                 l += p[e];
-                pf.v[e] = (_Float16)p[e];
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) high.p[e] = toward_zero(p[2 * e] * BELOW, p[2 * e + 1] * BELOW);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) low.v[e] = (_Float16)(p[e] - (float)high.v[e]);
             // values: two columns of eight keys at a time
 #pragma unroll
             for (int c = 0; c < W / 2; ++c) {
@@ -590,8 +598,10 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
                 }
                 Frag v0, v1;
                 transpose_keys(raw, v0, v1);
-                O[2 * c] = mfma16(v0.v, pf.v, O[2 * c]);
-                O[2 * c + 1] = mfma16(v1.v, pf.v, O[2 * c + 1]);
+                O[2 * c] = mfma16(v0.v, high.v, O[2 * c]);
+                O[2 * c + 1] = mfma16(v1.v, high.v, O[2 * c + 1]);
+                O[2 * c] = mfma16(v0.v, low.v, O[2 * c]);
+                O[2 * c + 1] = mfma16(v1.v, low.v, O[2 * c + 1]);
             }
             load_v(next, all);
             rows[0] = next[0];
