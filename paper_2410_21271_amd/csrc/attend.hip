@@ -268,9 +268,12 @@ __device__ __forceinline__ float lse_of(float m, float sum) { return LN2 * (m + 
 
 // Contributions c0, c0 + step, .. (`count` of them) of a unit, joined by one wavefront (wave 0 of 1) or by the workgroup (its wavefronts take
 // 64 float2 of the rows x dim of O in turn): the unit's result, or, for a group of contributions, a contribution in the place of the first.
+// Added up four at a time, in order, whatever CH and BATCH are, with nothing left to the compiler to fuse or not: a unit may have contributions from workgroups and from
+// wavefronts, either may be the last to arrive, and the bits are the same.
 template <int DIM, int CH, int BATCH>          // CH times 64 float2 and BATCH contributions are requested at a time
 __device__ __forceinline__ void join(const AttendArgs& a, const Parts& p, const Unit& u, unsigned c0, unsigned step, unsigned count, int nrows, int wave, int waves, bool final, float vs)
 {
+    static_assert(BATCH % 4 == 0, "contributions are added up four at a time");
     const int lane = threadIdx.x & 63, words = nrows * (DIM / 2);
     float m0 = -INFINITY, l0 = 0.f;
     for (int e0 = 64 * wave; e0 < words; e0 += 64 * waves * CH) {
@@ -295,28 +298,32 @@ __device__ __forceinline__ void join(const AttendArgs& a, const Parts& p, const 
 #pragma unroll
                 for (int i = 0; i < CH; ++i) x[k][i] = get2(src + 2 * a.rows + 2 * e[i]);
             }
-            float up = m;
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) up = fmaxf(up, ml[k].x);
-            const float f = factor(m, up);
-            l = m == -INFINITY ? l : l * f;
-            m = up;
+            for (int four = 0; four < BATCH; four += 4) {
+                if (c + four >= count) break;
+                float up = m;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const float g = __shfl(f, row[i], 64);
-                acc[i].x *= g;
-                acc[i].y *= g;
-            }
-#pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (c + k >= count) break;
-                const float fk = factor(ml[k].x, up);
-                l += ml[k].x == -INFINITY ? ml[k].y : ml[k].y * fk;
+                for (int k = four; k < four + 4; ++k) up = fmaxf(up, ml[k].x);
+                const float f = factor(m, up);
+                l = m == -INFINITY ? l : l * f;
+                m = up;
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const float gk = __shfl(fk, row[i], 64);
-                    acc[i].x += x[k][i].x * gk;
-                    acc[i].y += x[k][i].y * gk;
+                    const float g = __shfl(f, row[i], 64);
+                    acc[i].x *= g;
+                    acc[i].y *= g;
+                }
+#pragma unroll
+                for (int k = four; k < four + 4; ++k) {
+                    if (c + k >= count) break;
+                    const float fk = factor(ml[k].x, up);
+                    l = ml[k].x == -INFINITY ? l + ml[k].y : __builtin_fmaf(ml[k].y, fk, l);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const float gk = __shfl(fk, row[i], 64);
+                        acc[i].x = __builtin_fmaf(x[k][i].x, gk, acc[i].x);
+                        acc[i].y = __builtin_fmaf(x[k][i].y, gk, acc[i].y);
+                    }
                 }
             }
         }
