@@ -19,6 +19,8 @@
 #include "serving.hpp"
 #include "segments.hpp"
 
+#include <type_traits>
+
 namespace eora {
 namespace {
 
@@ -543,7 +545,7 @@ struct Up {
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
                 const int k = SHARE ? wave + NW * i : i, p = k / TILES, t = k % TILES, R = first + p < end ? first + p : end - 1;
-                const size_t tile = (size_t)R * ntk + (t < nt ? t : (nt ? nt - 1 : 0));      // (beyond the rank: the last tile again, times zeros)
+                const size_t tile = (size_t)R * ntk + (t < nt ? t : (nt ? nt - 1 : 0));      // (beyond the rank: the last tile again)
                 load_words<WORDS>(w[i], tiles + tile * (64 * WORDS));
             }
         };
@@ -663,33 +665,41 @@ struct Up {
             f4 acc[PB];
 #pragma unroll
             for (int p = 0; p < PB; ++p) acc[p] = f4{0.f, 0.f, 0.f, 0.f};
+            // Tiles of B behind the pair's rank are left out: with zeros of t, infinities in the tile that stands for them and scales of anything, NaN among it, would
+            // make NaN.  (In a copy of the loop of their own: 2048 rows of full rank take 1 % longer with a branch for each tile.)
+            auto multiply = [&](auto some) {
 #pragma unroll
-            for (int q = 0; q < TILES; ++q)
+                for (int q = 0; q < TILES; ++q) {
+                    if (decltype(some)::value && q >= nt) break;
 #pragma unroll
-                for (int p = 0; p < PB; ++p) {
-                    uint32_t now[WORDS];
-                    if constexpr (SHARE) {
-                        const uint32_t* src = stage + ((size_t)(buffer * STEP + p * TILES + q) * 64 + lane) * WORDS;
+                    for (int p = 0; p < PB; ++p) {
+                        uint32_t now[WORDS];
+                        if constexpr (SHARE) {
+                            const uint32_t* src = stage + ((size_t)(buffer * STEP + p * TILES + q) * 64 + lane) * WORDS;
 #pragma unroll
-                        for (int v = 0; v < WORDS; ++v) now[v] = src[v];
-                    } else {
+                            for (int v = 0; v < WORDS; ++v) now[v] = src[v];
+                        } else {
 #pragma unroll
-                        for (int v = 0; v < WORDS; ++v) now[v] = w[p * TILES + q][v];
-                    }
-                    h8 f[NF];
-                    decode_tile<FE>(now, 8u, f);
-                    f4 part = {0.f, 0.f, 0.f, 0.f};
-                    f4& sum = FE == S_F16 ? acc[p] : part;
+                            for (int v = 0; v < WORDS; ++v) now[v] = w[p * TILES + q][v];
+                        }
+                        h8 f[NF];
+                        decode_tile<FE>(now, 8u, f);
+                        f4 part = {0.f, 0.f, 0.f, 0.f};
+                        f4& sum = FE == S_F16 ? acc[p] : part;
 #pragma unroll
-                    for (int i = 0; i < NF; ++i) {
-                        sum = mfma16(f[i], high[q * NF + i], sum);
-                        sum = mfma16(f[i], low[q * NF + i], sum);
-                    }
-                    if constexpr (FE != S_F16) {
+                        for (int i = 0; i < NF; ++i) {
+                            sum = mfma16(f[i], high[q * NF + i], sum);
+                            sum = mfma16(f[i], low[q * NF + i], sum);
+                        }
+                        if constexpr (FE != S_F16) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[p][i] += (float)sc[p][(i * TILES + q) / 4][(i * TILES + q) % 4] * part[i];
+                            for (int i = 0; i < 4; ++i) acc[p][i] += (float)sc[p][(i * TILES + q) / 4][(i * TILES + q) % 4] * part[i];
+                        }
                     }
                 }
+            };
+            if (nt < TILES) multiply(std::true_type{});
+            else multiply(std::false_type{});
             const int most = 2 * (end - rb) - 1, at = piece < most ? piece : most, col = 16 * rb + 8 * at;
             // (without a pair the tiles are another's: whatever they give, -0 is added, which leaves base as it is)
 #pragma unroll
