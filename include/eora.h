@@ -347,7 +347,7 @@ int eora_linear_sp24_group(const void* x, const eora_sp_member* members, int n_m
  * workspace: eora_adapters_workspace_bytes() of the largest call.  Its bytes are ZERO before the first call (hipMemset, say); every call leaves it
  * usable for the next, of whatever sizes.  Up to 64 rows are one launch, in which a bounded wait (eora_debug_set_spin_limit()) hands t over:
  * eora_workspace_error() reports one that expired (y is then invalid, and the workspace to be zeroed again).
- * t = x.A^T is held in fp32 (multiplied with B's tiles as two fp16 of 22 bits together, whatever its magnitude); the sum with
+ * t = x.A^T is held in fp32 (multiplied with B's tiles as two fp16 of 20 bits together, whatever its magnitude); the sum with
  * base is rounded once.  Equal inputs give bit-equal outputs; a row's sums do not depend on the other rows'
  * contents, but may be split differently when M or the other rows' adapters change.
  * Constraints: M >= 0 (0: no-op), d_in % 128 == 0, d_out % 16 == 0, 1 <= n_adapters, r as for eora_linear_q (> 0).

@@ -14,8 +14,9 @@
 // a pair's work is cut into as many parts as there are workgroups for it.  So long runs of one pair (prompts) and a pair for each row (a batch of decoding requests) both fill the chip.
 // From 512 rows on they are put in the order of their pairs first (see Order).
 //
-// t is not rounded to fp16: each row's t is scaled by a power of two to a largest value in [256, 512) and split in two fp16 (22 bits, whatever the
-// size of t), both are multiplied with B's tile, and the sum is scaled back in fp32.  y is rounded once.
+// t is not rounded to fp16: each row's t is scaled by a power of two to a largest value in [256, 512) and split in two fp16 (20.7 bits, whatever the
+// size of t), both are multiplied with B's tile, and the sum is scaled back in fp32.  The first is cut off from a little below, so that both have t's sign: an infinite
+// element of B then gives an infinity, which halves of zero or of two signs would make a NaN.  y is rounded once.
 #include "serving.hpp"
 #include "segments.hpp"
 
@@ -639,14 +640,17 @@ struct Up {
         big = fmaxf(big, __shfl_xor(big, 32, 64));
         int ex = (int)(__float_as_uint(big) >> 23) - 127;  // exponent of the row's largest value
         ex = big == 0.f ? 8 : (ex < -110 ? -110 : (ex > 127 ? 127 : ex));
-        const float to = __uint_as_float((unsigned)(127 + 8 - ex) << 23), back = rank ? __uint_as_float((unsigned)(127 - 8 + ex) << 23) : 0.f;
+        const float to = __uint_as_float((unsigned)(127 + 8 - ex) << 23), below = to * (1.f - 0x1p-12f), back = rank ? __uint_as_float((unsigned)(127 - 8 + ex) << 23) : 0.f;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = t[k][e] * to;
-                high[k][e] = (_Float16)v;
-                low[k][e] = (_Float16)(fabsf(v) == INFINITY ? 0.f : v - (float)high[k][e]);
+            for (int e = 0; e < 8; e += 2) {
+                const h2 cut = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(t[k][e] * below, t[k][e + 1] * below));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    high[k][e + i] = cut[i];
+                    low[k][e + i] = (_Float16)fminf(t[k][e + i] * to - (float)cut[i], 512.f);        // (of an infinity 512, not NaN)
+                }
             }
 
         if constexpr (SHARE) {
