@@ -404,8 +404,15 @@ __device__ __forceinline__ T fetch(const char* p)
     else return *(const T*)p;
 }
 
+// The reductions' room in LDS
+struct Shared {
+    int scratch[NW];
+    float red_m[NW][16], red_l[NW][16];
+};
+
+// The run of workgroup g
 template <int DIM, int BITS, bool PAST>
-__global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const AttendArgs a)
+__device__ __forceinline__ void go(const AttendArgs& a, const Runs& runs, const int2* plan, unsigned g, float* red_o, Shared& shared)
 {
     constexpr int NT = DIM / 32;               // k-steps of the first product
     constexpr int W = DIM / 16;                // columns of V a lane holds, blocks of O^T
@@ -414,27 +421,12 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
     constexpr int VW = W * BYTES / 4;          // words of a value row a lane holds
     typedef uint32_t words __attribute__((ext_vector_type(VW < 4 ? VW : 4)));
     constexpr int VL = VW < 4 ? 1 : VW / 4;    // loads of a value row
+    // (where three wavefronts share a SIMD's registers, more float2 at a time spill: 37 requests of up to 1000 tokens 20.2 us with 4 and 4, 17.6)
+    constexpr int LONE_CH = DIM == 64 ? 2 : 4, LONE_BATCH = DIM == 64 ? 8 : 4;
 
-    __shared__ int scratch[NW];
-    __shared__ float red_m[NW][16], red_l[NW][16];
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    float* red_o = (float*)smem;               // NW x rows x DIM
-    int2* plan = (int2*)(red_o + NW * a.rows * DIM);
-
+    auto& red_m = shared.red_m;
+    auto& red_l = shared.red_l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
-    const unsigned g = blockIdx.x;
-    add_costs(a, plan, scratch);
-    __syncthreads();
-    // requests without a token have no unit
-    for (int b = (int)g; b < a.B; b += (int)gridDim.x) {
-        if (plan[b + 1].x != plan[b].x) continue;
-        for (int e = threadIdx.x; e < a.heads * (DIM / 8); e += THREADS) *(u4*)(a.out + (size_t)b * a.heads * DIM + 8 * e) = u4{0, 0, 0, 0};
-        if (a.lse)
-            for (int e = threadIdx.x; e < a.heads; e += THREADS) a.lse[(size_t)b * a.heads + e] = -INFINITY;
-    }
-    const Runs runs = runs_of(a, plan);
-    if (g >= runs.n) return;
-
     const bool together = together_at(a, runs, plan, g);
     unsigned at = runs.cut(NW * g + (together ? 0 : wave));
     const unsigned stop_at = runs.cut(NW * g + (together ? NW : wave + 1));
@@ -645,7 +637,7 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
                     for (int b = 0; b < W; b += 2) put2(part + 2 * a.rows + n * DIM + W * (4 * j + i) + b, O[b][i], O[b + 1][i]);
             }
             const unsigned w = NW * g + wave;
-            finish<DIM, 4, 4>(a, parts, u, g == parts.g0 ? w - parts.w0 : parts.first + (parts.g1 - parts.g0 - 1) + (w - NW * parts.g1), nrows, 0, 1, scratch, vs);
+            finish<DIM, LONE_CH, LONE_BATCH>(a, parts, u, g == parts.g0 ? w - parts.w0 : parts.first + (parts.g1 - parts.g0 - 1) + (w - NW * parts.g1), nrows, 0, 1, shared.scratch, vs);
             continue;
         }
 
@@ -703,8 +695,46 @@ __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const
         }
         if (full) continue;
         const Parts parts = parts_of(a, runs, plan, u);
-        finish<DIM, 2, 8>(a, parts, u, g == parts.g0 ? 0 : parts.first + (g - parts.g0 - 1), nrows, wave, NW, scratch, vs);
+        finish<DIM, 2, 8>(a, parts, u, g == parts.g0 ? 0 : parts.first + (g - parts.g0 - 1), nrows, wave, NW, shared.scratch, vs);
     }
+}
+
+// Past the caches where the requests hold so much (in whole tiles, and one a request): of less the last-level cache has some from the call before.  One cache call after call, then three
+// in turn, as a model's layers have them, through and past: 32 / 8 heads of 128, 104 MiB 25.5 and 28.3 us, 29.0 and 29.4; 120 MiB 27.9 and 29.0, 31.5 and 30.0; 512 MiB 93.1 and 81.4, 93.6
+// and 82.5; 13 heads of 64, 95 MiB 20.9 and 22.8, 23.5 and 23.9; 117 MiB 23.0 and 24.1, 27.6 and 24.9.  What they hold, not what their table has room for: with one of 131072 tokens, 1 request of
+// 8192 takes 19.7 past and 17.0 through, 8 of 500 12.2 and 11.0.
+constexpr size_t PAST_BYTES = (size_t)112 << 20;
+
+// WIDE: the table has room for so much, and the requests' lengths decide
+
+template <int DIM, int BITS, bool WIDE>
+__global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const AttendArgs a)
+{
+    __shared__ Shared shared;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    float* red_o = (float*)smem;               // NW x rows x DIM
+    int2* plan = (int2*)(red_o + NW * a.rows * DIM);
+
+    const unsigned g = blockIdx.x;
+    add_costs(a, plan, shared.scratch);
+    __syncthreads();
+    // requests without a token have no unit
+    for (int b = (int)g; b < a.B; b += (int)gridDim.x) {
+        if (plan[b + 1].x != plan[b].x) continue;
+        for (int e = threadIdx.x; e < a.heads * (DIM / 8); e += THREADS) *(u4*)(a.out + (size_t)b * a.heads * DIM + 8 * e) = u4{0, 0, 0, 0};
+        if (a.lse)
+            for (int e = threadIdx.x; e < a.heads; e += THREADS) a.lse[(size_t)b * a.heads + e] = -INFINITY;
+    }
+    const Runs runs = runs_of(a, plan);
+    if (g >= runs.n) return;
+    if constexpr (WIDE) {
+        const size_t held = (size_t)(unsigned)__builtin_amdgcn_readfirstlane(plan[a.B].x) * (unsigned)a.kv * (TILE * DIM * (BITS / 8) * 2);
+        if (held >= PAST_BYTES) {
+            go<DIM, BITS, true>(a, runs, plan, g, red_o, shared);
+            return;
+        }
+    }
+    go<DIM, BITS, false>(a, runs, plan, g, red_o, shared);
 }
 
 // query heads of a kv head in blocks of up to 16
@@ -715,11 +745,11 @@ void set_blocks(AttendArgs& a)
     a.rows = a.group < 16 ? a.group : 16;
 }
 
-template <int DIM, int BITS, bool PAST>
+template <int DIM, int BITS, bool WIDE>
 hipError_t start(AttendArgs& a, hipStream_t stream)
 {
     const size_t lds = NW * a.rows * DIM * sizeof(float) + ((size_t)a.B + 1) * sizeof(int2);
-    const auto kern = attend_kernel<DIM, BITS, PAST>;
+    const auto kern = attend_kernel<DIM, BITS, WIDE>;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
@@ -733,13 +763,12 @@ hipError_t start(AttendArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Past the caches where what the widest requests hold is half of the last-level cache or more (64 requests of 2048 tokens, 538 MB, 94.5 us through, 83.8 past; 64 of 527, 139 MB, 29.9,
-// 27.3; 160 to 8192 in 8 bits 214, 198); less may be there still from the call before (1 of 8192, 34 MB, 17.4, 20.0; 37 of up to 1000, 20.6, 22.1).
 template <int DIM, int BITS>
 hipError_t start(AttendArgs& a, hipStream_t stream)
 {
+    // (tables with no such room: the loop past the caches left out, 0.2 us of 7.5 for one request of 100 tokens)
     const size_t tokens = (size_t)a.width * a.page, seen = a.window > 0 && (size_t)a.window < tokens ? (size_t)a.window : tokens;
-    return a.B * seen * a.kv * DIM * (BITS / 8) * 2 >= ((size_t)128 << 20) ? start<DIM, BITS, true>(a, stream) : start<DIM, BITS, false>(a, stream);
+    return a.B * (seen + 2 * TILE) * a.kv * DIM * (BITS / 8) * 2 >= PAST_BYTES ? start<DIM, BITS, true>(a, stream) : start<DIM, BITS, false>(a, stream);
 }
 
 template <int DIM>
