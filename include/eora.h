@@ -396,8 +396,8 @@ int eora_cache_append(const void* q, const void* k, const void* v, const void* q
  * can be joined).  Several tokens of one request (a short prompt): one row each, with the lengths that each may see.
  * Scores, sums and out are fp32 until the end; a weight meets v with 20 bits (as two fp16).  Equal inputs give
  * bit-equal outputs; how the tokens are split between workgroups, and so the last bits, depends on the lengths of all requests.
- * workspace: eora_cache_attention_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its bytes are ZERO before the
- * first call (hipMemset, say); every call leaves it usable for the next, of whatever sizes.
+ * workspace: eora_cache_attention_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the
+ * first call (hipMemset, say), the rest may hold anything; every call leaves it usable for the next, of whatever sizes.
  * Constraints: 0 <= B <= 8192 (0: no-op), n_heads % n_kv_heads == 0, q_stride % 8 == 0, max_pages >= 1,
  * max_pages * page_size <= 2^30, B * (heads in blocks of 16) * max_tokens / 32 < 2e9, scale finite, the cache's above.
  * Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits) / SHAPE / VALUE (scale) / ALIGN / WORKSPACE / LAUNCH. */

@@ -35,7 +35,7 @@ constexpr int START = 1;                       // what beginning a unit costs, i
 // Cost of a workgroup's run at least, where a join costs more than a longer run.  Requests of one length (1 of 8192 tokens, 4 of 4096 in 8 bits: 10: 17.0, 18.8 us; 20: 17.4, 15.7;
 // 40: 20.8, 17.0), of several (37 of up to 1000 tokens, 13 heads of 64: 4: 20.6; 8: 20.1; 16: 23.1)
 constexpr int MIN_RUN = 20, FEW = 8;
-constexpr int MAX_WG = 1024;
+constexpr int MAX_WG = 1024;                   // workgroups that there are counters for
 constexpr int SLOTS = 2 * NW * MAX_WG;
 constexpr int COUNTERS = SLOTS + NW * MAX_WG;  // words before the partial results: a counter for each group of them, and for each unit
 constexpr float RAISE = 4.f, LOWER = 11.f;     // (2^15 is below fp16's 65504; raised less often, by 8, 64 requests of 1 to 4096 tokens take the same)
@@ -395,6 +395,8 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w)
 // 59.6 to 58.8.
 template <int DIM>
 constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
+constexpr int CUS = 256;
+static_assert(CUS * residents<64>() <= MAX_WG, "a launch of more workgroups than there are counters for");
 
 // Keys and values past the caches (once read, of no more use), or through them
 template <bool PAST, typename T>
@@ -758,7 +760,7 @@ hipError_t start(AttendArgs& a, hipStream_t stream)
     int each = (int)(159 * 1024 / (lds + 1024));
     each = each < residents<DIM>() ? each : residents<DIM>();
     const size_t most = (size_t)a.B * a.kv * a.hblocks * (((size_t)a.width * a.page + TILE - 1) / TILE + START + 1) / NW + 1;
-    a.nwg = most < (size_t)256 * each ? (int)most : 256 * each;
+    a.nwg = most < (size_t)CUS * each ? (int)most : CUS * each;
     kern<<<a.nwg, THREADS, lds, stream>>>(a);
     return hipGetLastError();
 }
@@ -785,7 +787,11 @@ size_t attend_workspace_bytes(int heads, int kv, int dim)
     a.heads = heads;
     a.kv = kv;
     set_blocks(a);
-    return ((size_t)COUNTERS + (size_t)2 * NW * MAX_WG * a.rows * (dim + 2)) * sizeof(float);
+    // two partial results a wavefront that a launch may have (a workspace for wide heads also serves narrower ones, of which there are more at a time)
+    size_t row = CUS * residents<64>() * (64 + 2);
+    if (dim >= 128 && row < CUS * residents<128>() * (128 + 2)) row = CUS * residents<128>() * (128 + 2);
+    if (dim >= 256 && row < CUS * residents<256>() * (256 + 2)) row = CUS * residents<256>() * (256 + 2);
+    return ((size_t)COUNTERS + 2 * NW * row * a.rows) * sizeof(float);
 }
 
 hipError_t launch_attend(AttendArgs a, hipStream_t stream)
