@@ -389,7 +389,7 @@ int eora_cache_append(const void* q, const void* k, const void* v, const void* q
  * over tokens max(0, lengths[b] - window) <= t < lengths[b] (window 0: all).  Token t is token t % page_size of page
  * page_table[b][t / page_size].
  * q: fp16, B rows q_stride elements apart.  page_table: B x max_pages int32; entries outside [0, n_pages) are no page: their
- * tokens are masked, as are scores of -inf.  lengths: B int32, taken as 0 .. max_pages * page_size.  A request without a
+ * tokens are masked and what lies there is not used; a score of -inf is a weight of 0.  lengths: B int32, taken as 0 .. max_pages * page_size.  A request without a
  * token (length 0, or all masked) has out = 0 and lse = -inf.  What the cache holds in other places is
  * never used, NaN included.
  * out: fp16 B x n_heads x head_dim; lse: fp32 B x n_heads or NULL (natural logarithm: with it results over parts of a cache

@@ -3,11 +3,11 @@
 //      y[m] = base[m] + s_a (x[m] A_a^T) B_a^T            a = adapter of row m, from a pool of any size
 //
 // Two parts: t = x A^T (fp32 partial sums of ranges of the contraction), then y from t and B.  One launch for up to 64 rows, where each of two would be half the time
-// (1 row 1024 -> 1024, rank 64: 7.5 us in one, 10.1 in two), two beyond.  Only the pairs that rows select are read, in the stored tiles of the layer kernels.
+// (1 row 1024 -> 1024, rank 64: 7.2 us in one, 9.8 in two; 64 of 256 pairs 4096 -> 4096, rank 128: 20.3, 22.3), two beyond.  Only the pairs that rows select are read, in the stored tiles of the layer kernels.
 //
 // Bound by memory at a few rows per pair (4 r flops a row against 2 bytes of a factor's element): the rows of a pair are the 16 columns (or rows)
-// of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight (64 requests, 4096 -> 4096, rank 128: 76 MB in 20.6 us).  With many rows of one pair, y's
-// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 69 us).
+// of the matrix instructions, mostly empty, and a wavefront's work is to keep tiles in flight (64 requests, 4096 -> 4096, rank 128: 76 MB in 20.3 us).  With many rows of one pair, y's
+// own traffic bounds it (2048 rows, 4096 -> 14336: 158 MB in 68 us).
 //
 // Rows by pairs: below 512 rows without sorting, in windows of 64 rows, an adapter index a lane; as many ballots as an index has bits give each lane the rows of its pair, and
 // the first row of each pair (its leader) its place among the window's pairs.  Every window has the same number of workgroups, which share its pairs out:
@@ -480,7 +480,7 @@ struct Wait {
             unsigned v = 0;
             if ((threadIdx.x & 63) == 0) v = ld_relaxed(a.header + READY + LINE * first);
             there = (unsigned)__builtin_amdgcn_readfirstlane(v) >= need;
-            if (!there) __builtin_amdgcn_s_sleep(20);        // (looking more often delays the counting: 1 row 4096 -> 14336 13.9 us with 2, 10.9)
+            if (!there) __builtin_amdgcn_s_sleep(20);        // (looking more often delays the counting: 1 row 4096 -> 14336 13.5 us with 2, 10.2)
         }
         if (!there && (threadIdx.x & 63) == 0) __hip_atomic_store(a.header + HDR_ERROR, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("" ::: "memory");                    // nothing of t is requested before
@@ -722,7 +722,7 @@ struct Up {
                 for (int i = 0; i < INS; ++i) {
                     _Float16* to = a.y + moved[i] + col;
                     if constexpr (SHARE) to = here > 0 ? to : nowhere + 512 * i;
-                    // (many rows: past L2, which has B's tiles and base to hold: 2048 rows, 4096 -> 14336, 72.4 us, 69.1; 30000 rows 1024 -> 2048 110, 92; followed by a reader of y the
+                    // (many rows: past L2, which has B's tiles and base to hold: 2048 rows, 4096 -> 14336, 71.1 us, 68.1; 30000 rows 1024 -> 2048 118.5, 115; followed by a reader of y the
                     // same as without)
                     if constexpr (SHARE) __builtin_nontemporal_store(y[i], (h8*)to);
                     else *(h8*)to = y[i];
@@ -854,8 +854,8 @@ __global__ __launch_bounds__(THREADS, NK <= 8 ? 2 : 1) void adapters_kernel(cons
 }
 
 // How a call goes: in one launch, in two by windows of 64 rows, in two by batches of 2048 in order.  Ordering costs 4 to 6 us and saves B's being read in every window (4096 -> 4096,
-// by windows and in order: 1024 rows of 64 pairs in turn, rank 64, 100 and 40 us; rank 128, 512 rows of 16 pairs in turn 22 and 23.5, 256 rows 17 and 22; 8192 rows of 16 pairs in turn 195
-// and 74, in runs of 60 99 and 97, of one pair 63 and 68).
+// by windows and in order: 1024 rows of 64 pairs in turn, rank 64, 83 and 31 us; rank 128, 512 rows of 16 pairs in turn 21.9 and 22.8, of one pair 18.9 and 22.0, 256 rows of 16 in turn 17.1 and
+// 23.0; 8192 rows of 16 pairs in turn 280 and 84.5, in runs of 60 134 and 116, of one pair 94 and 81).  By the number of rows alone: what the indices are the host does not know.
 enum Form { ONE_LAUNCH, WINDOWS, ORDERED };
 constexpr int MANY = 512;                      // rows from which they are put in order
 
@@ -935,8 +935,8 @@ hipError_t launch_adapters(AdapterArgs args, int fa, int fe, hipStream_t stream)
             a.down_wgs = down < 256 ? down : 256;
             a.up_wgs = up < 256 ? up : 256;
         } else {
-            // First: one workgroup a compute unit, with two chunks in its registers (two: 2048 rows 44 us, 48), but with more batches 128 each while that is no more than four a
-            // compute unit (8192 rows of one pair, 4096 -> 4096, with 64 each 71 us, 62).  Second: two.
+            // First: one workgroup a compute unit, with two chunks in its registers (two: 2048 rows 68.1 us, 71.9), but with more batches 128 each while that is no more than four a
+            // compute unit (8192 rows of one pair, 4096 -> 4096, with 64 each 83.3 us, 80.7; in runs of 60 119, 116; of 16 in turn 82.1, 84.5).  Second: two.
             a.down_wgs = form == WINDOWS || parts == 1 ? 256 / parts : (parts < 8 ? 128 : 1024 / parts);
             a.up_wgs = 512 / parts;
             const unsigned grid = (unsigned)parts * a.down_wgs;

@@ -3,8 +3,8 @@
 //      s_t = scale q . k_t,   out = sum_t 2^(s_t log2 e - m) v_t / sum_t 2^(s_t log2 e - m)       lo <= t < length
 //
 // Bound by memory: every key and value is read once (the query heads of a kv head, up to 16, share one read as the columns of the
-// matrix instructions), against 4 flops per query head and cached value.  32 / 8 heads of 128: 64 requests of 2048 tokens in 83.8 us, 6.4 TB/s, of 1 to 4096 (138 MB) in 38.4; 64 / 8 heads in
-// 8 bits: one of 131072 (268 MB) in 55.8, 160 to 8192 (1089 MB) in 198.
+// matrix instructions), against 4 flops per query head and cached value.  32 / 8 heads of 128: 64 requests of 2048 tokens in 83.8 us, 6.4 TB/s, of 1 to 4096 (138 MB) in 38.3; 64 / 8 heads in
+// 8 bits: one of 131072 (268 MB) in 56, 160 to 8192 (1089 MB) in 197.5.
 //
 // Tile: 32 keys a wavefront.  S^T = K Q^T: a lane (n = lane % 16, j = lane / 16) holds row n of K as the first operand, so an fp16 key row is read in
 // pieces of 64 bytes, and ends with the scores of head n for keys 4j + i and 16 + 4j + i: exactly its eight k-slots of the second product
@@ -14,9 +14,10 @@
 //
 // Softmax: m is a reference, common to the lanes of a head, not the exact maximum: LOWER below it when it is set, raised, and O and the sum rescaled, only when a score
 // has risen by RAISE or more since.  So the largest weight is 2^11 to 2^15, and one of 2^-36 of it still 2^-25, the least that fp16 rounds to anything: tokens far
-// below the largest, of which there may be many, keep their part (with a largest weight of 1, 4000 of them 16 and 17 nats below it were off by 0.3 and 1.9 %).  Scores, sums and O are fp32.  A weight meets V as two fp16, the second what the first leaves of it: 20.7 bits together, beside which the
-// rounding of the result is all that shows (one fp16 put out off by up to 2^-12 of sum p |v|).  The first is cut off from a little
-// below the weight, so that the second is positive as well: an infinite value then gives an infinity, which halves of zero or of two signs would make a NaN.
+// below the largest, of which there may be many, keep their part (with a largest weight of 1, 4000 of them 16 and 17 nats below it were off by 0.3 and 1.9 %).
+// Scores, sums and O are fp32.  A weight meets V as two fp16, the second what the first leaves of it: 20.7 bits together, beside which the rounding of the result is all
+// that shows (one fp16 put out off by up to 2^-12 of sum p |v|).  The first is cut off from a little below the weight, so that the second is positive as well: an infinite
+// value then gives an infinity, which halves of zero or of two signs would make a NaN (and does where a weight is below 2^-24 of the largest).
 //
 // Split: all units (a request's kv head, or block of 16 of its query heads) in one row are cut into equal runs, whatever the lengths are: a request of 100 000
 // tokens is spread over the whole chip, and one of 10 costs a tile.  A workgroup whose run lies in one unit works on it together and adds up in
@@ -30,10 +31,9 @@ namespace {
 
 constexpr int NW = 4, THREADS = 64 * NW;
 constexpr int TILE = 32;
-// (Measured sides below: loads through the caches throughout.)
-constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs; with 2, 64 requests of 1 to 4096 tokens 40.6 -> 41.4 us)
-// Cost of a workgroup's run at least, where a join costs more than a longer run.  Requests of one length (1 of 8192 tokens, 4 of 4096 in 8 bits: 10: 17.0, 18.8 us; 20: 17.4, 15.7;
-// 40: 20.8, 17.0), of several (37 of up to 1000 tokens, 13 heads of 64: 4: 20.6; 8: 20.1; 16: 23.1)
+constexpr int START = 1;                       // what beginning a unit costs, in tiles (see Runs; with 2, 64 requests of 1 to 4096 tokens 38.3 -> 38.8 us)
+// Cost of a workgroup's run at least, where a join costs more than a longer run.  Requests of one length (1 of 8192 tokens, 4 of 4096 in 8 bits: 10: 16.8, 18.8 us; 20: 17.1, 15.8;
+// 40: 20.5, 17.6), of several (37 of up to 1000 tokens, 13 heads of 64: 4: 18.6; 8: 17.9; 16: 22.7)
 constexpr int MIN_RUN = 20, FEW = 8;
 constexpr int MAX_WG = 1024;                   // workgroups that there are counters for
 constexpr int SLOTS = 2 * NW * MAX_WG;
@@ -192,7 +192,7 @@ __device__ __forceinline__ Unit unit_after(const AttendArgs& a, const int2* plan
 
 // Whether the wavefronts of a workgroup go through its run together, tile by tile in turn, with their results added up in LDS at each unit's end: in one unit,
 // or where units are long.  Otherwise each has a quarter of the run for itself (short units would leave three of four idle).
-// From so many tiles a unit on (64 requests of 1 to 4096 tokens, 37 of up to 1000: 4: 42.2, 23.4 us; 8: 40.6, 20.1; 16: 43.7, 20.1)
+// From so many tiles a unit on (64 requests of 1 to 4096 tokens, 37 of up to 1000: 4: 40.7, 22.9 us; 8: 38.3, 17.9; 16: 39.9, 17.9)
 constexpr unsigned LONG = 8;
 __device__ __forceinline__ bool together_at(const AttendArgs& a, const Runs& r, const int2* plan, unsigned g)
 {
@@ -391,7 +391,7 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w)
 }
 
 // Wavefronts a SIMD: what the registers leave room for, which hold one tile and, at D = 256, 64 words of O.  Eight wavefronts a compute unit have 64 to 128 KiB
-// in flight; with a second tile in registers, for half the wavefronts, 64 requests of 1 to 4096 tokens go from 40.6 us to 44.5, 160 to 8192 in 8 bits from 215 to 229, one of 131072 from
+// in flight; with a second tile in registers, for half the wavefronts, and loads through the caches, 64 requests of 1 to 4096 tokens went from 40.6 us to 44.5, 160 to 8192 in 8 bits from 215 to 229, one of 131072 from
 // 59.6 to 58.8.
 template <int DIM>
 constexpr int residents() { return DIM == 64 ? 3 : (DIM == 128 ? 2 : 1); }
