@@ -708,7 +708,6 @@ __device__ __forceinline__ void go(const AttendArgs& a, const Runs& runs, const 
 constexpr size_t PAST_BYTES = (size_t)112 << 20;
 
 // WIDE: the table has room for so much, and the requests' lengths decide
-
 template <int DIM, int BITS, bool WIDE>
 __global__ __launch_bounds__(THREADS, residents<DIM>()) void attend_kernel(const AttendArgs a)
 {
