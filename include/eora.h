@@ -408,6 +408,52 @@ int eora_cache_attention(const void* q, const void* pages_k, const void* pages_v
                          int n_pages, int page_size, int cache_bits, int max_pages, int window, float scale,
                          void* workspace, size_t workspace_bytes, void* stream);
 
+/* The cache with a scale for each block: e4m3 codes as above, and beside them pages_k_scales, pages_v_scales: n_pages x n_kv_heads x page_size / 16 bytes, one
+ * for each 16 tokens of a page and head.  A byte e + 127 says that the block's codes stand for code * 2^e (the powers of OCP microscaling formats), -15 <= e <= 8; bytes outside
+ * 112 .. 135 are taken as the nearest of these.  Every code of such a block stands for a number that fp16 holds exactly (at e = 8 the codes to 240).
+ *
+ * eora_cache_append() into such a cache, the scales found as the tokens come: e is the least with max |x| <= 448 * 2^e over the block's finite values (at most
+ * 8, at least -15).  A call that stores token 0 of a block begins it anew, from the values of this call alone; otherwise e only grows from what the block has,
+ * and codes that are there already are rounded again, ties to even, to the new power (exact unless they become subnormal).  Stored is the nearest code of x / 2^e,
+ * saturating at 448 (240 with e = 8); NaN is kept, and an infinity saturates.
+ * The rows of a call whose slots share a block lie among 16 consecutive rows (as the tokens of a request do that are given in order; rows that are not
+ * stored may lie between).  Where they do not, the contents of that block, and its scales, are undefined.  Two rows with one slot: which is stored is undefined.
+ * All else, and the errors, as for eora_cache_append() with cache_bits 8; bytes of scales need no alignment. */
+int eora_cache_append_blocks(const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
+                             const void* rotations, const void* positions, const void* slots, void* q_out,
+                             void* pages_k, void* pages_v, void* pages_k_scales, void* pages_v_scales,
+                             int M, int n_heads, int n_kv_heads, int head_dim, int q_stride, int k_stride, int v_stride,
+                             int rot_dim, int interleaved, int n_positions, float eps, int n_pages, int page_size, void* stream);
+
+/* Tokens slots[m] (M int64) of a cache as fp16 rows: k, v: M x n_kv_heads x head_dim.  scale_block 0: k_scale and v_scale by head (cache_bits 8) or NULL
+ * (16), values rounded once; 16 (cache_bits 8 only): bytes by block, exact.  Slots outside [0, n_pages * page_size): rows of zeros.
+ * Constraints: M >= 0 (0: no-op), the cache's.  Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits, scale_block) / SHAPE / ALIGN / LAUNCH. */
+int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scale, const void* v_scale, const void* slots, void* k, void* v,
+                    int M, int n_kv_heads, int head_dim, int n_pages, int page_size, int cache_bits, int scale_block, void* stream);
+
+/* Attention of several tokens of each request over its pages, with a window and first tokens that stay visible.  Rows row_starts[b] .. row_starts[b + 1] - 1 of q (M rows in all) are the
+ * last tokens of request b, whose tokens (theirs among them) are in the cache: row i of n has position p = lengths[b] - n + i and sees the tokens
+ *      t <= p  with  t > p - window  or  t < sinks          (window 0: all t <= p),
+ * for query head i of kv head i / (n_heads / n_kv_heads) as in eora_cache_attention(), with pages, scores and lse as there.  A row that sees nothing (a position below 0, all
+ * masked) has out = 0 and lse = -inf.  What a row does not see is never used for it, NaN and infinities included, also where other rows see it.
+ * row_starts: B + 1 int32, not decreasing, taken as 0 .. M; rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
+ * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.
+ * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits in the form for single tokens,
+ * else as one fp16 (rounded to nearest, the largest 2^11 or more).  Equal inputs give bit-equal outputs; how tokens are split between workgroups, and so the last bits, depends on
+ * the lengths and rows of all requests.
+ * workspace: eora_cache_attention_rows_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the first call, the rest
+ * may hold anything; every call leaves it usable for the next, of whatever sizes and of either form.
+ * Constraints: M >= 0, 0 <= B <= 8192 (M or B 0: no-op), n_heads % n_kv_heads == 0, q_stride % 8 == 0, max_pages >= 1, max_pages * page_size <= 2^30,
+ * window >= 0, sinks >= 0, scale finite, (M * n_heads / 128 + B * n_kv_heads) < 8e6, M * (n_heads / n_kv_heads) < 2^31; without row_starts as
+ * eora_cache_attention(); the cache's.
+ * Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits, scale_block) / SHAPE / VALUE (scale) / ALIGN / WORKSPACE / LAUNCH. */
+size_t eora_cache_attention_rows_workspace_bytes(int M, int B, int n_heads, int n_kv_heads, int head_dim, int max_tokens);      /* 0: invalid */
+int eora_cache_attention_rows(const void* q, const void* pages_k, const void* pages_v, const void* k_scale, const void* v_scale,
+                              const void* page_table, const void* lengths, const void* row_starts, void* out, void* lse,
+                              int M, int B, int n_heads, int n_kv_heads, int head_dim, int q_stride,
+                              int n_pages, int page_size, int cache_bits, int scale_block, int max_pages, int window, int sinks, float scale,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Parity exports (integer / exact work, compared bit for bit against the CPU oracle).
  * ------------------------------------------------------------------------------------------ */

@@ -102,3 +102,87 @@ def cache_attention(q, pages_k, pages_v, page_table, lengths, window, scale):
             most[b, i] = np.abs(V).max()
             logit[b, i] = (abs(scale) * (np.abs(K) @ np.abs(q[b, i]))).max()
     return out, lse, size, most, logit
+
+
+# ---------------------------------------------------------------------------------------------------- scales by block
+BLOCK = 16
+LEAST_POWER, MOST_POWER = -15, 8
+
+
+def block_power(values):
+    """The least e of -15 .. 8 with |x| <= 448 2^e for all finite values (8 where there is none)."""
+    x = np.abs(np.asarray(values, np.float64))
+    top = x[np.isfinite(x)].max(initial=0.0)
+    e = LEAST_POWER
+    while e < MOST_POWER and top > E4M3_MAX * 2.0 ** e:
+        e += 1
+    return e
+
+
+def block_codes(x, e):
+    """Values of the nearest codes to x / 2^e: at most 448, or 240 where e is 8."""
+    most = 240.0 if e == MOST_POWER else E4M3_MAX
+    return e4m3_nearest(np.clip(np.asarray(x, np.float64) / 2.0 ** e, -most, most))
+
+
+def cache_append_blocks(rows, slots, codes, powers):
+    """rows: M x kv x dim, keys (turned) or values, float64; codes: n_pages x kv x page x dim, values of the codes; powers: n_pages x kv x page / 16.
+    Changes codes and powers."""
+    n_pages, kv, page, _ = codes.shape
+    mine = {}
+    for m, s in enumerate(int(s) for s in slots):
+        if 0 <= s < n_pages * page:
+            mine.setdefault(s // BLOCK, []).append((s % BLOCK, m))
+    for block, got in mine.items():
+        p, i = block * BLOCK // page, block * BLOCK % page // BLOCK
+        for h in range(kv):
+            e = block_power(np.stack([rows[m, h] for _, m in got]))
+            old = min(max(int(powers[p, h, i]), LEAST_POWER), MOST_POWER)
+            here = codes[p, h, BLOCK * i:BLOCK * i + BLOCK]
+            if all(place != 0 for place, _ in got):
+                e = max(e, old)
+                if e != old:
+                    here[:] = block_codes(here * 2.0 ** old, e)
+            for place, m in got:
+                here[place] = block_codes(rows[m, h], e)
+            powers[p, h, i] = e
+
+
+def cache_attention_rows(q, pages_k, pages_v, page_table, lengths, row_starts, window, sinks, scale):
+    """q: M x heads x dim; pages: n_pages x kv x page x dim, float64 values.  row_starts None: one row a request.  Rows of no request are NaN.
+    Returns (out, lse, sum of p |v|, largest |v|, largest sum of |scale q k|)."""
+    M, heads, dim = q.shape
+    n_pages, kv, page, _ = pages_k.shape
+    B = page_table.shape[0]
+    starts = np.arange(B + 1) if row_starts is None else np.clip(np.asarray(row_starts, np.int64), 0, M)
+    out, size = np.full((M, heads, dim), np.nan), np.zeros((M, heads, dim))
+    lse, most, logit = np.full((M, heads), np.nan), np.zeros((M, heads)), np.zeros((M, heads))
+    for b in range(B):
+        n, rows = min(max(int(lengths[b]), 0), page_table.shape[1] * page), int(starts[b + 1] - starts[b])
+        t = np.arange(n)
+        paged = (page_table[b, t // page] >= 0) & (page_table[b, t // page] < n_pages)
+        for r in range(rows):
+            m, p = int(starts[b]) + r, n - rows + r
+            see = paged & (t <= p)
+            if window:
+                see &= (t > p - window) | (t < sinks)
+            at = t[see]
+            out[m], lse[m] = 0.0, -np.inf
+            if not len(at):
+                continue
+            pages, place = page_table[b, at // page], at % page
+            for i in range(heads):
+                h = i // (heads // kv)
+                K, V = pages_k[pages, h, place], pages_v[pages, h, place]
+                with np.errstate(invalid="ignore"):
+                    s = scale * (K @ q[m, i])
+                    top = s.max()
+                    if top == -np.inf:
+                        continue
+                    w = np.exp(s - top)
+                    out[m, i] = ((w @ V) if np.isfinite(V).all() else np.where(w[:, None] == 0, 0.0, w[:, None] * V).sum(0)) / w.sum()
+                    size[m, i] = (w @ np.abs(V)) / w.sum()
+                    lse[m, i] = top + math.log(w.sum())
+                    most[m, i] = np.abs(V).max()
+                    logit[m, i] = (abs(scale) * (np.abs(K) @ np.abs(q[m, i]))).max()
+    return out, lse, size, most, logit

@@ -87,6 +87,10 @@ def _load():
         "eora_cache_append": (ci, [vp] * 13 + [ci] * 10 + [ctypes.c_float] + [ci] * 3 + [vp]),
         "eora_cache_attention_workspace_bytes": (sz, [ci] * 5),
         "eora_cache_attention": (ci, [vp] * 9 + [ci] * 10 + [ctypes.c_float, vp, sz, vp]),
+        "eora_cache_append_blocks": (ci, [vp] * 13 + [ci] * 10 + [ctypes.c_float] + [ci] * 2 + [vp]),
+        "eora_cache_read": (ci, [vp] * 7 + [ci] * 7 + [vp]),
+        "eora_cache_attention_rows_workspace_bytes": (sz, [ci] * 6),
+        "eora_cache_attention_rows": (ci, [vp] * 10 + [ci] * 13 + [ctypes.c_float, vp, sz, vp]),
         "eora_factors_workspace_bytes": (sz, [ci, ci, ci]),
         "eora_factors_store_f16": (ci, [vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp]),
         "eora_factors_store_q": (ci, [vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp]),
@@ -109,7 +113,8 @@ EXPORTS = ["eora_status_string", "eora_qweight_bytes", "eora_qzeros_bytes", "eor
            "eora_factors_workspace_bytes", "eora_factors", "eora_linear_q_multi", "eora_pack_factor_q3", "eora_factors_store_f16", "eora_factors_store_q", "eora_linear_sp24_group",
            "eora_debug_last_launch", "eora_debug_probe", "eora_linear_q_static", "eora_debug_set_resident_min_blocks", "eora_debug_set_factors_route",
            "eora_debug_prefill_parts", "eora_debug_factors_near", "eora_debug_factors_parts", "eora_debug_prefill_plan", "eora_debug_last_prefill",
-           "eora_adapters_workspace_bytes", "eora_linear_adapters", "eora_cache_append", "eora_cache_attention_workspace_bytes", "eora_cache_attention"]
+           "eora_adapters_workspace_bytes", "eora_linear_adapters", "eora_cache_append", "eora_cache_attention_workspace_bytes", "eora_cache_attention",
+           "eora_cache_append_blocks", "eora_cache_read", "eora_cache_attention_rows_workspace_bytes", "eora_cache_attention_rows"]
 
 
 def status_string(status):
@@ -437,6 +442,34 @@ def cache_attention(q, pages_k, pages_v, k_scale, v_scale, page_table, lengths, 
     _check(lib.eora_cache_attention(_dp(q), _dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), _dp(page_table), _dp(lengths),
                                     _dp(out), _dp(lse), B, n_heads, n_kv_heads, head_dim, q_stride, n_pages, page_size, cache_bits,
                                     max_pages, window, scale, _dp(workspace), _nbytes(workspace), _stream()), "cache_attention")
+
+
+def cache_append_blocks(q, k, v, q_weight, k_weight, rotations, positions, slots, q_out, pages_k, pages_v, pages_k_scales, pages_v_scales, M,
+                        n_heads, n_kv_heads, head_dim, q_stride, k_stride, v_stride, rot_dim, interleaved, n_positions, eps, n_pages, page_size):
+    _check(lib.eora_cache_append_blocks(_dp(q), _dp(k), _dp(v), _dp(q_weight), _dp(k_weight), _dp(rotations), _dp(positions), _dp(slots),
+                                        _dp(q_out), _dp(pages_k), _dp(pages_v), _dp(pages_k_scales), _dp(pages_v_scales), M, n_heads, n_kv_heads, head_dim,
+                                        q_stride, k_stride, v_stride, rot_dim, int(bool(interleaved)), n_positions, eps, n_pages, page_size,
+                                        _stream()), "cache_append_blocks")
+
+
+def cache_read(pages_k, pages_v, k_scale, v_scale, slots, k, v, M, n_kv_heads, head_dim, n_pages, page_size, cache_bits, scale_block):
+    _check(lib.eora_cache_read(_dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), _dp(slots), _dp(k), _dp(v), M, n_kv_heads, head_dim,
+                               n_pages, page_size, cache_bits, scale_block, _stream()), "cache_read")
+
+
+def cache_attention_rows_workspace_bytes(M, B, n_heads, n_kv_heads, head_dim, max_tokens):
+    return lib.eora_cache_attention_rows_workspace_bytes(M, B, n_heads, n_kv_heads, head_dim, max_tokens)
+
+
+def new_attention_rows_workspace(M, B, n_heads, n_kv_heads, head_dim, max_tokens):
+    return _torch.zeros(cache_attention_rows_workspace_bytes(M, B, n_heads, n_kv_heads, head_dim, max_tokens), dtype=_torch.uint8, device="cuda")
+
+
+def cache_attention_rows(q, pages_k, pages_v, k_scale, v_scale, page_table, lengths, row_starts, out, lse, M, B, n_heads, n_kv_heads, head_dim,
+                         q_stride, n_pages, page_size, cache_bits, scale_block, max_pages, window, sinks, scale, workspace):
+    _check(lib.eora_cache_attention_rows(_dp(q), _dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), _dp(page_table), _dp(lengths), _dp(row_starts),
+                                         _dp(out), _dp(lse), M, B, n_heads, n_kv_heads, head_dim, q_stride, n_pages, page_size, cache_bits, scale_block,
+                                         max_pages, window, sinks, scale, _dp(workspace), _nbytes(workspace), _stream()), "cache_attention_rows")
 
 
 # ------------------------------------------------------------------ calibration (Alg. 1 steps 1-6)

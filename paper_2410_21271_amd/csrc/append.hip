@@ -9,33 +9,13 @@
 // exchange (with eight neighbouring columns a lane, the partners fetched from another one and the sum over LDS, the instructions of a value bound it: 96 us).  The sum of squares is three to five
 // exchanges within a row of lanes.  A workgroup belongs to one token and keeps the token's (cos, sin) and the weights in registers over all heads that it
 // passes; few tokens are cut over several workgroups.  All arithmetic is in fp32; a value is rounded once, when it is stored.
+#include "heads.hpp"
 #include "serving.hpp"
-#include "tiles.hpp"
 
 namespace eora {
 namespace {
 
 constexpr int THREADS = 256;
-
-// v plus the value of another lane of its row of 16
-template <int CTRL>
-__device__ __forceinline__ float plus_dpp(float v)
-{
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
-// sum over the LPH lanes of a head, in all of them
-template <int LPH>
-__device__ __forceinline__ float sum_of_head(float v)
-{
-    v = plus_dpp<0xB1>(v);                                // lanes 1, 0, 3, 2 of each four
-    v = plus_dpp<0x4E>(v);                                // lanes 2, 3, 0, 1
-    v = plus_dpp<0x141>(v);                               // the eight lanes mirrored: the other four
-    if constexpr (LPH >= 16) v = plus_dpp<0x140>(v);      // the sixteen mirrored: the other eight
-    if constexpr (LPH >= 32) v += __shfl_xor(v, 16, 64);
-    return v;
-}
-
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
 template <int DIM, bool Q8, bool INTERLEAVED>
 __global__ __launch_bounds__(THREADS) void append_kernel(const AppendArgs a)

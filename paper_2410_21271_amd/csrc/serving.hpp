@@ -1,5 +1,5 @@
 // Internal launch interface of the operators between a decoder layer's linears: many requests' adapters (adapters.hip),
-// head norms and rotations into the cache (append.hip), attention over the cache (attend.hip).
+// head norms and rotations into the cache (append.hip, blocks.hip), attention over the cache (attend.hip, attend_far.hip, prompt.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -32,18 +32,67 @@ struct AppendArgs {
 };
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
 
+// A cache with a scale for each block: 16 tokens of a page and head share a power of two, a byte e + 127 (n_pages x kv x page / 16)
+constexpr int BLOCK_TOKENS = 16;
+constexpr int SCALE_LEAST = -15, SCALE_MOST = 8;
+
+struct BlocksArgs {
+    const _Float16* q;              // as AppendArgs
+    const _Float16* k;
+    const _Float16* v;
+    const _Float16* q_weight;
+    const _Float16* k_weight;
+    const float* rotations;
+    const int* positions;
+    const long long* slots;
+    _Float16* q_out;
+    void* pages_k;                  // codes
+    void* pages_v;
+    uint8_t* k_scales;
+    uint8_t* v_scales;
+    int M, heads, kv, dim;
+    int q_stride, k_stride, v_stride;
+    int rot, interleaved, n_positions;
+    float eps;
+    int page;
+    unsigned n_slots;
+    int m0, tokens;                 // rows of this launch (these set by the launcher)
+    int slices;                     // workgroups per token for its queries
+    int look;                       // rows that a wavefront looks through for first rows of blocks
+};
+hipError_t launch_append_blocks(BlocksArgs a, hipStream_t stream);
+
+struct ReadArgs {
+    const void* pages_k;
+    const void* pages_v;
+    const void* k_scale;            // by head (float) or by block (bytes), or null
+    const void* v_scale;
+    const long long* slots;         // M
+    _Float16* k;                    // M x kv x dim
+    _Float16* v;
+    int M, kv, dim, page, bits;
+    bool blocks;
+    unsigned n_slots;
+};
+hipError_t launch_read(const ReadArgs& a, hipStream_t stream);
+
+// Words at the start of a workspace of attention that are zero between calls, of every kind; partial results lie behind them
+constexpr int ATTEND_COUNTERS = 12288;
+
 struct AttendArgs {
     const _Float16* q;              // B rows of heads x dim, q_stride apart
     const void* pages_k;            // pages x kv x page x dim
     const void* pages_v;
     const float* k_scale;           // kv (8-bit cache), else null
     const float* v_scale;
+    const uint8_t* k_scales;        // by block, or null (launch_attend_far() only, as `sinks`)
+    const uint8_t* v_scales;
     const int* table;               // B x width
     const int* lengths;             // B
     _Float16* out;                  // B x heads x dim
     float* lse;                     // B x heads, or null
     float* parts;                   // arrival counters, partial results of units that several wavefronts share
-    int B, heads, kv, dim, q_stride, n_pages, page, bits, width, window;
+    int B, heads, kv, dim, q_stride, n_pages, page, bits, width, window, sinks;
     float scale;
     int group, hblocks, rows;       // query heads per kv head; blocks of 16 of them; of them in a block (set by the launcher)
     int nwg;                        // workgroups (set by the launcher)
@@ -51,6 +100,28 @@ struct AttendArgs {
 constexpr int ATTEND_MAX_B = 8192;          // requests per call: their tile counts sit in LDS
 size_t attend_workspace_bytes(int heads, int kv, int dim);
 hipError_t launch_attend(AttendArgs a, hipStream_t stream);
+hipError_t launch_attend_far(AttendArgs a, hipStream_t stream);        // first tokens that stay visible, scales by block
+
+struct PromptArgs {
+    const _Float16* q;              // M rows of heads x dim, q_stride apart
+    const void* pages_k;            // pages x kv x page x dim
+    const void* pages_v;
+    const float* k_scale;           // kv (8-bit cache with a scale a head), else null
+    const float* v_scale;
+    const uint8_t* k_scales;        // by block, or null
+    const uint8_t* v_scales;
+    const int* table;               // B x width
+    const int* lengths;             // B
+    const int* starts;              // B + 1: rows of each request
+    _Float16* out;                  // M x heads x dim
+    float* lse;                     // M x heads, or null
+    float* parts;                   // arrival counters, partial results of tiles that several workgroups share
+    int M, B, heads, kv, dim, q_stride, n_pages, page, bits, width, window, sinks;
+    float scale;
+};
+size_t prompt_workspace_bytes(int dim);
+long long prompt_units(int M, int B, int heads, int kv, int dim);      // workgroups of a launch at most
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream);
 
 struct AdapterArgs {
     const _Float16* x;              // M x d_in
