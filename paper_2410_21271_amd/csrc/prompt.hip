@@ -55,6 +55,17 @@ __device__ __forceinline__ float max_of_halves(float v)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// 64 pieces of 16 bytes from memory straight into 1 KiB of LDS, lane after lane.  The compiler does not know of the request: it counts in vmcnt all the same, so the compiler's own
+// waits only get longer, and whoever reads the bytes waits for them (arrived()) before the barrier in front of the reads.
+__device__ __forceinline__ void memory_to_lds(const char* base, unsigned off, unsigned lds)
+{
+    const unsigned long long at = (unsigned long long)base;
+    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)at), high = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"((unsigned long long)high << 32 | low) : "memory", "m0");
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // A request as the kernel takes it: n tokens, rows [first, first + rows), tiles of its pairs, tiles of keys of its longest tile at most, parts a tile is cut into
 struct Request {
     int n, first, rows, tiles, cost;
@@ -178,9 +189,9 @@ __device__ __forceinline__ float2 get2(const float* p)
 }
 __device__ __forceinline__ float factor(float m, float to) { return m == -INFINITY ? 0.f : exp2_(m - to); }
 
-// a partial result: RG wavefronts x (DIM / 2 + 1) x 64 lanes x two words, the last pair (m, sum)
+// words of a partial result: (m, sum) and O of each pair
 template <int DIM>
-constexpr size_t part_words() { return (size_t)RG * (DIM / 4 + 1) * 128; }
+constexpr size_t part_words() { return (size_t)TQ * (DIM + 2); }
 
 template <int DIM, int BITS, bool BLOCKS>
 __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_kernel(const PromptArgs a)
@@ -196,12 +207,16 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ int scratch[2 * 8 + 4 + 2 * 8];
-    __shared__ int marks[2][2];                // (team, stage): the step whose values have one that is not finite
+    __shared__ int odd_one;                    // some value that not all rows see is not finite
     __shared__ int last;
+    __shared__ float red_m[TEAMS][TQ], red_l[TEAMS][TQ];
 
     Unit u;
     if (!unit_of<THREADS>(a, blockIdx.x, u, scratch)) return;
-    const Request r = request_of(a, u.b);
+    Request r = request_of(a, u.b);
+    r.n = __builtin_amdgcn_readfirstlane(r.n);
+    r.first = __builtin_amdgcn_readfirstlane(r.first);
+    r.rows = __builtin_amdgcn_readfirstlane(r.rows);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / RG, rg = wave % RG;
     const int tt = threadIdx.x % TEAM, col = lane & 31, half = lane >> 5;
     const int group = a.heads / a.kv, pairs = r.rows * group, from = r.n - r.rows;             // from: position of row 0 (below 0: rows that see nothing)
@@ -233,90 +248,140 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     const int wlow = from + w0 / group, whigh = w1 > w0 ? from + (w1 - 1) / group : -1;
     const bool all = w1 - w0 == 32;
 
-    // Rows of the next 64 groups of 16 keys of this team: lane 4 i + g has group g of its tile i (-1: no page, or no key that a row sees)
-    long long rows_of = -1;
+    // Blocks of 16 tokens (page, head and place in one number) of the next 64 groups of 16 keys of this team: lane 4 i + g has that of group g of its tile i (-1: no page, or no key
+    // that a row sees), and its scales' bytes
+    int block_of = -1;
     uint32_t bytes_of = 0;
     const int* table = a.table + (size_t)u.b * a.width;
+    const int per_page = a.page / BLOCK_TOKENS;
+    auto block_at = [&](int key) {
+        const int p = key / a.page, page = table[p];
+        return (unsigned)page < (unsigned)a.n_pages ? (page * a.kv + u.h) * per_page + (key - p * a.page) / BLOCK_TOKENS : -1;
+    };
+    auto gone_at = [&](int key0) {
+        unsigned gone = 0;
+        for (int g = 0; g < 4; ++g) gone |= (unsigned)(key0 + 16 * g < hi && block_at(key0 + 16 * g) < 0) << g;
+        return gone;
+    };
     auto look = [&](int i0) {
         const int i = i0 + (lane >> 2), key = i < mine ? key_of(k0 + team + TEAMS * i) + 16 * (lane & 3) : hi;
-        rows_of = -1;
-        bytes_of = 0;
-        if (key < hi) {
-            const int p = key / a.page, page = table[p];
-            if ((unsigned)page < (unsigned)a.n_pages) {
-                rows_of = ((long long)page * a.kv + u.h) * a.page + (key - p * a.page);
-                if constexpr (BLOCKS) bytes_of = a.k_scales[rows_of / BLOCK_TOKENS] | (uint32_t)a.v_scales[rows_of / BLOCK_TOKENS] << 8;
+        block_of = key < hi ? block_at(key) : -1;
+        if constexpr (BLOCKS) bytes_of = block_of < 0 ? 0 : a.k_scales[block_of] | (uint32_t)a.v_scales[block_of] << 8;
+    };
+    // A tile's groups, as look() found them
+    struct Groups {
+        int i;
+        unsigned gone;                         // groups without a page
+        uint32_t k_bytes, v_bytes;             // four each
+    };
+    auto groups_of = [&](int i) {
+        Groups t;
+        t.i = i;
+        t.gone = t.k_bytes = t.v_bytes = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int x = __builtin_amdgcn_readlane(block_of, 4 * (i & 15) + g);
+            t.gone |= (unsigned)(x < 0) << g;
+            if constexpr (BLOCKS) {
+                const uint32_t w = __builtin_amdgcn_readlane(bytes_of, 4 * (i & 15) + g);
+                t.k_bytes |= (w & 255) << (8 * g);
+                t.v_bytes |= (w >> 8) << (8 * g);
+            }
+        }
+        return t;
+    };
+    // Whether a tile's values can go to LDS as they are: all rows see all of its tokens
+    auto plain = [&](int key0, unsigned gone) { return gone == 0 && key0 + KT <= low + 1 && (a.window == 0 || key0 > high - a.window || key0 + KT <= a.sinks); };
+
+    // Pieces of 16 bytes in memory: this lane's place among those that its wavefront moves at a time, which lie in one group of keys; piece e of the wavefront begins with key key_at(e)
+    const int tw = wave % RG, lrow = lane / PR, lpiece = lane % PR;
+    auto key_at = [&](int e) { return tw * (64 / PR) + e * (TEAM / PR); };
+    const int turn = tw * (64 / PR) + lrow;    // its key, but for multiples of 8
+    auto group_at = [&](int e) { return TEAM / PR <= 16 ? e * (TEAM / PR) / 16 : (TEAM / PR == 32 ? 2 * e + (tw >> 1) : tw); };
+    auto memory_of = [&](const void* pages, const Groups& t, int e) {
+        const int found = __builtin_amdgcn_readlane(block_of, 4 * (t.i & 15) + group_at(e)), x = found < 0 ? 0 : found;
+        return (const char*)pages + ((size_t)(unsigned)x * BLOCK_TOKENS + key_at(e) % 16) * (DIM * BITS / 8);
+    };
+    // straight from memory to LDS (fp16): pieces change places on the way, as the addresses say
+    const unsigned k_off = (unsigned)(lrow * ROW + 16 * (lpiece ^ (turn & 7))), v_off = (unsigned)(lrow * ROW + 16 * (lpiece ^ (2 * (turn & VX))));
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(team * 2 * STAGE);
+    auto direct = [&](const void* pages, const Groups& t, unsigned off, unsigned to) {
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) memory_to_lds(memory_of(pages, t, e), off, to + (unsigned)(key_at(e) * ROW));
+    };
+    // by way of registers
+    u4 mk[PIECES], mv[PIECES];
+    auto fetch = [&](const void* pages, const Groups& t, u4 (&w)[PIECES]) {
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) w[e] = *(const u4*)(memory_of(pages, t, e) + 16u * lane);
+    };
+    auto expand = [&](const u4& w, float scale, Frag (&f)[PER / 8]) {
+        if constexpr (BITS == 16) {
+            f[0].q = w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[e / 2].p[2 * (e % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, false);
+                f[e / 2].p[2 * (e % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, true);
             }
         }
     };
-    auto row_at = [&](int i, int g) {
-        const int from_lane = 4 * (i & 15) + g;
-        const unsigned l = __builtin_amdgcn_readlane((unsigned)rows_of, from_lane), h = __builtin_amdgcn_readlane((unsigned)(rows_of >> 32), from_lane);
-        return (long long)((unsigned long long)h << 32 | l);
-    };
-    // Pieces on their way from memory to LDS: piece tt + TEAM i of the tile's, keys' and values'
-    u4 mk[PIECES], mv[PIECES];
-    uint32_t mbytes[PIECES];
-    int mgone = 0;                             // bit i: no page
-    auto load = [&](int i) {
-        mgone = 0;
+    auto put_keys = [&](uint32_t bytes, int stage) {
+        unsigned char* to = smem + (team * 2 + stage) * STAGE;
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
-            const int piece = __builtin_amdgcn_readfirstlane((tt & ~63) + TEAM * e), g = piece / PR / 16;       // (a wavefront's pieces lie in one group)
-            const long long at = row_at(i, g);
-            if constexpr (BLOCKS) mbytes[e] = __builtin_amdgcn_readlane(bytes_of, 4 * (i & 15) + g);
-            mgone |= (at < 0) << e;
-            const size_t base = (size_t)((at < 0 ? 0 : at) + piece / PR % 16) * (DIM * BITS / 8);
-            const unsigned off = 16u * lane;
-            mk[e] = *(const u4*)((const char*)a.pages_k + base + off);
-            mv[e] = *(const u4*)((const char*)a.pages_v + base + off);
+            Frag f[PER / 8];
+            expand(mk[e], BLOCKS ? power_of(bytes >> (8 * group_at(e)) & 255) : 1.f, f);
+            const int key = key_at(e) + lrow;
+#pragma unroll
+            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (turn & 7))) = f[w].q;
         }
     };
-    auto store = [&](int i, int stage) {
-        const int key0 = key_of(k0 + team + TEAMS * i);
-        // tokens that no row sees are zeros: those behind the last, those between the first ones and the window, those without a page
-        const bool clean = key0 + KT <= hi && (key0 >= lo || key0 + KT <= sinks) && mgone == 0;
-        // whether some rows see one and others do not
-        const bool torn = key0 + KT > low + 1 || (a.window > 0 && key0 <= high - a.window && key0 + KT > sinks);
-        unsigned char* to = smem + (team * 2 + stage) * STAGE;
+    // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
+    auto put_values = [&](int key0, unsigned gone, uint32_t bytes, int stage) {
+        unsigned char* to = smem + (team * 2 + stage) * STAGE + KT * ROW;
+        const bool as_it_is = plain(key0, gone);
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
-            const int piece = tt + TEAM * e, key = piece / PR, c = piece - key * PR;
-            Frag k[PER / 8], v[PER / 8];
-            if constexpr (BITS == 16) {
-                k[0].q = mk[e];
-                v[0].q = mv[e];
-            } else {
-                const float ks = BLOCKS ? power_of(mbytes[e] & 255) : 1.f, vs = BLOCKS ? power_of(mbytes[e] >> 8) : 1.f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    k[w / 2].p[2 * (w % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(mk[e][w], ks, false);
-                    k[w / 2].p[2 * (w % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(mk[e][w], ks, true);
-                    v[w / 2].p[2 * (w % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(mv[e][w], vs, false);
-                    v[w / 2].p[2 * (w % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(mv[e][w], vs, true);
-                }
-            }
-            if (!clean) {
+            Frag f[PER / 8];
+            expand(mv[e], BLOCKS ? power_of(bytes >> (8 * group_at(e)) & 255) : 1.f, f);
+            const int key = key_at(e) + lrow;
+            if (!as_it_is) {
                 const int at = key0 + key;
-                const bool seen = at < hi && (at >= lo || at < sinks) && !(mgone >> e & 1);
+                const bool seen = at < hi && (at >= lo || at < sinks) && !(gone >> (key / 16) & 1);
 #pragma unroll
-                for (int w = 0; w < PER / 8; ++w) {
-                    v[w].q = seen ? v[w].q : u4{0, 0, 0, 0};
-                }
+                for (int w = 0; w < PER / 8; ++w)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t x = seen ? f[w].u[q] : 0u;
+                        const uint32_t low_half = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, high_half = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
+                        odd |= (low_half | high_half) != 0;
+                        f[w].u[q] = x & ~(low_half | high_half);
+                    }
             }
 #pragma unroll
-            for (int w = 0; w < PER / 8; ++w) {
-                const int chunk = c * (PER / 8) + w;                    // of 16 bytes in the row
-                *(u4*)(to + key * ROW + 16 * (chunk ^ (key & 7))) = k[w].q;
-                *(u4*)(to + KT * ROW + key * ROW + 16 * (chunk ^ (2 * (key & VX)))) = v[w].q;
-                if (torn) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) odd |= (v[w].u[q] & 0x7c00u) == 0x7c00u || (v[w].u[q] & 0x7c000000u) == 0x7c000000u;
-                }
-            }
+            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (2 * (turn & VX)))) = f[w].q;
         }
-        if (torn && __any(odd) && lane == 0) marks[team][stage] = i + 1;
+        if (!as_it_is && odd) odd_one = 1;
+    };
+    // Keys of tile i, and values, on their way to their stage; arrived() before the barrier in front of their first use
+    auto tile_at = [&](int i) { return key_of(k0 + team + TEAMS * i); };
+    auto send_keys = [&](const Groups& t, int i) {
+        if constexpr (BITS == 16) direct(a.pages_k, t, k_off, lds0 + (unsigned)((i & 1) * STAGE));
+        else fetch(a.pages_k, t, mk);
+    };
+    auto send_values = [&](const Groups& t, int i) {
+        if constexpr (BITS == 16) {
+            if (plain(tile_at(i), t.gone)) {
+                direct(a.pages_v, t, v_off, lds0 + (unsigned)((i & 1) * STAGE + KT * ROW));
+            } else {
+                fetch(a.pages_v, t, mv);
+                put_values(tile_at(i), t.gone, 0, i & 1);
+            }
+        } else {
+            fetch(a.pages_v, t, mv);
+        }
     };
 
     // q, its sign that of the scale
@@ -340,40 +405,71 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     // where this lane reads: K, row col: piece 2 t + half; V, transposed: rows 4 half + lane % 16 / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of 32
     const int k_at = col * ROW, k_turn = half ^ (col & 7);
     const int v_key = 4 * half + (lane & 15) / 4, v_at = KT * ROW + v_key * ROW + 8 * (lane & 3), v_turn = (lane >> 4 & 1) ^ (v_key & VX);
-
-    if (tt < 2) marks[team][tt] = 0;
-    look(0);
-    if (mine > 0) load(0);
-    __syncthreads();
-    if (mine > 0) store(0, 0);
-    __syncthreads();
-    for (int i = 0; i < steps; ++i) {
-        const int stage = i & 1;
-        const int key0 = i < mine ? key_of(k0 + team + TEAMS * i) : 0;
-        unsigned gone = 0;                     // groups of the tile without a page
-        if (i < mine) {
+    const unsigned char* mine_at = smem + team * 2 * STAGE;
+    auto first_product = [&](const unsigned char* base, f16x (&S)[2]) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) gone |= (unsigned)(row_at(i, g) < 0) << g;
-        }
-        if (i + 1 < mine) {
-            if (((i + 1) & 15) == 0) look(i + 1);
-            load(i + 1);
-        }
-        // (rows of a wavefront see none of it: behind them, or before their windows)
-        const bool some = i < mine && key0 <= whigh && (a.window == 0 || key0 + KT > wlow - a.window + 1 || key0 < a.sinks);
-        if (some) {
-            const unsigned char* base = smem + (team * 2 + stage) * STAGE;
-            f16x S[2];
+        for (int b = 0; b < 2; ++b) {
+            f16x z = {};
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                S[b] = f16x{};
-#pragma unroll
-                for (int t = 0; t < NK; ++t) {
-                    Frag k;
-                    k.q = *(const u4*)(base + k_at + 32 * b * ROW + 16 * ((2 * t) ^ k_turn));
-                    S[b] = mfma32(k.v, q[t].v, S[b]);
-                }
+            for (int t = 0; t < NK; ++t) {
+                Frag k;
+                k.q = *(const u4*)(base + k_at + 32 * b * ROW + 16 * ((2 * t) ^ k_turn));
+                z = mfma32(k.v, q[t].v, z);
             }
+            S[b] = z;
+        }
+    };
+    auto largest = [&](const f16x (&S)[2]) {
+        float top = fmaxf(S[0][0], S[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, S[0][e]), S[1][e]);
+        return top;
+    };
+
+    // Tile i: its scores are there when its step begins, found beside the softmax of the tile before it
+    f16x Sa[2], Sb[2];
+    float top = -INFINITY;
+    unsigned gone = 0, gone_next = 0;          // of tiles i and i + 1
+    if (threadIdx.x == 0) odd_one = 0;
+    __syncthreads();
+    look(0);
+    if (mine > 0) {
+        const Groups t = groups_of(0);
+        gone = t.gone;
+        send_keys(t, 0);
+        if constexpr (BITS == 8) put_keys(t.k_bytes, 0);
+        send_values(t, 0);
+        if constexpr (BITS == 8) put_values(tile_at(0), gone, t.v_bytes, 0);
+        if (mine > 1) {
+            const Groups n = groups_of(1);
+            send_keys(n, 1);
+            if constexpr (BITS == 8) put_keys(n.k_bytes, 1);
+        }
+    }
+    arrived();
+    __syncthreads();
+    if (mine > 0) {
+        first_product(mine_at, Sa);
+        top = largest(Sa);
+    }
+    __syncthreads();
+    auto step = [&](int i, f16x (&S)[2], f16x (&N)[2], int stage) {
+        uint32_t v_bytes = 0, k_bytes = 0;
+        if (i + 1 < mine) {
+            const Groups t = groups_of(i + 1);
+            gone_next = t.gone;
+            v_bytes = t.v_bytes;
+            send_values(t, i + 1);
+        }
+        if (i + 2 < mine) {
+            if (((i + 2) & 15) == 0) look(i + 2);
+            const Groups t = groups_of(i + 2);
+            k_bytes = t.k_bytes;
+            send_keys(t, i + 2);
+        }
+        if (i < mine) {
+            const unsigned char* base = mine_at + stage * STAGE;
+            const int key0 = tile_at(i);
             const bool whole = all && gone == 0 && key0 + KT <= wlow + 1 && (a.window == 0 || key0 > whigh - a.window || key0 + KT <= a.sinks);
             if (!whole) {
 #pragma unroll
@@ -384,10 +480,8 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                         const bool seen = key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks) && !(gone >> (2 * b + e / 8) & 1);
                         S[b][e] = seen ? S[b][e] : -INFINITY;
                     }
+                top = largest(S);
             }
-            float top = fmaxf(S[0][0], S[1][0]);
-#pragma unroll
-            for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, S[0][e]), S[1][e]);
             top *= by;
             if (__any(top > m + (RAISE + LOWER))) {
                 top = max_of_halves(top);
@@ -398,103 +492,140 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                 for (int d = 0; d < ND; ++d) O[d] *= f;
             }
             const float ref = m == -INFINITY ? 0.f : m;
+            // (behind the last tile: what lies there, unused)
+            first_product(mine_at + (stage ^ 1) * STAGE, N);
             Frag p[4];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
                     const float x = exp2_(__builtin_fmaf(S[b][e], by, -ref)), y = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
-                    l += x;
+                    l += x;                    // (not what the weights are rounded to: lse would be off by 2^-12)
                     l += y;
                     p[2 * b + e / 8].p[e % 8 / 2] = h2{(_Float16)x, (_Float16)y};
                 }
-            auto second = [&](bool careful) {
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        Frag v;
+                for (int d = 0; d < ND; ++d) {
+                    Frag v;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const unsigned char* at = base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_turn);
-                            const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)at);
-                            __builtin_memcpy(&v.u[2 * e], &w, 8);
-                        }
-                        if (careful) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if ((v.u[e] & 0x7c00u) == 0x7c00u) v.u[e] &= 0xffff0000u;
-                                if ((v.u[e] & 0x7c000000u) == 0x7c000000u) v.u[e] &= 0xffffu;
-                            }
-                        }
-                        O[d] = mfma32(v.v, p[s].v, O[d]);
+                    for (int e = 0; e < 2; ++e) {
+                        const unsigned char* at = base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_turn);
+                        const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)at);
+                        __builtin_memcpy(&v.u[2 * e], &w, 8);
                     }
-            };
-            if (marks[team][stage] != i + 1) {
-                second(false);
-            } else {
-                // values that are not finite, key by key, for the rows that have a weight for them
-                second(true);
-                for (int key = 0; key < KT; ++key) {
-                    // the weight: register 8 (key / 16) + 4 (key / 8 % 2) + key % 4 of the lanes of half key / 4 % 2
-                    uint32_t w = 0;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) w = e == key / 16 * 4 + key / 8 % 2 * 2 + key % 4 / 2 ? p[e / 4].u[e % 4] : w;
-                    w = key % 2 ? w >> 16 : w & 0xffffu;
-                    const auto both = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-                    const float x = (float)__builtin_bit_cast(_Float16, (unsigned short)(key / 4 % 2 ? both[1] : both[0]));
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int c = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
-                            const float v = (float)*(const _Float16*)(base + KT * ROW + key * ROW + 32 * ((c / 16) ^ (key & VX)) + 2 * (c % 16));
-                            if (x != 0.f && !(fabsf(v) < INFINITY)) O[d][e] += x * v;
-                        }
+                    O[d] = mfma32(v.v, p[s].v, O[d]);
                 }
-            }
+            top = largest(N);
         }
-        if (i + 1 < mine) store(i + 1, stage ^ 1);
+        if constexpr (BITS == 8) {
+            if (i + 2 < mine) put_keys(k_bytes, stage);
+            if (i + 1 < mine) put_values(tile_at(i + 1), gone_next, v_bytes, stage ^ 1);
+        }
+        gone = gone_next;
+        arrived();
         __syncthreads();
+    };
+    for (int i = 0; i < steps; i += 2) {
+        step(i, Sa, Sb, 0);
+        if (i + 1 < steps) step(i + 1, Sb, Sa, 1);
     }
     {
         const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
     }
 
-    // the teams' results, added up (all have passed the loop's last barrier)
+    // The teams' results meet in LDS, as rows of fp32 (all have passed the loop's last barrier).  This lane's elements: columns 32 d + 8 q + 4 half of row 32 rg + col; pieces of
+    // 16 bytes change places within their row, so that the lanes that write at a time meet different banks.
+    float* sum = (float*)smem;
+    const int mine_row = 32 * rg + col;
+    auto piece_at = [&](int r, int c) { return sum + r * DIM + 4 * (c ^ (r & 15)); };
+    if (half == 0) {
+        red_m[team][mine_row] = m;
+        red_l[team][mine_row] = l;
+    }
+    if (team == TEAMS - 1) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *(f4*)piece_at(mine_row, 8 * d + 2 * e + half) = f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
+    }
+    __syncthreads();
     if constexpr (TEAMS == 2) {
-        float* red = (float*)smem + (size_t)rg * (16 * ND + 2) * 64 + lane;
-        if (team == 1) {
-            red[0] = m;
-            red[64] = l;
+        if (team == 0) {
+            const float mo = red_m[1][mine_row], up = fmaxf(m, mo), f = factor(m, up), g = factor(mo, up), lo2 = red_l[1][mine_row];
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) red[(2 + 16 * d + e) * 64] = O[d][e];
-        }
-        __syncthreads();
-        if (team == 0) {
-            const float mo = red[0], lo2 = red[64], up = fmaxf(m, mo), f = factor(m, up), g = factor(mo, up);
+                for (int e = 0; e < 4; ++e) {
+                    f4* at = (f4*)piece_at(mine_row, 8 * d + 2 * e + half);
+                    *at = *at * g + f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]} * f;
+                }
             l = (m == -INFINITY ? l : l * f) + (mo == -INFINITY ? lo2 : lo2 * g);
             m = up;
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) O[d][e] = O[d][e] * f + red[(2 + 16 * d + e) * 64] * g;
+            if (half == 0) {
+                red_m[0][mine_row] = m;
+                red_l[0][mine_row] = l;
+            }
         }
+        __syncthreads();
+    }
+    if (odd_one) {
+        // Values that are not finite, in tiles of which not all rows see all: for the rows that see them, unless their score is -inf
+        for (int e = threadIdx.x; e < TQ * (DIM / 4); e += THREADS) {
+            const int r2 = e / (DIM / 4), c = e % (DIM / 4), pr = pair0 + r2;
+            if (pr >= pair1) continue;
+            const int rw = pr / group, at_pos = from + rw, head2 = u.h * group + pr - rw * group;
+            f4 add = {0.f, 0.f, 0.f, 0.f};
+            for (int i = k0; i < k1; ++i) {
+                const int key0 = key_of(i);
+                for (int key = key0; key < key0 + KT && key <= at_pos; ++key) {
+                    if (!(a.window == 0 || key > at_pos - a.window || key < a.sinks)) continue;
+                    const int block = block_at(key & ~(BLOCK_TOKENS - 1));
+                    if (block < 0) continue;
+                    const size_t at = ((size_t)(unsigned)block * BLOCK_TOKENS + key % BLOCK_TOKENS) * DIM;
+                    bool any = false;
+                    float v[4];
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        if constexpr (BITS == 16) v[q4] = (float)((const _Float16*)a.pages_v)[at + 4 * c + q4];
+                        else v[q4] = (((const uint8_t*)a.pages_v)[at + 4 * c + q4] & 127) == 127 ? __builtin_nanf("") : 0.f;
+                        any |= !(fabsf(v[q4]) < INFINITY);
+                    }
+                    if (!any || plain(key0, gone_at(key0))) continue;
+                    if constexpr (BITS == 16) {
+                        const _Float16 *x = a.q + (size_t)(r.first + rw) * a.q_stride + (size_t)head2 * DIM, *y = (const _Float16*)a.pages_k + at;
+                        float score = 0.f;
+                        for (int t = 0; t < DIM; ++t) score += (float)x[t] * (float)y[t];
+                        if (score * scale == -INFINITY) continue;
+                    }
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) add[q4] += fabsf(v[q4]) < INFINITY ? 0.f : v[q4];
+                }
+            }
+            *(f4*)piece_at(r2, c) += add;
+        }
+        __syncthreads();
     }
 
     const float vs = BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f;
+    // Pieces of four columns: thread after thread along the rows
+    constexpr int MY = TQ * (DIM / 4) / THREADS;
+    const int used = pair1 - pair0;
     if (parts > 1) {
-        float* part = a.parts + COUNTERS + (size_t)u.place * part_words<DIM>() + (size_t)rg * (DIM / 4 + 1) * 128 + 2 * lane;
-        if (team == 0) {
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) put2(part + (8 * d + e / 2) * 128, O[d][e], O[d][e + 1]);
-            put2(part + DIM / 4 * 128, m, l);
+        // a partial result: rows of (m, sum), then rows of DIM
+        float* part = a.parts + COUNTERS + (size_t)u.place * part_words<DIM>();
+#pragma unroll 4
+        for (int e = 0; e < MY; ++e) {
+            const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
+            if (r2 < used) {
+                const f4 x = *(const f4*)piece_at(r2, c);
+                put2(part + 2 * TQ + 4 * at, x[0], x[1]);
+                put2(part + 2 * TQ + 4 * at + 2, x[2], x[3]);
+            }
         }
+        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, red_m[0][threadIdx.x], red_l[0][threadIdx.x]);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -503,40 +634,54 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
             if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         __syncthreads();
-        if (!last || team != 0) return;
-        m = -INFINITY;
-        l = 0.f;
+        if (!last) return;
+        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words<DIM>();
+        const size_t step_words = (size_t)a.kv * part_words<DIM>();
+        for (int e = 0; e < MY; ++e) {
+            const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
+            if (r2 >= used) break;
+            float mm = -INFINITY, ll = 0.f;
+            f4 x = {0.f, 0.f, 0.f, 0.f};
+            // (four at a time on their way)
+            for (int c0 = 0; c0 < parts; c0 += 4) {
+                float2 ml[4], y[4][2];
 #pragma unroll
-        for (int d = 0; d < ND; ++d) O[d] = f16x{};
-        for (int c = 0; c < parts; ++c) {
-            const float* src = a.parts + COUNTERS + (size_t)(u.first + c * a.kv) * part_words<DIM>() + (size_t)rg * (DIM / 4 + 1) * 128 + 2 * lane;
-            const float2 ml = get2(src + DIM / 4 * 128);
-            const float up = fmaxf(m, ml.x), f = factor(m, up), g = factor(ml.x, up);
-            l = (m == -INFINITY ? l : l * f) + (ml.x == -INFINITY ? ml.y : ml.y * g);
-            m = up;
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float2 x = get2(src + (8 * d + e / 2) * 128);
-                    O[d][e] = O[d][e] * f + x.x * g;
-                    O[d][e + 1] = O[d][e + 1] * f + x.y * g;
+                for (int k = 0; k < 4; ++k) {
+                    const float* one = src + (size_t)(c0 + k < parts ? c0 + k : parts - 1) * step_words;
+                    ml[k] = get2(one + 2 * r2);
+                    y[k][0] = get2(one + 2 * TQ + 4 * at);
+                    y[k][1] = get2(one + 2 * TQ + 4 * at + 2);
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (c0 + k >= parts) break;
+                    const float up = fmaxf(mm, ml[k].x), f = factor(mm, up), g = factor(ml[k].x, up);
+                    ll = (mm == -INFINITY ? ll : ll * f) + (ml[k].x == -INFINITY ? ml[k].y : ml[k].y * g);
+                    mm = up;
+                    x = x * f + f4{y[k][0].x, y[k][0].y, y[k][1].x, y[k][1].y} * g;
+                }
+            }
+            *(f4*)piece_at(r2, c) = x;         // (its own thread reads it below)
+            if (c == 0) {
+                red_m[0][r2] = mm;
+                red_l[0][r2] = ll;
+            }
         }
+        __syncthreads();
     }
-    if (team != 0 || !there) return;
-    const size_t at = (size_t)(r.first + row) * a.heads + qh;
-    const float f = vs / l;
+    for (int e = 0; e < MY; ++e) {
+        const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
+        if (r2 >= used) break;
+        const int pr = pair0 + r2, rw = pr / group;
+        const size_t place = (size_t)(r.first + rw) * a.heads + u.h * group + (pr - rw * group);
+        const float ll = red_l[0][r2], f = vs / ll;
+        const f4 x = *(const f4*)piece_at(r2, c);
+        h4 y;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            h4 y;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) y[c] = (_Float16)(l == 0.f ? 0.f : O[d][e + c] * f);
-            *(h4*)(a.out + at * DIM + 32 * d + 2 * e + 4 * half) = y;
-        }
-    if (half == 0 && a.lse) a.lse[at] = LN2 * (m + __log2f(l));
+        for (int q4 = 0; q4 < 4; ++q4) y[q4] = (_Float16)(ll == 0.f ? 0.f : x[q4] * f);
+        *(h4*)(a.out + place * DIM + 4 * c) = y;
+        if (c == 0 && a.lse) a.lse[place] = LN2 * (red_m[0][r2] + __log2f(ll));
+    }
 }
 
 template <int DIM, int BITS, bool BLOCKS>
