@@ -203,6 +203,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     constexpr int PER = 16 / (BITS / 8);       // elements of a 16-byte piece in memory
     constexpr int PIECES = KT * DIM / PER / TEAM;                 // pieces of K (of V) a thread moves
     constexpr int PR = DIM / PER;              // pieces of a row
+    constexpr int AHEAD = 4;                   // matrix instructions between an operand's read and its use
     constexpr int VX = DIM == 64 ? 3 : 7;      // how many units of 32 bytes of V's rows change places
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -492,32 +493,50 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                 for (int d = 0; d < ND; ++d) O[d] *= f;
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            // (behind the last tile: what lies there, unused)
-            first_product(mine_at + (stage ^ 1) * STAGE, N);
-            Frag p[4];
+            // One matrix instruction a slot, kept in this order: beside those of the next tile's scores (behind the last tile: of what lies there, unused) two weights of this one
+            // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
+            const unsigned char* next = mine_at + (stage ^ 1) * STAGE;
+            Frag kf[AHEAD], vf[AHEAD], p[4];
+            auto read_k = [&](int x) { kf[x % AHEAD].q = *(const u4*)(next + k_at + 32 * (x % 2) * ROW + 16 * ((2 * (x / 2)) ^ k_turn)); };
+            auto read_v = [&](int x) {
+                const int s = x / ND, d = x % ND;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float x = exp2_(__builtin_fmaf(S[b][e], by, -ref)), y = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
-                    l += x;                    // (not what the weights are rounded to: lse would be off by 2^-12)
-                    l += y;
-                    p[2 * b + e / 8].p[e % 8 / 2] = h2{(_Float16)x, (_Float16)y};
+                for (int e = 0; e < 2; ++e) {
+                    const unsigned char* at = base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_turn);
+                    const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)at);
+                    __builtin_memcpy(&vf[x % AHEAD].u[2 * e], &w, 8);
                 }
+            };
+            auto weights = [&](int x) {        // elements 2 x and 2 x + 1
+                const int b = x / 8, e = 2 * x % 16;
+                const float v = exp2_(__builtin_fmaf(S[b][e], by, -ref)), w = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
+                l += v;                        // (not what the weights are rounded to: lse would be off by 2^-12)
+                l += w;
+                p[2 * b + e / 8].p[e % 8 / 2] = h2{(_Float16)v, (_Float16)w};
+            };
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+            for (int x = 0; x < AHEAD; ++x) read_k(x);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    Frag v;
+            for (int x = 0; x < 2 * NK; ++x) {
+                const int b = x % 2, t = x / 2;
+                if (t == 0) N[b] = f16x{};
+                N[b] = mfma32(kf[x % AHEAD].v, q[t].v, N[b]);
+                if (x + AHEAD < 2 * NK) read_k(x + AHEAD);
+                else read_v(x + AHEAD - 2 * NK);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const unsigned char* at = base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_turn);
-                        const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)at);
-                        __builtin_memcpy(&v.u[2 * e], &w, 8);
-                    }
-                    O[d] = mfma32(v.v, p[s].v, O[d]);
-                }
-            top = largest(N);
+                for (int w = 16 * x / (2 * NK); w < 16 * (x + 1) / (2 * NK); ++w) weights(w);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int x = 0; x < 4 * ND; ++x) {
+                const int s = x / ND, d = x % ND;
+                O[d] = mfma32(vf[x % AHEAD].v, p[s].v, O[d]);
+                if (x + AHEAD < 4 * ND) read_v(x + AHEAD);
+#pragma unroll
+                for (int e = 16 * x / (4 * ND); e < 16 * (x + 1) / (4 * ND); ++e) top = e == 0 ? fmaxf(N[0][0], N[1][0]) : fmaxf(fmaxf(top, N[0][e]), N[1][e]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if constexpr (BITS == 8) {
             if (i + 2 < mine) put_keys(k_bytes, stage);
