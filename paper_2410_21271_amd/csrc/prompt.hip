@@ -249,10 +249,11 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     const int wlow = from + w0 / group, whigh = w1 > w0 ? from + (w1 - 1) / group : -1;
     const bool all = w1 - w0 == 32;
 
-    // Blocks of 16 tokens (page, head and place in one number) of the next 64 groups of 16 keys of this team: lane 4 i + g has that of group g of its tile i (-1: no page, or no key
-    // that a row sees), and its scales' bytes
-    int block_of = -1;
-    uint32_t bytes_of = 0;
+    // Blocks of 16 tokens of the next 64 groups of 16 keys of this team: lane 4 i + g has where that of group g of its tile i begins in the cache, in bytes (0: no page, or no key that a
+    // row sees: those are in `lost`), and its scales
+    unsigned off_low = 0, off_high = 0;
+    float k_power = 1.f, v_power = 1.f;
+    unsigned long long lost = 0;
     const int* table = a.table + (size_t)u.b * a.width;
     const int per_page = a.page / BLOCK_TOKENS;
     auto block_at = [&](int key) {
@@ -264,33 +265,19 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
         for (int g = 0; g < 4; ++g) gone |= (unsigned)(key0 + 16 * g < hi && block_at(key0 + 16 * g) < 0) << g;
         return gone;
     };
+    auto tile_at = [&](int i) { return key_of(k0 + team + TEAMS * i); };
     auto look = [&](int i0) {
-        const int i = i0 + (lane >> 2), key = i < mine ? key_of(k0 + team + TEAMS * i) + 16 * (lane & 3) : hi;
-        block_of = key < hi ? block_at(key) : -1;
-        if constexpr (BLOCKS) bytes_of = block_of < 0 ? 0 : a.k_scales[block_of] | (uint32_t)a.v_scales[block_of] << 8;
-    };
-    // A tile's groups, as look() found them
-    struct Groups {
-        int i;
-        unsigned gone;                         // groups without a page
-        uint32_t k_bytes, v_bytes;             // four each
-    };
-    auto groups_of = [&](int i) {
-        Groups t;
-        t.i = i;
-        t.gone = t.k_bytes = t.v_bytes = 0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int x = __builtin_amdgcn_readlane(block_of, 4 * (i & 15) + g);
-            t.gone |= (unsigned)(x < 0) << g;
-            if constexpr (BLOCKS) {
-                const uint32_t w = __builtin_amdgcn_readlane(bytes_of, 4 * (i & 15) + g);
-                t.k_bytes |= (w & 255) << (8 * g);
-                t.v_bytes |= (w >> 8) << (8 * g);
-            }
+        const int i = i0 + (lane >> 2), key = i < mine ? tile_at(i) + 16 * (lane & 3) : hi, block = key < hi ? block_at(key) : -1;
+        lost = __ballot(block < 0);
+        const size_t off = (size_t)(unsigned)(block < 0 ? 0 : block) * (BLOCK_TOKENS * DIM * BITS / 8);
+        off_low = (unsigned)off;
+        off_high = (unsigned)(off >> 32);
+        if constexpr (BLOCKS) {
+            k_power = power_of(block < 0 ? 0 : a.k_scales[block]);
+            v_power = power_of(block < 0 ? 0 : a.v_scales[block]);
         }
-        return t;
     };
+    auto gone_of = [&](int i) { return (unsigned)(lost >> (4 * (i & 15))) & 15u; };
     // Whether a tile's values can go to LDS as they are: all rows see all of its tokens
     auto plain = [&](int key0, unsigned gone) { return gone == 0 && key0 + KT <= low + 1 && (a.window == 0 || key0 > high - a.window || key0 + KT <= a.sinks); };
 
@@ -299,22 +286,24 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     auto key_at = [&](int e) { return tw * (64 / PR) + e * (TEAM / PR); };
     const int turn = tw * (64 / PR) + lrow;    // its key, but for multiples of 8
     auto group_at = [&](int e) { return TEAM / PR <= 16 ? e * (TEAM / PR) / 16 : (TEAM / PR == 32 ? 2 * e + (tw >> 1) : tw); };
-    auto memory_of = [&](const void* pages, const Groups& t, int e) {
-        const int found = __builtin_amdgcn_readlane(block_of, 4 * (t.i & 15) + group_at(e)), x = found < 0 ? 0 : found;
-        return (const char*)pages + ((size_t)(unsigned)x * BLOCK_TOKENS + key_at(e) % 16) * (DIM * BITS / 8);
+    const unsigned rows_off = (unsigned)(tw * (64 / PR) % 16 * (DIM * BITS / 8));               // (of a piece behind its block's beginning, but for e)
+    auto memory_of = [&](const void* pages, int i, int e) {
+        const int from_lane = 4 * (i & 15) + group_at(e);
+        const unsigned low_word = __builtin_amdgcn_readlane(off_low, from_lane), high_word = __builtin_amdgcn_readlane(off_high, from_lane);
+        return (const char*)pages + ((unsigned long long)high_word << 32 | low_word) + e * (TEAM / PR) % 16 * (DIM * BITS / 8);
     };
     // straight from memory to LDS (fp16): pieces change places on the way, as the addresses say
-    const unsigned k_off = (unsigned)(lrow * ROW + 16 * (lpiece ^ (turn & 7))), v_off = (unsigned)(lrow * ROW + 16 * (lpiece ^ (2 * (turn & VX))));
+    const unsigned k_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ (turn & 7))), v_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ (2 * (turn & VX))));
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(team * 2 * STAGE);
-    auto direct = [&](const void* pages, const Groups& t, unsigned off, unsigned to) {
-#pragma unroll
-        for (int e = 0; e < PIECES; ++e) memory_to_lds(memory_of(pages, t, e), off, to + (unsigned)(key_at(e) * ROW));
-    };
+    const unsigned aside = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(TEAMS * 2 * STAGE + wave * 1024);     // (what nobody reads)
+    auto direct_keys = [&](int i, int e, int stage) { memory_to_lds(memory_of(a.pages_k, i, e), k_off, lds0 + (unsigned)(stage * STAGE + key_at(e) * ROW)); };
     // by way of registers
     u4 mk[PIECES], mv[PIECES];
-    auto fetch = [&](const void* pages, const Groups& t, u4 (&w)[PIECES]) {
-#pragma unroll
-        for (int e = 0; e < PIECES; ++e) w[e] = *(const u4*)(memory_of(pages, t, e) + 16u * lane);
+    float v_by[PIECES];
+    auto fetch_keys = [&](int i, int e) { mk[e] = *(const u4*)(memory_of(a.pages_k, i, e) + (rows_off + 16u * lane)); };
+    auto fetch_values = [&](int i, int e) {
+        mv[e] = *(const u4*)(memory_of(a.pages_v, i, e) + (rows_off + 16u * lane));
+        v_by[e] = BLOCKS ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_power), 4 * (i & 15) + group_at(e))) : 1.f;
     };
     auto expand = [&](const u4& w, float scale, Frag (&f)[PER / 8]) {
         if constexpr (BITS == 16) {
@@ -327,26 +316,24 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
             }
         }
     };
-    auto put_keys = [&](uint32_t bytes, int stage) {
+    auto put_keys = [&](int i, int e, int stage) {
         unsigned char* to = smem + (team * 2 + stage) * STAGE;
+        Frag f[PER / 8];
+        expand(mk[e], BLOCKS ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_power), 4 * (i & 15) + group_at(e))) : 1.f, f);
+        const int key = key_at(e) + lrow;
 #pragma unroll
-        for (int e = 0; e < PIECES; ++e) {
-            Frag f[PER / 8];
-            expand(mk[e], BLOCKS ? power_of(bytes >> (8 * group_at(e)) & 255) : 1.f, f);
-            const int key = key_at(e) + lrow;
-#pragma unroll
-            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (turn & 7))) = f[w].q;
-        }
+        for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (turn & 7))) = f[w].q;
     };
     // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
-    auto put_values = [&](int key0, unsigned gone, uint32_t bytes, int stage) {
-        unsigned char* to = smem + (team * 2 + stage) * STAGE + KT * ROW;
+    auto put_values = [&](int i, unsigned gone) {
+        unsigned char* to = smem + (team * 2 + (i & 1)) * STAGE + KT * ROW;
+        const int key0 = tile_at(i);
         const bool as_it_is = plain(key0, gone);
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
             Frag f[PER / 8];
-            expand(mv[e], BLOCKS ? power_of(bytes >> (8 * group_at(e)) & 255) : 1.f, f);
+            expand(mv[e], v_by[e], f);
             const int key = key_at(e) + lrow;
             if (!as_it_is) {
                 const int at = key0 + key;
@@ -366,25 +353,6 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
         }
         if (!as_it_is && odd) odd_one = 1;
     };
-    // Keys of tile i, and values, on their way to their stage; arrived() before the barrier in front of their first use
-    auto tile_at = [&](int i) { return key_of(k0 + team + TEAMS * i); };
-    auto send_keys = [&](const Groups& t, int i) {
-        if constexpr (BITS == 16) direct(a.pages_k, t, k_off, lds0 + (unsigned)((i & 1) * STAGE));
-        else fetch(a.pages_k, t, mk);
-    };
-    auto send_values = [&](const Groups& t, int i) {
-        if constexpr (BITS == 16) {
-            if (plain(tile_at(i), t.gone)) {
-                direct(a.pages_v, t, v_off, lds0 + (unsigned)((i & 1) * STAGE + KT * ROW));
-            } else {
-                fetch(a.pages_v, t, mv);
-                put_values(tile_at(i), t.gone, 0, i & 1);
-            }
-        } else {
-            fetch(a.pages_v, t, mv);
-        }
-    };
-
     // q, its sign that of the scale
     const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
     Frag q[NK];
@@ -435,16 +403,27 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     __syncthreads();
     look(0);
     if (mine > 0) {
-        const Groups t = groups_of(0);
-        gone = t.gone;
-        send_keys(t, 0);
-        if constexpr (BITS == 8) put_keys(t.k_bytes, 0);
-        send_values(t, 0);
-        if constexpr (BITS == 8) put_values(tile_at(0), gone, t.v_bytes, 0);
-        if (mine > 1) {
-            const Groups n = groups_of(1);
-            send_keys(n, 1);
-            if constexpr (BITS == 8) put_keys(n.k_bytes, 1);
+        gone = gone_of(0);
+        const int more = mine > 1 ? 1 : 0;
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) {
+            if constexpr (BITS == 16) direct_keys(0, e, 0);
+            else fetch_keys(0, e);
+            fetch_values(0, e);
+        }
+        if constexpr (BITS == 16) {
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) direct_keys(more, e, 1);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) put_keys(0, e, 0);
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) fetch_keys(more, e);
+        }
+        put_values(0, gone);
+        if constexpr (BITS == 8) {
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) put_keys(more, e, 1);
         }
     }
     arrived();
@@ -455,19 +434,33 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     }
     __syncthreads();
     auto step = [&](int i, f16x (&S)[2], f16x (&N)[2], int stage) {
-        uint32_t v_bytes = 0, k_bytes = 0;
-        if (i + 1 < mine) {
-            const Groups t = groups_of(i + 1);
-            gone_next = t.gone;
-            v_bytes = t.v_bytes;
-            send_values(t, i + 1);
+        const bool more = i + 1 < mine;
+        const int iv = more ? i + 1 : i, ik = i + 2 < mine ? i + 2 : (mine > 0 ? mine - 1 : 0);         // (behind the last tile: it again, to where nobody reads)
+        bool as_it_is = false;
+        if (more) {
+            gone_next = gone_of(iv);
+            as_it_is = plain(tile_at(iv), gone_next);
+            if (BITS == 16 && !as_it_is) {
+#pragma unroll
+                for (int e = 0; e < PIECES; ++e) fetch_values(iv, e);
+                put_values(iv, gone_next);
+            }
         }
-        if (i + 2 < mine) {
-            if (((i + 2) & 15) == 0) look(i + 2);
-            const Groups t = groups_of(i + 2);
-            k_bytes = t.k_bytes;
-            send_keys(t, i + 2);
+        if constexpr (BITS == 8) {
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) fetch_values(iv, e);
         }
+        // (tile iv is of the last look yet)
+        unsigned v_low[PIECES], v_high[PIECES];
+        if constexpr (BITS == 16) {
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) {
+                const unsigned long long at = (unsigned long long)memory_of(a.pages_v, iv, e);
+                v_low[e] = __builtin_amdgcn_readfirstlane((unsigned)at);
+                v_high[e] = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+            }
+        }
+        if (((i + 2) & 15) == 0 && i + 2 < mine) look(i + 2);
         if (i < mine) {
             const unsigned char* base = mine_at + stage * STAGE;
             const int key0 = tile_at(i);
@@ -524,6 +517,13 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                 N[b] = mfma32(kf[x % AHEAD].v, q[t].v, N[b]);
                 if (x + AHEAD < 2 * NK) read_k(x + AHEAD);
                 else read_v(x + AHEAD - 2 * NK);
+                if (x < PIECES) {
+                    if constexpr (BITS == 16) direct_keys(ik, x, stage);
+                    else fetch_keys(ik, x);
+                } else if (BITS == 16 && x < 2 * PIECES) {
+                    const int e = x - PIECES;
+                    memory_to_lds((const char*)((unsigned long long)v_high[e] << 32 | v_low[e]), v_off, as_it_is ? lds0 + (unsigned)((stage ^ 1) * STAGE + KT * ROW + key_at(e) * ROW) : aside);
+                }
 #pragma unroll
                 for (int w = 16 * x / (2 * NK); w < 16 * (x + 1) / (2 * NK); ++w) weights(w);
                 __builtin_amdgcn_sched_barrier(0);
@@ -539,8 +539,11 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
             }
         }
         if constexpr (BITS == 8) {
-            if (i + 2 < mine) put_keys(k_bytes, stage);
-            if (i + 1 < mine) put_values(tile_at(i + 1), gone_next, v_bytes, stage ^ 1);
+            if (i < mine) {
+#pragma unroll
+                for (int e = 0; e < PIECES; ++e) put_keys(ik, e, stage);
+            }
+            if (more) put_values(iv, gone_next);
         }
         gone = gone_next;
         arrived();
@@ -706,7 +709,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    constexpr int lds = teams<DIM>() * 2 * 2 * KT * 2 * DIM;
+    constexpr int lds = teams<DIM>() * (2 * 2 * KT * 2 * DIM + (BITS == 16 ? RG * 1024 : 0));
     const auto kern = prompt_kernel<DIM, BITS, BLOCKS>;
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
