@@ -171,18 +171,22 @@ def cache_attention_rows(q, pages_k, pages_v, page_table, lengths, row_starts, w
             if not len(at):
                 continue
             pages, place = page_table[b, at // page], at % page
-            for i in range(heads):
-                h = i // (heads // kv)
+            for h in range(kv):
+                mine = slice(h * (heads // kv), (h + 1) * (heads // kv))         # the query heads of this kv head
                 K, V = pages_k[pages, h, place], pages_v[pages, h, place]
                 with np.errstate(invalid="ignore"):
-                    s = scale * (K @ q[m, i])
-                    top = s.max()
-                    if top == -np.inf:
-                        continue
-                    w = np.exp(s - top)
-                    out[m, i] = ((w @ V) if np.isfinite(V).all() else np.where(w[:, None] == 0, 0.0, w[:, None] * V).sum(0)) / w.sum()
-                    size[m, i] = (w @ np.abs(V)) / w.sum()
-                    lse[m, i] = top + math.log(w.sum())
-                    most[m, i] = np.abs(V).max()
-                    logit[m, i] = (abs(scale) * (np.abs(K) @ np.abs(q[m, i]))).max()
+                    s = scale * (q[m, mine] @ K.T)
+                    top = s.max(-1)
+                    some = ~(top == -np.inf)
+                    w = np.exp(s - np.where(some, top, 0.0)[:, None])
+                    total = np.where(some, w.sum(-1), 1.0)
+                    if np.isfinite(V).all():
+                        o = w @ V
+                    else:
+                        o = np.stack([np.where(x[:, None] == 0, 0.0, x[:, None] * V).sum(0) for x in w])
+                    out[m, mine] = np.where(some[:, None], o / total[:, None], 0.0)
+                    size[m, mine] = np.where(some[:, None], (w @ np.abs(V)) / total[:, None], 0.0)
+                    lse[m, mine] = np.where(some, top + np.log(total), -np.inf)
+                    most[m, mine] = np.abs(V).max()
+                    logit[m, mine] = (abs(scale) * (np.abs(q[m, mine]) @ np.abs(K).T)).max(-1)
     return out, lse, size, most, logit

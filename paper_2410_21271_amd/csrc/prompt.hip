@@ -28,19 +28,19 @@
 namespace eora {
 namespace {
 
-constexpr int RG = 4, TQ = 32 * RG;            // wavefronts of a team, pairs of a tile
+// Wavefronts of a team (RG), 32 pairs each; teams of a workgroup
+constexpr int teams_of(int dim, int rg) { return dim == 256 || rg == 8 ? 1 : 2; }
+constexpr int FEW = 4, MANY = 8;
 constexpr int KT = 64;                         // keys of a tile
 constexpr int CUS = 256;
-constexpr int WANT = 2 * CUS;                  // parts that all tiles together are cut into at least, where they have the work
+// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see unit_of().  (Those of 256 pairs are half as many.)
+constexpr int want_of(int rg) { return 2 * CUS * FEW / rg; }
+constexpr int MAX_PARTS = 2 * want_of(FEW);
 constexpr int LEAST_PART = 4;                  // tiles of keys of a part
-constexpr int MAX_PARTS = 2 * WANT;            // partial results: see unit_of()
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr float RAISE = 4.f, LOWER = 11.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-template <int DIM>
-constexpr int teams() { return DIM == 256 ? 1 : 2; }
 
 typedef float f16x __attribute__((ext_vector_type(16)));
 typedef __fp16 tr4 __attribute__((__vector_size__(8)));
@@ -70,6 +70,7 @@ __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::
 struct Request {
     int n, first, rows, tiles, cost;
 };
+template <int TQ>
 __device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
 {
     Request r;
@@ -97,7 +98,7 @@ struct Unit {
 };
 // All threads.  Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have less
 // than 2 WANT parts.
-template <int THREADS>
+template <int THREADS, int TQ, int WANT>
 __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& u, int* scratch)
 {
     constexpr int NW = THREADS / 64;
@@ -107,7 +108,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
     int* totals = found + 4;                                                    // 2 NW
     unsigned long long work = 0;
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
-        const Request r = request_of(a, b);
+        const Request r = request_of<TQ>(a, b);
         work += (unsigned long long)r.tiles * r.cost;
     }
 #pragma unroll
@@ -125,7 +126,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
         const int b = b0 + (int)threadIdx.x;
         unsigned units = 0, cut = 0;
         if (b < a.B) {
-            const Request r = request_of(a, b);
+            const Request r = request_of<TQ>(a, b);
             const unsigned parts = r.cost <= share ? 1u : (unsigned)((r.cost + share - 1) / share);
             units = (unsigned)r.tiles * parts * (unsigned)a.kv;
             cut = parts > 1 ? units : 0;
@@ -164,7 +165,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
     }
     u.b = __builtin_amdgcn_readfirstlane(found[0]);
     if (u.b < 0) return false;
-    const Request r = request_of(a, u.b);
+    const Request r = request_of<TQ>(a, u.b);
     const int local = __builtin_amdgcn_readfirstlane(found[1]), cut = __builtin_amdgcn_readfirstlane(found[2]);
     u.parts = r.cost <= share ? 1 : (int)((r.cost + share - 1) / share);
     const int rest = local / a.kv, tile = rest / u.parts;
@@ -190,21 +191,36 @@ __device__ __forceinline__ float2 get2(const float* p)
 __device__ __forceinline__ float factor(float m, float to) { return m == -INFINITY ? 0.f : exp2_(m - to); }
 
 // words of a partial result: (m, sum) and O of each pair
-template <int DIM>
-constexpr size_t part_words() { return (size_t)TQ * (DIM + 2); }
+constexpr size_t part_words(int dim, int rg) { return (size_t)32 * rg * (dim + 2); }
 
-template <int DIM, int BITS, bool BLOCKS>
-__global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_kernel(const PromptArgs a)
+// K in LDS: rows in groups of 1 KiB, as they come from memory, with a gap behind each group
+constexpr int k_group(int dim) { return 512 / dim; }
+constexpr int K_GAP = 64, K_GAP_256 = 32;
+constexpr int k_pitch(int dim) { return 1024 + (dim == 256 ? K_GAP_256 : K_GAP); }
+constexpr int stage_bytes(int dim) { return KT / k_group(dim) * k_pitch(dim) + KT * 2 * dim; }
+template <int DIM, int BITS, int RG>
+constexpr int lds_bytes()
 {
-    constexpr int TEAMS = teams<DIM>(), THREADS = 64 * RG * TEAMS, TEAM = 64 * RG;
+    constexpr int loop = teams_of(DIM, RG) * (2 * stage_bytes(DIM) + (BITS == 16 ? RG * 1024 : 0)), end = 32 * RG * DIM * 4;
+    return loop > end ? loop : end;
+}
+
+template <int DIM, int BITS, bool BLOCKS, int RG>
+__global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG) / 4) void prompt_kernel(const PromptArgs a)
+{
+    constexpr int TEAMS = teams_of(DIM, RG), THREADS = 64 * RG * TEAMS, TEAM = 64 * RG, TQ = 32 * RG;
     constexpr int ROW = 2 * DIM;               // bytes of a row in LDS
-    constexpr int STAGE = 2 * KT * ROW;        // keys, then values
+    constexpr int GROUP = k_group(DIM), PITCH = k_pitch(DIM);
+    constexpr int STAGE = stage_bytes(DIM), VALUES = STAGE - KT * ROW;            // keys, then values
     constexpr int NK = DIM / 16, ND = DIM / 32;                   // k-steps of the first product, blocks of O^T
     constexpr int PER = 16 / (BITS / 8);       // elements of a 16-byte piece in memory
     constexpr int PIECES = KT * DIM / PER / TEAM;                 // pieces of K (of V) a thread moves
     constexpr int PR = DIM / PER;              // pieces of a row
     constexpr int AHEAD = 4;                   // matrix instructions between an operand's read and its use
-    constexpr int VX = DIM == 64 ? 3 : 7;      // how many units of 32 bytes of V's rows change places
+    // How pieces of 16 bytes change places in the row of a key, so that the lanes that read at a time meet different banks: 16 keys' pieces of the same columns; two units of 32 bytes
+    // of four keys
+    auto k_turn_of = [](int key) { return DIM == 64 ? key >> 1 & 3 : (DIM == 128 ? key & 3 : key & 1); };
+    auto v_turn_of = [](int key) { return 4 * (DIM == 64 ? key >> 1 & 1 : key & 3); };
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ int scratch[2 * 8 + 4 + 2 * 8];
@@ -213,8 +229,8 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     __shared__ float red_m[TEAMS][TQ], red_l[TEAMS][TQ];
 
     Unit u;
-    if (!unit_of<THREADS>(a, blockIdx.x, u, scratch)) return;
-    Request r = request_of(a, u.b);
+    if (!unit_of<THREADS, TQ, want_of(RG)>(a, blockIdx.x, u, scratch)) return;
+    Request r = request_of<TQ>(a, u.b);
     r.n = __builtin_amdgcn_readfirstlane(r.n);
     r.first = __builtin_amdgcn_readfirstlane(r.first);
     r.rows = __builtin_amdgcn_readfirstlane(r.rows);
@@ -284,8 +300,9 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     // Pieces of 16 bytes in memory: this lane's place among those that its wavefront moves at a time, which lie in one group of keys; piece e of the wavefront begins with key key_at(e)
     const int tw = wave % RG, lrow = lane / PR, lpiece = lane % PR;
     auto key_at = [&](int e) { return tw * (64 / PR) + e * (TEAM / PR); };
-    const int turn = tw * (64 / PR) + lrow;    // its key, but for multiples of 8
-    auto group_at = [&](int e) { return TEAM / PR <= 16 ? e * (TEAM / PR) / 16 : (TEAM / PR == 32 ? 2 * e + (tw >> 1) : tw); };
+    auto k_place = [&](int key, int piece) { return key / GROUP * PITCH + key % GROUP * ROW + 16 * (piece ^ k_turn_of(key)); };
+    auto v_place = [&](int key, int piece) { return VALUES + key * ROW + 16 * (piece ^ v_turn_of(key)); };
+    auto group_at = [&](int e) { return key_at(e) / 16; };
     const unsigned rows_off = (unsigned)(tw * (64 / PR) % 16 * (DIM * BITS / 8));               // (of a piece behind its block's beginning, but for e)
     auto memory_of = [&](const void* pages, int i, int e) {
         const int from_lane = 4 * (i & 15) + group_at(e);
@@ -293,10 +310,10 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
         return (const char*)pages + ((unsigned long long)high_word << 32 | low_word) + e * (TEAM / PR) % 16 * (DIM * BITS / 8);
     };
     // straight from memory to LDS (fp16): pieces change places on the way, as the addresses say
-    const unsigned k_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ (turn & 7))), v_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ (2 * (turn & VX))));
+    const unsigned k_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ k_turn_of(key_at(0) + lrow))), v_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ v_turn_of(key_at(0) + lrow)));
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(team * 2 * STAGE);
     const unsigned aside = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(TEAMS * 2 * STAGE + wave * 1024);     // (what nobody reads)
-    auto direct_keys = [&](int i, int e, int stage) { memory_to_lds(memory_of(a.pages_k, i, e), k_off, lds0 + (unsigned)(stage * STAGE + key_at(e) * ROW)); };
+    auto direct_keys = [&](int i, int e, int stage) { memory_to_lds(memory_of(a.pages_k, i, e), k_off, lds0 + (unsigned)(stage * STAGE + key_at(e) / GROUP * PITCH)); };
     // by way of registers
     u4 mk[PIECES], mv[PIECES];
     float v_by[PIECES];
@@ -322,11 +339,11 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
         expand(mk[e], BLOCKS ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_power), 4 * (i & 15) + group_at(e))) : 1.f, f);
         const int key = key_at(e) + lrow;
 #pragma unroll
-        for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (turn & 7))) = f[w].q;
+        for (int w = 0; w < PER / 8; ++w) *(u4*)(to + k_place(key, lpiece * (PER / 8) + w)) = f[w].q;
     };
     // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
     auto put_values = [&](int i, unsigned gone) {
-        unsigned char* to = smem + (team * 2 + (i & 1)) * STAGE + KT * ROW;
+        unsigned char* to = smem + (team * 2 + (i & 1)) * STAGE;
         const int key0 = tile_at(i);
         const bool as_it_is = plain(key0, gone);
         bool odd = false;
@@ -349,7 +366,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                     }
             }
 #pragma unroll
-            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + key * ROW + 16 * ((lpiece * (PER / 8) + w) ^ (2 * (turn & VX)))) = f[w].q;
+            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + v_place(key, lpiece * (PER / 8) + w)) = f[w].q;
         }
         if (!as_it_is && odd) odd_one = 1;
     };
@@ -372,8 +389,9 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     float m = -INFINITY, l = 0.f;
 
     // where this lane reads: K, row col: piece 2 t + half; V, transposed: rows 4 half + lane % 16 / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of 32
-    const int k_at = col * ROW, k_turn = half ^ (col & 7);
-    const int v_key = 4 * half + (lane & 15) / 4, v_at = KT * ROW + v_key * ROW + 8 * (lane & 3), v_turn = (lane >> 4 & 1) ^ (v_key & VX);
+    constexpr int BLOCK_OF_KEYS = 32 / GROUP * PITCH;
+    const int k_at = col / GROUP * PITCH + col % GROUP * ROW, k_turn = half ^ k_turn_of(col);
+    const int v_key = 4 * half + (lane & 15) / 4, v_at = VALUES + v_key * ROW + 8 * (lane & 3), v_turn = (lane >> 4 & 1) ^ (v_turn_of(v_key) / 2);
     const unsigned char* mine_at = smem + team * 2 * STAGE;
     auto first_product = [&](const unsigned char* base, f16x (&S)[2]) {
 #pragma unroll
@@ -382,7 +400,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
 #pragma unroll
             for (int t = 0; t < NK; ++t) {
                 Frag k;
-                k.q = *(const u4*)(base + k_at + 32 * b * ROW + 16 * ((2 * t) ^ k_turn));
+                k.q = *(const u4*)(base + k_at + b * BLOCK_OF_KEYS + 16 * ((2 * t) ^ k_turn));
                 z = mfma32(k.v, q[t].v, z);
             }
             S[b] = z;
@@ -490,7 +508,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
             // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
             const unsigned char* next = mine_at + (stage ^ 1) * STAGE;
             Frag kf[AHEAD], vf[AHEAD], p[4];
-            auto read_k = [&](int x) { kf[x % AHEAD].q = *(const u4*)(next + k_at + 32 * (x % 2) * ROW + 16 * ((2 * (x / 2)) ^ k_turn)); };
+            auto read_k = [&](int x) { kf[x % AHEAD].q = *(const u4*)(next + k_at + x % 2 * BLOCK_OF_KEYS + 16 * ((2 * (x / 2)) ^ k_turn)); };
             auto read_v = [&](int x) {
                 const int s = x / ND, d = x % ND;
 #pragma unroll
@@ -522,7 +540,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
                     else fetch_keys(ik, x);
                 } else if (BITS == 16 && x < 2 * PIECES) {
                     const int e = x - PIECES;
-                    memory_to_lds((const char*)((unsigned long long)v_high[e] << 32 | v_low[e]), v_off, as_it_is ? lds0 + (unsigned)((stage ^ 1) * STAGE + KT * ROW + key_at(e) * ROW) : aside);
+                    memory_to_lds((const char*)((unsigned long long)v_high[e] << 32 | v_low[e]), v_off, as_it_is ? lds0 + (unsigned)((stage ^ 1) * STAGE + VALUES + key_at(e) * ROW) : aside);
                 }
 #pragma unroll
                 for (int w = 16 * x / (2 * NK); w < 16 * (x + 1) / (2 * NK); ++w) weights(w);
@@ -637,7 +655,7 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     const int used = pair1 - pair0;
     if (parts > 1) {
         // a partial result: rows of (m, sum), then rows of DIM
-        float* part = a.parts + COUNTERS + (size_t)u.place * part_words<DIM>();
+        float* part = a.parts + COUNTERS + (size_t)u.place * part_words(DIM, RG);
 #pragma unroll 4
         for (int e = 0; e < MY; ++e) {
             const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
@@ -657,8 +675,8 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
         }
         __syncthreads();
         if (!last) return;
-        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words<DIM>();
-        const size_t step_words = (size_t)a.kv * part_words<DIM>();
+        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words(DIM, RG);
+        const size_t step_words = (size_t)a.kv * part_words(DIM, RG);
         for (int e = 0; e < MY; ++e) {
             const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
             if (r2 >= used) break;
@@ -706,15 +724,28 @@ __global__ __launch_bounds__(64 * RG * teams<DIM>(), teams<DIM>()) void prompt_k
     }
 }
 
+// From so many tiles of 256 pairs on (of all kv heads together) workgroups have such tiles
+constexpr long long MANY_TILES = 512;
+
+template <int DIM, int BITS, bool BLOCKS, int RG>
+hipError_t start(const PromptArgs& a, hipStream_t stream)
+{
+    constexpr int lds = lds_bytes<DIM, BITS, RG>();
+    const auto kern = prompt_kernel<DIM, BITS, BLOCKS, RG>;
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    kern<<<(unsigned)prompt_units(a.M, a.B, a.heads, a.kv, RG), 64 * RG * teams_of(DIM, RG), lds, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    constexpr int lds = teams<DIM>() * (2 * 2 * KT * 2 * DIM + (BITS == 16 ? RG * 1024 : 0));
-    const auto kern = prompt_kernel<DIM, BITS, BLOCKS>;
-    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    kern<<<(unsigned)prompt_units(a.M, a.B, a.heads, a.kv, DIM), 64 * RG * teams<DIM>(), lds, stream>>>(a);
-    return hipGetLastError();
+    // (heads of 256 leave no registers for two wavefronts a SIMD; of 64 in 8 bits, half of eight wavefronts would have nothing to move)
+    if constexpr (DIM == 128 || (DIM == 64 && BITS == 16)) {
+        if ((long long)a.M * a.heads >= 32 * MANY * MANY_TILES) return start<DIM, BITS, BLOCKS, MANY>(a, stream);
+    }
+    return start<DIM, BITS, BLOCKS, FEW>(a, stream);
 }
 
 template <int DIM>
@@ -726,17 +757,13 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
 
 }  // namespace
 
-long long prompt_units(int M, int B, int heads, int kv, int dim)
+long long prompt_units(int M, int B, int heads, int kv, int rg)
 {
     const long long group = heads / kv;
-    return (((long long)M * group + TQ - 1) / TQ + B) * kv + MAX_PARTS;
+    return (((long long)M * group + 32 * rg - 1) / (32 * rg) + B) * kv + 2 * want_of(rg);
 }
 
-size_t prompt_workspace_bytes(int dim)
-{
-    const size_t words = dim == 64 ? part_words<64>() : (dim == 128 ? part_words<128>() : part_words<256>());
-    return (COUNTERS + MAX_PARTS * words) * sizeof(float);
-}
+size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words(dim, FEW)) * sizeof(float); }
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream)
 {

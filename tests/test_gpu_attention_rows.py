@@ -145,6 +145,29 @@ SHAPES = [
 ]
 
 
+# 2^17 pairs of a row and a query head and more: tiles of 256
+MANY = [
+    ([(300, 200), (77, 30), (1, 1), (64, 34)], 512, 1, 64, "fp16", 16),
+    ([(257, 150), (40, 50), (120, 80)], 480, 2, 128, "fp16", 48),
+    ([(130, 130), (900, 3), (200, 70)], 704, 1, 128, "blocks", 16),
+    ([(100, 90), (350, 170)], 512, 4, 128, "heads", 32),
+]
+
+
+@pytest.mark.parametrize("requests,heads,kv,dim,form,page", MANY)
+def test_many_pairs(gpu, requests, heads, kv, dim, form, page):
+    c = Rows(heads + dim, requests, heads, kv, dim, form, page)
+    assert c.M * heads >= 2 ** 17
+    c.check(gpu)
+    c.check(gpu, 50, 7)
+
+
+def test_many_pairs_cut_along_the_keys(gpu):
+    """One long request among short ones, in tiles of 256 pairs."""
+    Rows(54, [(3000, 3)] + [(10, 10)] * 50, 256, 1, 128, "blocks", 16).check(gpu)
+    Rows(55, [(2000, 2)] + [(7, 7)] * 75, 256, 1, 64, "fp16", 16).check(gpu, 900, 5)
+
+
 @pytest.mark.parametrize("requests,heads,kv,dim,form,page", SHAPES)
 def test_shapes(gpu, requests, heads, kv, dim, form, page):
     c = Rows(len(requests) + heads + dim, requests, heads, kv, dim, form, page, tail=2)
@@ -259,12 +282,14 @@ def test_many_tokens_far_below_the_largest(gpu):
     c.check(gpu, scale=1.0)
 
 
-@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dim,pairs", [(64, 1), (128, 1), (256, 1), (64, 194), (128, 194)])
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
-def test_what_a_row_does_not_see_is_not_used(gpu, dim, value):
+def test_what_a_row_does_not_see_is_not_used(gpu, dim, pairs, value):
     """Keys and values that are not finite, of tokens that some rows of a tile see and others do not: rows that do not see them have the bits that they have without them."""
+    heads = 4 * pairs
+
     def case():
-        return Rows(44, [(150, 100), (70, 70)], 4, 2, dim, "fp16", 16)
+        return Rows(44, [(150, 100), (70, 70)], heads, 2, dim, "fp16", 16)
     clean = case()
     base, base_lse = clean.run(gpu, 60, 2)
     for what in ("k", "v"):
@@ -279,11 +304,11 @@ def test_what_a_row_does_not_see_is_not_used(gpu, dim, value):
             for r in range(c.starts[b], c.starts[b + 1]):
                 p = c.lengths[b] - c.starts[b + 1] + r
                 hit = any(t <= p and (t > p - 60 or t < 2) for at, t in ((0, 75), (1, 30), (1, 0)) if at == b)
-                assert np.array_equal(out[r, :2], base[r, :2]), "the other kv head"
+                assert np.array_equal(out[r, :heads // 2], base[r, :heads // 2]), "the other kv head"
                 if not hit:
                     assert np.array_equal(out[r], base[r]) and np.array_equal(lse[r], base_lse[r]), "row %d of request %d" % (r, b)
                 elif what == "v":
-                    for i in (2, 3):
+                    for i in (heads // 2, heads - 1):
                         close(out[r, i, 5], want[r, i, 5], 0, "row %d" % r)
                         assert np.array_equal(np.delete(out[r, i], 5), np.delete(base[r, i], 5))
 
