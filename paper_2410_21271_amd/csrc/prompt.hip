@@ -25,17 +25,17 @@
 #include "heads.hpp"
 #include "serving.hpp"
 
+#include <utility>
+
 namespace eora {
 namespace {
 
-// Wavefronts of a team (RG), 32 pairs each; teams of a workgroup
-constexpr int teams_of(int dim, int rg) { return dim == 256 || rg == 8 ? 1 : 2; }
-constexpr int FEW = 4, MANY = 8;
+constexpr int RG = 4, THREADS = 64 * RG, TQ = 32 * RG;           // wavefronts; pairs of a tile
 constexpr int KT = 64;                         // keys of a tile
 constexpr int CUS = 256;
-// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see unit_of().  (Those of 256 pairs are half as many.)
-constexpr int want_of(int rg) { return 2 * CUS * FEW / rg; }
-constexpr int MAX_PARTS = 2 * want_of(FEW);
+// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see unit_of().
+constexpr int WANT = 2 * CUS;
+constexpr int MAX_PARTS = 2 * WANT;
 constexpr int LEAST_PART = 4;                  // tiles of keys of a part
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
@@ -55,14 +55,16 @@ __device__ __forceinline__ float max_of_halves(float v)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// 64 pieces of 16 bytes from memory straight into 1 KiB of LDS, lane after lane.  The compiler does not know of the request: it counts in vmcnt all the same, so the compiler's own
-// waits only get longer, and whoever reads the bytes waits for them (arrived()) before the barrier in front of the reads.
+// 64 pieces of 16 bytes from memory straight into 1 KiB of LDS, lane after lane: from base + off + OFF to lds + OFF.  The compiler does not know of the request: it counts in vmcnt all
+// the same, so the compiler's own waits only get longer, and whoever reads the bytes waits for them (arrived()) before the barrier in front of the reads.
+template <int OFF>
 __device__ __forceinline__ void memory_to_lds(const char* base, unsigned off, unsigned lds)
 {
+    static_assert(OFF >= 0 && OFF < 4096, "");
     const unsigned long long at = (unsigned long long)base;
     const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)at), high = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"((unsigned long long)high << 32 | low) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+                 : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"((unsigned long long)high << 32 | low), "i"(OFF) : "memory", "m0");
 }
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -70,7 +72,6 @@ __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::
 struct Request {
     int n, first, rows, tiles, cost;
 };
-template <int TQ>
 __device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
 {
     Request r;
@@ -98,7 +99,6 @@ struct Unit {
 };
 // All threads.  Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have less
 // than 2 WANT parts.
-template <int THREADS, int TQ, int WANT>
 __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& u, int* scratch)
 {
     constexpr int NW = THREADS / 64;
@@ -108,7 +108,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
     int* totals = found + 4;                                                    // 2 NW
     unsigned long long work = 0;
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
-        const Request r = request_of<TQ>(a, b);
+        const Request r = request_of(a, b);
         work += (unsigned long long)r.tiles * r.cost;
     }
 #pragma unroll
@@ -126,7 +126,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
         const int b = b0 + (int)threadIdx.x;
         unsigned units = 0, cut = 0;
         if (b < a.B) {
-            const Request r = request_of<TQ>(a, b);
+            const Request r = request_of(a, b);
             const unsigned parts = r.cost <= share ? 1u : (unsigned)((r.cost + share - 1) / share);
             units = (unsigned)r.tiles * parts * (unsigned)a.kv;
             cut = parts > 1 ? units : 0;
@@ -165,7 +165,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& 
     }
     u.b = __builtin_amdgcn_readfirstlane(found[0]);
     if (u.b < 0) return false;
-    const Request r = request_of<TQ>(a, u.b);
+    const Request r = request_of(a, u.b);
     const int local = __builtin_amdgcn_readfirstlane(found[1]), cut = __builtin_amdgcn_readfirstlane(found[2]);
     u.parts = r.cost <= share ? 1 : (int)((r.cost + share - 1) / share);
     const int rest = local / a.kv, tile = rest / u.parts;
@@ -190,32 +190,39 @@ __device__ __forceinline__ float2 get2(const float* p)
 }
 __device__ __forceinline__ float factor(float m, float to) { return m == -INFINITY ? 0.f : exp2_(m - to); }
 
+// f(0) .. f(N - 1), each number a type
+template <int N, typename F, int... I>
+__device__ __forceinline__ void each_of(const F& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void each_piece(const F& f) { each_of<N>(f, std::make_integer_sequence<int, N>{}); }
+
 // words of a partial result: (m, sum) and O of each pair
-constexpr size_t part_words(int dim, int rg) { return (size_t)32 * rg * (dim + 2); }
+constexpr size_t part_words(int dim) { return (size_t)TQ * (dim + 2); }
 
 // K in LDS: rows in groups of 1 KiB, as they come from memory, with a gap behind each group
 constexpr int k_group(int dim) { return 512 / dim; }
 constexpr int K_GAP = 64, K_GAP_256 = 32;
 constexpr int k_pitch(int dim) { return 1024 + (dim == 256 ? K_GAP_256 : K_GAP); }
 constexpr int stage_bytes(int dim) { return KT / k_group(dim) * k_pitch(dim) + KT * 2 * dim; }
-template <int DIM, int BITS, int RG>
+template <int DIM, int BITS>
 constexpr int lds_bytes()
 {
-    constexpr int loop = teams_of(DIM, RG) * (2 * stage_bytes(DIM) + (BITS == 16 ? RG * 1024 : 0)), end = 32 * RG * DIM * 4;
+    constexpr int loop = 2 * stage_bytes(DIM) + BLOCK_TOKENS * DIM * BITS / 8, end = TQ * DIM * 4;
     return loop > end ? loop : end;
 }
 
-template <int DIM, int BITS, bool BLOCKS, int RG>
-__global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG) / 4) void prompt_kernel(const PromptArgs a)
+// Workgroups a compute unit has at a time, as registers and LDS allow
+constexpr int residents(int dim) { return dim == 256 ? 1 : 2; }
+
+template <int DIM, int BITS, bool BLOCKS>
+__global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const PromptArgs a)
 {
-    constexpr int TEAMS = teams_of(DIM, RG), THREADS = 64 * RG * TEAMS, TEAM = 64 * RG, TQ = 32 * RG;
     constexpr int ROW = 2 * DIM;               // bytes of a row in LDS
     constexpr int GROUP = k_group(DIM), PITCH = k_pitch(DIM);
     constexpr int STAGE = stage_bytes(DIM), VALUES = STAGE - KT * ROW;            // keys, then values
     constexpr int NK = DIM / 16, ND = DIM / 32;                   // k-steps of the first product, blocks of O^T
-    constexpr int PER = 16 / (BITS / 8);       // elements of a 16-byte piece in memory
-    constexpr int PIECES = KT * DIM / PER / TEAM;                 // pieces of K (of V) a thread moves
-    constexpr int PR = DIM / PER;              // pieces of a row
+    constexpr int BYTES = DIM * BITS / 8;      // of a row in memory
+    constexpr int PIECES = BLOCK_TOKENS * BYTES / 1024;           // KiB of a wavefront's 16 keys (or values) of a tile
     constexpr int AHEAD = 4;                   // matrix instructions between an operand's read and its use
     // How pieces of 16 bytes change places in the row of a key, so that the lanes that read at a time meet different banks: 16 keys' pieces of the same columns; two units of 32 bytes
     // of four keys
@@ -226,16 +233,16 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
     __shared__ int scratch[2 * 8 + 4 + 2 * 8];
     __shared__ int odd_one;                    // some value that not all rows see is not finite
     __shared__ int last;
-    __shared__ float red_m[TEAMS][TQ], red_l[TEAMS][TQ];
+    __shared__ float row_m[TQ], row_l[TQ];
 
     Unit u;
-    if (!unit_of<THREADS, TQ, want_of(RG)>(a, blockIdx.x, u, scratch)) return;
-    Request r = request_of<TQ>(a, u.b);
+    if (!unit_of(a, blockIdx.x, u, scratch)) return;
+    Request r = request_of(a, u.b);
     r.n = __builtin_amdgcn_readfirstlane(r.n);
     r.first = __builtin_amdgcn_readfirstlane(r.first);
     r.rows = __builtin_amdgcn_readfirstlane(r.rows);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / RG, rg = wave % RG;
-    const int tt = threadIdx.x % TEAM, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
     const int group = a.heads / a.kv, pairs = r.rows * group, from = r.n - r.rows;             // from: position of row 0 (below 0: rows that see nothing)
     const int pair0 = u.tile * TQ, pair1 = pair0 + TQ < pairs ? pair0 + TQ : pairs;
 
@@ -254,21 +261,21 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
     parts = parts < 1 ? 1 : (parts < u.parts ? parts : u.parts);
     if (u.part >= parts) return;
     const int k0 = (int)((long long)tiles * u.part / parts), k1 = (int)((long long)tiles * (u.part + 1) / parts);
-    const int steps = (k1 - k0 + TEAMS - 1) / TEAMS, mine = (k1 - k0 - team + TEAMS - 1) / TEAMS;
+    const int steps = k1 - k0;
 
     // this lane's pair, and the positions that this wavefront's pairs have
-    const int pair = pair0 + 32 * rg + col;
+    const int pair = pair0 + 32 * wave + col;
     const bool there = pair < pair1;
     const int row = there ? pair / group : 0, qh = u.h * group + (there ? pair - row * group : 0);
     const int pos = there ? from + row : -1;
-    const int w0 = pair0 + 32 * rg, w1 = w0 + 32 < pair1 ? w0 + 32 : pair1;                    // (w1 <= w0: no pair)
+    const int w0 = pair0 + 32 * wave, w1 = w0 + 32 < pair1 ? w0 + 32 : pair1;                    // (w1 <= w0: no pair)
     const int wlow = from + w0 / group, whigh = w1 > w0 ? from + (w1 - 1) / group : -1;
     const bool all = w1 - w0 == 32;
 
-    // Blocks of 16 tokens of the next 64 groups of 16 keys of this team: lane 4 i + g has where that of group g of its tile i begins in the cache, in bytes (0: no page, or no key that a
+    // Blocks of 16 tokens of the next 64 groups of 16 keys: lane 4 i + g has where that of group g of its tile i begins in the cache, in bytes (0: no page, or no key that a
     // row sees: those are in `lost`), and its scales
     unsigned off_low = 0, off_high = 0;
-    float k_power = 1.f, v_power = 1.f;
+    unsigned k_byte = 0, v_byte = 0;
     unsigned long long lost = 0;
     const int* table = a.table + (size_t)u.b * a.width;
     const int per_page = a.page / BLOCK_TOKENS;
@@ -281,95 +288,110 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
         for (int g = 0; g < 4; ++g) gone |= (unsigned)(key0 + 16 * g < hi && block_at(key0 + 16 * g) < 0) << g;
         return gone;
     };
-    auto tile_at = [&](int i) { return key_of(k0 + team + TEAMS * i); };
+    auto tile_at = [&](int i) { return key_of(k0 + i); };
     auto look = [&](int i0) {
-        const int i = i0 + (lane >> 2), key = i < mine ? tile_at(i) + 16 * (lane & 3) : hi, block = key < hi ? block_at(key) : -1;
+        const int i = i0 + (lane >> 2), key = i < steps ? tile_at(i) + 16 * (lane & 3) : hi, block = key < hi ? block_at(key) : -1;
         lost = __ballot(block < 0);
-        const size_t off = (size_t)(unsigned)(block < 0 ? 0 : block) * (BLOCK_TOKENS * DIM * BITS / 8);
+        const size_t off = (size_t)(unsigned)(block < 0 ? 0 : block) * (BLOCK_TOKENS * BYTES);
         off_low = (unsigned)off;
         off_high = (unsigned)(off >> 32);
         if constexpr (BLOCKS) {
-            k_power = power_of(block < 0 ? 0 : a.k_scales[block]);
-            v_power = power_of(block < 0 ? 0 : a.v_scales[block]);
+            k_byte = block < 0 ? 0 : a.k_scales[block];
+            v_byte = block < 0 ? 0 : a.v_scales[block];
         }
     };
     auto gone_of = [&](int i) { return (unsigned)(lost >> (4 * (i & 15))) & 15u; };
     // Whether a tile's values can go to LDS as they are: all rows see all of its tokens
     auto plain = [&](int key0, unsigned gone) { return gone == 0 && key0 + KT <= low + 1 && (a.window == 0 || key0 > high - a.window || key0 + KT <= a.sinks); };
 
-    // Pieces of 16 bytes in memory: this lane's place among those that its wavefront moves at a time, which lie in one group of keys; piece e of the wavefront begins with key key_at(e)
-    const int tw = wave % RG, lrow = lane / PR, lpiece = lane % PR;
-    auto key_at = [&](int e) { return tw * (64 / PR) + e * (TEAM / PR); };
+    // A wavefront moves the tile's group of 16 keys that has its number, a KiB at a time: this lane's row of the KiB, and its piece of 16 bytes of it
+    constexpr int PR = BYTES / 16, ROWS = 64 / PR;
+    const int lrow = lane / PR, lpiece = lane % PR;
+    auto block_of = [&](int i) {
+        const int from_lane = 4 * (i & 15) + wave;
+        return (unsigned long long)__builtin_amdgcn_readlane(off_high, from_lane) << 32 | __builtin_amdgcn_readlane(off_low, from_lane);
+    };
+    auto power_at = [&](unsigned bytes, int i) { return BLOCKS ? power_of(__builtin_amdgcn_readlane(bytes, 4 * (i & 15) + wave)) : 1.f; };
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, aside = lds0 + 2 * STAGE;      // (what nobody reads)
+    constexpr int K_MINE = BLOCK_TOKENS / GROUP * PITCH, V_MINE = BLOCK_TOKENS * ROW;           // a wavefront's part of a stage
+    // fp16: pieces change places on the way, as the addresses say.  8 bits: codes as they are, at the beginning of the wavefront's part; it spreads them out there itself
+    const unsigned linear = 16u * lane, k_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ k_turn_of(lrow))) : linear;
+    const unsigned v_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ v_turn_of(lrow))) : linear;
+    auto send_keys = [&](const char* base, auto piece, int stage) {
+        constexpr int e = decltype(piece)::value, far = e / 4 * 4096, off = e % 4 * 1024;
+        memory_to_lds<off>(base + far, k_off, lds0 + (unsigned)(stage * STAGE + wave * K_MINE + (BITS == 16 ? e * PITCH - off : far)));
+    };
+    auto send_values = [&](const char* base, auto piece, unsigned to) {         // (of heads of 256 a KiB has two of the four keys whose pieces change places together)
+        constexpr int e = decltype(piece)::value, far = e / 4 * 4096, off = e % 4 * 1024;
+        memory_to_lds<off>(base + far, BITS == 16 && DIM == 256 && e % 2 ? v_off ^ 128u : v_off, to + far);
+    };
+    auto values_to = [&](int stage) { return lds0 + (unsigned)(stage * STAGE + VALUES + wave * V_MINE); };
+    auto codes = [](const u4& w, float scale, Frag (&f)[2]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[e / 2].p[2 * (e % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, false);
+            f[e / 2].p[2 * (e % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, true);
+        }
+    };
     auto k_place = [&](int key, int piece) { return key / GROUP * PITCH + key % GROUP * ROW + 16 * (piece ^ k_turn_of(key)); };
     auto v_place = [&](int key, int piece) { return VALUES + key * ROW + 16 * (piece ^ v_turn_of(key)); };
-    auto group_at = [&](int e) { return key_at(e) / 16; };
-    const unsigned rows_off = (unsigned)(tw * (64 / PR) % 16 * (DIM * BITS / 8));               // (of a piece behind its block's beginning, but for e)
-    auto memory_of = [&](const void* pages, int i, int e) {
-        const int from_lane = 4 * (i & 15) + group_at(e);
-        const unsigned low_word = __builtin_amdgcn_readlane(off_low, from_lane), high_word = __builtin_amdgcn_readlane(off_high, from_lane);
-        return (const char*)pages + ((unsigned long long)high_word << 32 | low_word) + e * (TEAM / PR) % 16 * (DIM * BITS / 8);
-    };
-    // straight from memory to LDS (fp16): pieces change places on the way, as the addresses say
-    const unsigned k_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ k_turn_of(key_at(0) + lrow))), v_off = rows_off + (unsigned)(lrow * ROW + 16 * (lpiece ^ v_turn_of(key_at(0) + lrow)));
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(team * 2 * STAGE);
-    const unsigned aside = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + (unsigned)(TEAMS * 2 * STAGE + wave * 1024);     // (what nobody reads)
-    auto direct_keys = [&](int i, int e, int stage) { memory_to_lds(memory_of(a.pages_k, i, e), k_off, lds0 + (unsigned)(stage * STAGE + key_at(e) / GROUP * PITCH)); };
-    // by way of registers
-    u4 mk[PIECES], mv[PIECES];
-    float v_by[PIECES];
-    auto fetch_keys = [&](int i, int e) { mk[e] = *(const u4*)(memory_of(a.pages_k, i, e) + (rows_off + 16u * lane)); };
-    auto fetch_values = [&](int i, int e) {
-        mv[e] = *(const u4*)(memory_of(a.pages_v, i, e) + (rows_off + 16u * lane));
-        v_by[e] = BLOCKS ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_power), 4 * (i & 15) + group_at(e))) : 1.f;
-    };
-    auto expand = [&](const u4& w, float scale, Frag (&f)[PER / 8]) {
-        if constexpr (BITS == 16) {
-            f[0].q = w;
-        } else {
+    auto spread_keys = [&](int stage, float scale) {
+        unsigned char* to = smem + stage * STAGE;
+        u4 w[PIECES];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[e / 2].p[2 * (e % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, false);
-                f[e / 2].p[2 * (e % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, true);
-            }
-        }
-    };
-    auto put_keys = [&](int i, int e, int stage) {
-        unsigned char* to = smem + (team * 2 + stage) * STAGE;
-        Frag f[PER / 8];
-        expand(mk[e], BLOCKS ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_power), 4 * (i & 15) + group_at(e))) : 1.f, f);
-        const int key = key_at(e) + lrow;
-#pragma unroll
-        for (int w = 0; w < PER / 8; ++w) *(u4*)(to + k_place(key, lpiece * (PER / 8) + w)) = f[w].q;
-    };
-    // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
-    auto put_values = [&](int i, unsigned gone) {
-        unsigned char* to = smem + (team * 2 + (i & 1)) * STAGE;
-        const int key0 = tile_at(i);
-        const bool as_it_is = plain(key0, gone);
-        bool odd = false;
+        for (int e = 0; e < PIECES; ++e) w[e] = *(const u4*)(to + wave * K_MINE + e * 1024 + linear);
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
-            Frag f[PER / 8];
-            expand(mv[e], v_by[e], f);
-            const int key = key_at(e) + lrow;
-            if (!as_it_is) {
-                const int at = key0 + key;
-                const bool seen = at < hi && (at >= lo || at < sinks) && !(gone >> (key / 16) & 1);
+            Frag f[2];
+            codes(w[e], scale, f);
 #pragma unroll
-                for (int w = 0; w < PER / 8; ++w)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t x = seen ? f[w].u[q] : 0u;
-                        const uint32_t low_half = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, high_half = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
-                        odd |= (low_half | high_half) != 0;
-                        f[w].u[q] = x & ~(low_half | high_half);
-                    }
-            }
-#pragma unroll
-            for (int w = 0; w < PER / 8; ++w) *(u4*)(to + v_place(key, lpiece * (PER / 8) + w)) = f[w].q;
+            for (int h = 0; h < 2; ++h) *(u4*)(to + k_place(BLOCK_TOKENS * wave + e * ROWS + lrow, 2 * lpiece + h)) = f[h].q;
         }
-        if (!as_it_is && odd) odd_one = 1;
     };
+    // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
+    auto clean = [&](Frag& f, int key, int key0, unsigned gone) {
+        const int at = key0 + key;
+        const bool seen = at < hi && (at >= lo || at < sinks) && !(gone >> wave & 1);
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = seen ? f.u[e] : 0u;
+            const uint32_t low_half = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, high_half = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
+            odd |= (low_half | high_half) != 0;
+            f.u[e] = x & ~(low_half | high_half);
+        }
+        if (odd) odd_one = 1;
+    };
+    auto spread_values = [&](int stage, float scale, int key0, unsigned gone, bool as_it_is) {
+        unsigned char* to = smem + stage * STAGE;
+        u4 w[PIECES];
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) w[e] = *(const u4*)(to + VALUES + wave * V_MINE + e * 1024 + linear);
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) {
+            Frag f[2];
+            codes(w[e], scale, f);
+            const int key = BLOCK_TOKENS * wave + e * ROWS + lrow;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!as_it_is) clean(f[h], key, key0, gone);
+                *(u4*)(to + v_place(key, 2 * lpiece + h)) = f[h].q;
+            }
+        }
+    };
+    // fp16 values that need it, by way of registers
+    auto put_values = [&](const char* base, int stage, int key0, unsigned gone) {
+        Frag f[PIECES];
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) f[e].q = *(const u4*)(base + (e * 1024 + linear));
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) {
+            const int key = BLOCK_TOKENS * wave + e * ROWS + lrow;
+            clean(f[e], key, key0, gone);
+            *(u4*)(smem + stage * STAGE + v_place(key, lpiece)) = f[e].q;
+        }
+    };
+
     // q, its sign that of the scale
     const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
     Frag q[NK];
@@ -392,7 +414,6 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
     constexpr int BLOCK_OF_KEYS = 32 / GROUP * PITCH;
     const int k_at = col / GROUP * PITCH + col % GROUP * ROW, k_turn = half ^ k_turn_of(col);
     const int v_key = 4 * half + (lane & 15) / 4, v_at = VALUES + v_key * ROW + 8 * (lane & 3), v_turn = (lane >> 4 & 1) ^ (v_turn_of(v_key) / 2);
-    const unsigned char* mine_at = smem + team * 2 * STAGE;
     auto first_product = [&](const unsigned char* base, f16x (&S)[2]) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -417,70 +438,47 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
     f16x Sa[2], Sb[2];
     float top = -INFINITY;
     unsigned gone = 0, gone_next = 0;          // of tiles i and i + 1
+    const bool busy = w1 > w0;                 // (a wavefront without a pair moves its part of the tiles, and no more)
     if (threadIdx.x == 0) odd_one = 0;
-    __syncthreads();
     look(0);
-    if (mine > 0) {
+    if (steps > 0) {
         gone = gone_of(0);
-        const int more = mine > 1 ? 1 : 0;
-#pragma unroll
-        for (int e = 0; e < PIECES; ++e) {
-            if constexpr (BITS == 16) direct_keys(0, e, 0);
-            else fetch_keys(0, e);
-            fetch_values(0, e);
-        }
-        if constexpr (BITS == 16) {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) direct_keys(more, e, 1);
-        } else {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) put_keys(0, e, 0);
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) fetch_keys(more, e);
-        }
-        put_values(0, gone);
+        const int key0 = tile_at(0), second = steps > 1 ? 1 : 0;
+        const bool as_it_is = plain(key0, gone);
+        const unsigned long long here = block_of(0), there_on = block_of(second);
+        const char *k0_at = (const char*)a.pages_k + here, *v0_at = (const char*)a.pages_v + here, *k1_at = (const char*)a.pages_k + there_on;
+        each_piece<PIECES>([&](auto e) { send_keys(k0_at, e, 0); });
+        if (BITS == 8 || as_it_is) each_piece<PIECES>([&](auto e) { send_values(v0_at, e, values_to(0)); });
+        each_piece<PIECES>([&](auto e) { send_keys(k1_at, e, 1); });
+        __syncthreads();                       // (odd_one)
+        if (BITS == 16 && !as_it_is) put_values(v0_at, 0, key0, gone);
+        arrived();
         if constexpr (BITS == 8) {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) put_keys(more, e, 1);
+            spread_keys(0, power_at(k_byte, 0));
+            spread_values(0, power_at(v_byte, 0), key0, gone, as_it_is);
+            spread_keys(1, power_at(k_byte, second));
         }
     }
-    arrived();
     __syncthreads();
-    if (mine > 0) {
-        first_product(mine_at, Sa);
+    if (steps > 0 && busy) {
+        first_product(smem, Sa);
         top = largest(Sa);
     }
     __syncthreads();
     auto step = [&](int i, f16x (&S)[2], f16x (&N)[2], int stage) {
-        const bool more = i + 1 < mine;
-        const int iv = more ? i + 1 : i, ik = i + 2 < mine ? i + 2 : (mine > 0 ? mine - 1 : 0);         // (behind the last tile: it again, to where nobody reads)
-        bool as_it_is = false;
-        if (more) {
-            gone_next = gone_of(iv);
-            as_it_is = plain(tile_at(iv), gone_next);
-            if (BITS == 16 && !as_it_is) {
-#pragma unroll
-                for (int e = 0; e < PIECES; ++e) fetch_values(iv, e);
-                put_values(iv, gone_next);
-            }
-        }
-        if constexpr (BITS == 8) {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) fetch_values(iv, e);
-        }
-        // (tile iv is of the last look yet)
-        unsigned v_low[PIECES], v_high[PIECES];
-        if constexpr (BITS == 16) {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                const unsigned long long at = (unsigned long long)memory_of(a.pages_v, iv, e);
-                v_low[e] = __builtin_amdgcn_readfirstlane((unsigned)at);
-                v_high[e] = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
-            }
-        }
-        if (((i + 2) & 15) == 0 && i + 2 < mine) look(i + 2);
-        if (i < mine) {
-            const unsigned char* base = mine_at + stage * STAGE;
+        // tiles whose values and keys this step moves (behind the last tile: it again, to where nobody reads)
+        const bool more = i + 1 < steps;
+        const int iv = more ? i + 1 : i, ik = i + 2 < steps ? i + 2 : steps - 1, key_next = tile_at(iv);
+        const char* v_base = (const char*)a.pages_v + block_of(iv);
+        const float v_by = power_at(v_byte, iv);
+        gone_next = gone_of(iv);
+        const bool as_it_is = plain(key_next, gone_next);
+        if (BITS == 16 && more && !as_it_is) put_values(v_base, stage ^ 1, key_next, gone_next);
+        const unsigned v_to = more && (BITS == 8 || as_it_is) ? values_to(stage ^ 1) : aside;
+        if (((i + 2) & 15) == 0 && i + 2 < steps) look(i + 2);
+        const char* k_base = (const char*)a.pages_k + block_of(ik);
+        if (busy) {
+            const unsigned char* base = smem + stage * STAGE;
             const int key0 = tile_at(i);
             const bool whole = all && gone == 0 && key0 + KT <= wlow + 1 && (a.window == 0 || key0 > whigh - a.window || key0 + KT <= a.sinks);
             if (!whole) {
@@ -506,7 +504,7 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
             const float ref = m == -INFINITY ? 0.f : m;
             // One matrix instruction a slot, kept in this order: beside those of the next tile's scores (behind the last tile: of what lies there, unused) two weights of this one
             // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
-            const unsigned char* next = mine_at + (stage ^ 1) * STAGE;
+            const unsigned char* next = smem + (stage ^ 1) * STAGE;
             Frag kf[AHEAD], vf[AHEAD], p[4];
             auto read_k = [&](int x) { kf[x % AHEAD].q = *(const u4*)(next + k_at + x % 2 * BLOCK_OF_KEYS + 16 * ((2 * (x / 2)) ^ k_turn)); };
             auto read_v = [&](int x) {
@@ -528,24 +526,18 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
 #pragma unroll
             for (int x = 0; x < AHEAD; ++x) read_k(x);
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int x = 0; x < 2 * NK; ++x) {
-                const int b = x % 2, t = x / 2;
+            each_piece<2 * NK>([&](auto slot) {
+                constexpr int x = decltype(slot)::value, b = x % 2, t = x / 2;
                 if (t == 0) N[b] = f16x{};
                 N[b] = mfma32(kf[x % AHEAD].v, q[t].v, N[b]);
                 if (x + AHEAD < 2 * NK) read_k(x + AHEAD);
                 else read_v(x + AHEAD - 2 * NK);
-                if (x < PIECES) {
-                    if constexpr (BITS == 16) direct_keys(ik, x, stage);
-                    else fetch_keys(ik, x);
-                } else if (BITS == 16 && x < 2 * PIECES) {
-                    const int e = x - PIECES;
-                    memory_to_lds((const char*)((unsigned long long)v_high[e] << 32 | v_low[e]), v_off, as_it_is ? lds0 + (unsigned)((stage ^ 1) * STAGE + VALUES + key_at(e) * ROW) : aside);
-                }
+                if constexpr (x < PIECES) send_keys(k_base, slot, stage);
+                else if constexpr (x < 2 * PIECES) send_values(v_base, std::integral_constant<int, x - PIECES>{}, v_to);
 #pragma unroll
                 for (int w = 16 * x / (2 * NK); w < 16 * (x + 1) / (2 * NK); ++w) weights(w);
                 __builtin_amdgcn_sched_barrier(0);
-            }
+            });
 #pragma unroll
             for (int x = 0; x < 4 * ND; ++x) {
                 const int s = x / ND, d = x % ND;
@@ -555,16 +547,16 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
                 for (int e = 16 * x / (4 * ND); e < 16 * (x + 1) / (4 * ND); ++e) top = e == 0 ? fmaxf(N[0][0], N[1][0]) : fmaxf(fmaxf(top, N[0][e]), N[1][e]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+            each_piece<PIECES>([&](auto e) { send_keys(k_base, e, stage); });
+            each_piece<PIECES>([&](auto e) { send_values(v_base, e, v_to); });
         }
+        arrived();
         if constexpr (BITS == 8) {
-            if (i < mine) {
-#pragma unroll
-                for (int e = 0; e < PIECES; ++e) put_keys(ik, e, stage);
-            }
-            if (more) put_values(iv, gone_next);
+            spread_keys(stage, power_at(k_byte, ik));
+            if (more) spread_values(stage ^ 1, v_by, key_next, gone_next, as_it_is);
         }
         gone = gone_next;
-        arrived();
         __syncthreads();
     };
     for (int i = 0; i < steps; i += 2) {
@@ -576,41 +568,20 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
         l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
     }
 
-    // The teams' results meet in LDS, as rows of fp32 (all have passed the loop's last barrier).  This lane's elements: columns 32 d + 8 q + 4 half of row 32 rg + col; pieces of
+    // The results go to LDS, as rows of fp32 (all have passed the loop's last barrier).  This lane's elements: columns 32 d + 8 q + 4 half of row 32 wave + col; pieces of
     // 16 bytes change places within their row, so that the lanes that write at a time meet different banks.
     float* sum = (float*)smem;
-    const int mine_row = 32 * rg + col;
+    const int my_row = 32 * wave + col;
     auto piece_at = [&](int r, int c) { return sum + r * DIM + 4 * (c ^ (r & 15)); };
     if (half == 0) {
-        red_m[team][mine_row] = m;
-        red_l[team][mine_row] = l;
+        row_m[my_row] = m;
+        row_l[my_row] = l;
     }
-    if (team == TEAMS - 1) {
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *(f4*)piece_at(mine_row, 8 * d + 2 * e + half) = f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
-    }
+        for (int e = 0; e < 4; ++e) *(f4*)piece_at(my_row, 8 * d + 2 * e + half) = f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
     __syncthreads();
-    if constexpr (TEAMS == 2) {
-        if (team == 0) {
-            const float mo = red_m[1][mine_row], up = fmaxf(m, mo), f = factor(m, up), g = factor(mo, up), lo2 = red_l[1][mine_row];
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f4* at = (f4*)piece_at(mine_row, 8 * d + 2 * e + half);
-                    *at = *at * g + f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]} * f;
-                }
-            l = (m == -INFINITY ? l : l * f) + (mo == -INFINITY ? lo2 : lo2 * g);
-            m = up;
-            if (half == 0) {
-                red_m[0][mine_row] = m;
-                red_l[0][mine_row] = l;
-            }
-        }
-        __syncthreads();
-    }
     if (odd_one) {
         // Values that are not finite, in tiles of which not all rows see all: for the rows that see them, unless their score is -inf
         for (int e = threadIdx.x; e < TQ * (DIM / 4); e += THREADS) {
@@ -655,7 +626,7 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
     const int used = pair1 - pair0;
     if (parts > 1) {
         // a partial result: rows of (m, sum), then rows of DIM
-        float* part = a.parts + COUNTERS + (size_t)u.place * part_words(DIM, RG);
+        float* part = a.parts + COUNTERS + (size_t)u.place * part_words(DIM);
 #pragma unroll 4
         for (int e = 0; e < MY; ++e) {
             const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
@@ -665,7 +636,7 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
                 put2(part + 2 * TQ + 4 * at + 2, x[2], x[3]);
             }
         }
-        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, red_m[0][threadIdx.x], red_l[0][threadIdx.x]);
+        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, row_m[threadIdx.x], row_l[threadIdx.x]);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -675,8 +646,8 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
         }
         __syncthreads();
         if (!last) return;
-        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words(DIM, RG);
-        const size_t step_words = (size_t)a.kv * part_words(DIM, RG);
+        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words(DIM);
+        const size_t step_words = (size_t)a.kv * part_words(DIM);
         for (int e = 0; e < MY; ++e) {
             const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
             if (r2 >= used) break;
@@ -703,8 +674,8 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
             }
             *(f4*)piece_at(r2, c) = x;         // (its own thread reads it below)
             if (c == 0) {
-                red_m[0][r2] = mm;
-                red_l[0][r2] = ll;
+                row_m[r2] = mm;
+                row_l[r2] = ll;
             }
         }
         __syncthreads();
@@ -714,38 +685,25 @@ __global__ __launch_bounds__(64 * RG * teams_of(DIM, RG), RG * teams_of(DIM, RG)
         if (r2 >= used) break;
         const int pr = pair0 + r2, rw = pr / group;
         const size_t place = (size_t)(r.first + rw) * a.heads + u.h * group + (pr - rw * group);
-        const float ll = red_l[0][r2], f = vs / ll;
+        const float ll = row_l[r2], f = vs / ll;
         const f4 x = *(const f4*)piece_at(r2, c);
         h4 y;
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) y[q4] = (_Float16)(ll == 0.f ? 0.f : x[q4] * f);
         *(h4*)(a.out + place * DIM + 4 * c) = y;
-        if (c == 0 && a.lse) a.lse[place] = LN2 * (red_m[0][r2] + __log2f(ll));
+        if (c == 0 && a.lse) a.lse[place] = LN2 * (row_m[r2] + __log2f(ll));
     }
-}
-
-// From so many tiles of 256 pairs on (of all kv heads together) workgroups have such tiles
-constexpr long long MANY_TILES = 512;
-
-template <int DIM, int BITS, bool BLOCKS, int RG>
-hipError_t start(const PromptArgs& a, hipStream_t stream)
-{
-    constexpr int lds = lds_bytes<DIM, BITS, RG>();
-    const auto kern = prompt_kernel<DIM, BITS, BLOCKS, RG>;
-    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    kern<<<(unsigned)prompt_units(a.M, a.B, a.heads, a.kv, RG), 64 * RG * teams_of(DIM, RG), lds, stream>>>(a);
-    return hipGetLastError();
 }
 
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    // (heads of 256 leave no registers for two wavefronts a SIMD; of 64 in 8 bits, half of eight wavefronts would have nothing to move)
-    if constexpr (DIM == 128 || (DIM == 64 && BITS == 16)) {
-        if ((long long)a.M * a.heads >= 32 * MANY * MANY_TILES) return start<DIM, BITS, BLOCKS, MANY>(a, stream);
-    }
-    return start<DIM, BITS, BLOCKS, FEW>(a, stream);
+    constexpr int lds = lds_bytes<DIM, BITS>();
+    const auto kern = prompt_kernel<DIM, BITS, BLOCKS>;
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    kern<<<(unsigned)prompt_units(a.M, a.B, a.heads, a.kv), THREADS, lds, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <int DIM>
@@ -757,13 +715,12 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
 
 }  // namespace
 
-long long prompt_units(int M, int B, int heads, int kv, int rg)
+long long prompt_units(int M, int B, int heads, int kv)
 {
-    const long long group = heads / kv;
-    return (((long long)M * group + 32 * rg - 1) / (32 * rg) + B) * kv + 2 * want_of(rg);
+    return (((long long)M * (heads / kv) + TQ - 1) / TQ + B) * kv + MAX_PARTS;
 }
 
-size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words(dim, FEW)) * sizeof(float); }
+size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words(dim)) * sizeof(float); }
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream)
 {

@@ -120,7 +120,7 @@ struct PromptArgs {
     float scale;
 };
 size_t prompt_workspace_bytes(int dim);
-long long prompt_units(int M, int B, int heads, int kv, int rg = 4);   // workgroups of a launch at most, with tiles of 32 rg pairs
+long long prompt_units(int M, int B, int heads, int kv);               // workgroups of a launch at most
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream);
 
 struct AdapterArgs {
