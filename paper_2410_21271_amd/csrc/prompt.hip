@@ -68,7 +68,7 @@ __device__ __forceinline__ void memory_to_lds(const char* base, unsigned off, un
 }
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// A request as the kernel takes it: n tokens, rows [first, first + rows), tiles of its pairs, tiles of keys of its longest tile at most, parts a tile is cut into
+// A request as the kernel takes it: n tokens, rows [first, first + rows), tiles of its pairs, tiles of keys of its longest one at most
 struct Request {
     int n, first, rows, tiles, cost;
 };
@@ -92,88 +92,138 @@ __device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
     return r;
 }
 
-// What a workgroup does: part `part` of `parts` of a tile.  place: its partial results' number; of its tile's first part.
+// What a workgroup does: part `part` of `parts` of a tile of a request.  place: its partial results' number; first: of its tile's first part.
 struct Unit {
+    Request r;
     int b, h, tile, part, parts;
     int place, first;
 };
-// All threads.  Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have less
-// than 2 WANT parts.
-__device__ __forceinline__ bool unit_of(const PromptArgs& a, unsigned id, Unit& u, int* scratch)
+// Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have at most 2 WANT parts.
+// (The work is added up in floats, in one order: everyone finds the same share.)
+__device__ __forceinline__ int share_of(float work, int kv)
 {
-    constexpr int NW = THREADS / 64;
+    const float x = work * (float)kv * (1.f / WANT);
+    const int share = x < 1e9f ? (int)x + 1 : 0x7fffffff;
+    return share < LEAST_PART ? LEAST_PART : share;
+}
+__device__ __forceinline__ int parts_of(const Request& r, int share) { return r.cost <= share ? 1 : (int)((unsigned)(r.cost - 1) / (unsigned)share) + 1; }
+__device__ __forceinline__ Unit unit_in(const PromptArgs& a, const Request& r, int b, int parts, int local, int cut)
+{
+    Unit u;
+    u.r = r;
+    u.b = b;
+    u.parts = parts;
+    const int rest = (int)((unsigned)local / (unsigned)a.kv), tile = (int)((unsigned)rest / (unsigned)parts);
+    u.h = local - rest * a.kv;
+    u.part = rest - tile * parts;
+    u.tile = r.tiles - 1 - tile;               // (the last rows see most)
+    u.first = cut + tile * parts * a.kv + u.h;
+    u.place = u.first + u.part * a.kv;
+    return u;
+}
+// the sum over this lane and those before it
+template <typename T>
+__device__ __forceinline__ T scan(T v)
+{
+    auto add = [&](auto ctrl, auto rows) {
+        const int w = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+        v += __builtin_bit_cast(T, w);
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xF>{});         // the lane before, of the row of 16
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});         // the last of rows 0 and 2 to rows 1 and 3
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});         // the last of row 1 to rows 2 and 3
+    return v;
+}
+// Up to 64 requests: each wavefront for itself, a request a lane, read once.
+__device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u)
+{
+    const int lane = threadIdx.x & 63;
+    Request r = request_of(a, lane < a.B ? lane : a.B - 1);
+    if (lane >= a.B) r.tiles = 0;
+    const int share = share_of(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)), a.kv);
+    const int parts = parts_of(r, share), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
+    const int v = scan(units), c = scan(cut);
+    const unsigned long long mine = __ballot(id >= v - units && id < v);
+    if (mine == 0) return false;
+    const int b = __builtin_ctzll(mine);
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, b); };
+    Request q;
+    q.n = of(r.n);
+    q.first = of(r.first);
+    q.rows = of(r.rows);
+    q.tiles = of(r.tiles);
+    q.cost = of(r.cost);
+    u = unit_in(a, q, b, of(parts), id - of(v - units), of(c - cut));
+    return true;
+}
+// Any number of them: all threads, a request each at a time.
+__device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, int* scratch)
+{
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    unsigned long long* sums = (unsigned long long*)scratch;                    // NW
-    int* found = scratch + 2 * NW;                                              // b, id within the request, parts before
-    int* totals = found + 4;                                                    // 2 NW
-    unsigned long long work = 0;
+    float* sums = (float*)scratch;                                              // RG
+    int* found = scratch + RG;                                                  // b, id within the request, parts before
+    int* totals = found + 4;                                                    // 2 RG
+    float work = 0.f;
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
         const Request r = request_of(a, b);
-        work += (unsigned long long)r.tiles * r.cost;
+        work += (float)r.tiles * (float)r.cost;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) work += __shfl_xor(work, o, 64);
-    if (lane == 0) sums[wave] = work;
+    work = scan(work);
+    if (lane == 63) sums[wave] = work;
     if (threadIdx.x == 0) found[0] = -1;
     __syncthreads();
-    work = 0;
+    work = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) work += sums[w];
-    unsigned long long share = (work * (unsigned)a.kv + WANT - 1) / WANT;
-    share = share < LEAST_PART ? LEAST_PART : share;
-    unsigned before = 0, cut_before = 0;
+    for (int w = 0; w < RG; ++w) work += sums[w];
+    const int share = share_of(work, a.kv);
+    int before = 0, cut_before = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
-        unsigned units = 0, cut = 0;
+        int units = 0, cut = 0;
         if (b < a.B) {
             const Request r = request_of(a, b);
-            const unsigned parts = r.cost <= share ? 1u : (unsigned)((r.cost + share - 1) / share);
-            units = (unsigned)r.tiles * parts * (unsigned)a.kv;
+            const int parts = parts_of(r, share);
+            units = r.tiles * parts * a.kv;
             cut = parts > 1 ? units : 0;
         }
-        unsigned v = units, c = cut;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const unsigned x = __shfl_up(v, o, 64), y = __shfl_up(c, o, 64);
-            v += lane >= o ? x : 0;
-            c += lane >= o ? y : 0;
-        }
+        int v = scan(units), c = scan(cut);
         if (lane == 63) {
-            totals[2 * wave] = (int)v;
-            totals[2 * wave + 1] = (int)c;
+            totals[2 * wave] = v;
+            totals[2 * wave + 1] = c;
         }
         __syncthreads();
-        unsigned sum = 0, cut_sum = 0;
+        int sum = 0, cut_sum = 0;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            v += w < wave ? (unsigned)totals[2 * w] : 0;
-            c += w < wave ? (unsigned)totals[2 * w + 1] : 0;
-            sum += (unsigned)totals[2 * w];
-            cut_sum += (unsigned)totals[2 * w + 1];
+        for (int w = 0; w < RG; ++w) {
+            v += w < wave ? totals[2 * w] : 0;
+            c += w < wave ? totals[2 * w + 1] : 0;
+            sum += totals[2 * w];
+            cut_sum += totals[2 * w + 1];
         }
         v += before;
         c += cut_before;
         if (id >= v - units && id < v) {
             found[0] = b;
-            found[1] = (int)(id - (v - units));
-            found[2] = (int)(c - cut);
+            found[1] = id - (v - units);
+            found[2] = c - cut;
         }
         before += sum;
         cut_before += cut_sum;
         __syncthreads();
         if (id < before) break;
     }
-    u.b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (u.b < 0) return false;
-    const Request r = request_of(a, u.b);
-    const int local = __builtin_amdgcn_readfirstlane(found[1]), cut = __builtin_amdgcn_readfirstlane(found[2]);
-    u.parts = r.cost <= share ? 1 : (int)((r.cost + share - 1) / share);
-    const int rest = local / a.kv, tile = rest / u.parts;
-    u.h = local - rest * a.kv;
-    u.part = rest - tile * u.parts;
-    u.tile = r.tiles - 1 - tile;               // (the last rows see most)
-    u.first = cut + (tile * u.parts) * a.kv + u.h;
-    u.place = u.first + u.part * a.kv;
+    const int b = __builtin_amdgcn_readfirstlane(found[0]);
+    if (b < 0) return false;
+    Request r = request_of(a, b);
+    r.n = __builtin_amdgcn_readfirstlane(r.n);
+    r.first = __builtin_amdgcn_readfirstlane(r.first);
+    r.rows = __builtin_amdgcn_readfirstlane(r.rows);
+    r.tiles = __builtin_amdgcn_readfirstlane(r.tiles);
+    r.cost = __builtin_amdgcn_readfirstlane(r.cost);
+    u = unit_in(a, r, b, parts_of(r, share), __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[2]));
     return true;
 }
 
@@ -230,17 +280,14 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     auto v_turn_of = [](int key) { return 4 * (DIM == 64 ? key >> 1 & 1 : key & 3); };
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    __shared__ int scratch[2 * 8 + 4 + 2 * 8];
+    __shared__ int scratch[RG + 4 + 2 * RG];
     __shared__ int odd_one;                    // some value that not all rows see is not finite
     __shared__ int last;
     __shared__ float row_m[TQ], row_l[TQ];
 
     Unit u;
-    if (!unit_of(a, blockIdx.x, u, scratch)) return;
-    Request r = request_of(a, u.b);
-    r.n = __builtin_amdgcn_readfirstlane(r.n);
-    r.first = __builtin_amdgcn_readfirstlane(r.first);
-    r.rows = __builtin_amdgcn_readfirstlane(r.rows);
+    if (!(a.B <= 64 ? unit_of_few(a, (int)blockIdx.x, u) : unit_of(a, (int)blockIdx.x, u, scratch))) return;
+    const Request r = u.r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int group = a.heads / a.kv, pairs = r.rows * group, from = r.n - r.rows;             // from: position of row 0 (below 0: rows that see nothing)
