@@ -30,13 +30,18 @@
 namespace eora {
 namespace {
 
-constexpr int RG = 4, THREADS = 64 * RG, TQ = 32 * RG;           // wavefronts; pairs of a tile
-constexpr int KT = 64;                         // keys of a tile
+constexpr int RG = 4, THREADS = 64 * RG;       // wavefronts of a workgroup
+// Pairs and keys of a tile, and keys of a part of it at least: of many rows (a wavefront a quarter of the pairs), and of few (a wavefront every fourth tile of keys)
+struct Wide {
+    static constexpr int TQ = 128, KT = 64, LEAST_PART = 4;
+};
+struct Narrow {
+    static constexpr int TQ = 32, KT = 32, LEAST_PART = 16;
+};
 constexpr int CUS = 256;
-// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see unit_of().
+// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see share_of()
 constexpr int WANT = 2 * CUS;
 constexpr int MAX_PARTS = 2 * WANT;
-constexpr int LEAST_PART = 4;                  // tiles of keys of a part
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr float RAISE = 4.f, LOWER = 11.f;
@@ -72,8 +77,10 @@ __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::
 struct Request {
     int n, first, rows, tiles, cost;
 };
+template <typename SHAPE>
 __device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
 {
+    constexpr int TQ = SHAPE::TQ, KT = SHAPE::KT;
     Request r;
     const int most = a.width * a.page, group = a.heads / a.kv;
     int n = a.lengths[b], s = a.starts[b], e = a.starts[b + 1];
@@ -100,11 +107,12 @@ struct Unit {
 };
 // Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have at most 2 WANT parts.
 // (The work is added up in floats, in one order: everyone finds the same share.)
+template <typename SHAPE>
 __device__ __forceinline__ int share_of(float work, int kv)
 {
     const float x = work * (float)kv * (1.f / WANT);
     const int share = x < 1e9f ? (int)x + 1 : 0x7fffffff;
-    return share < LEAST_PART ? LEAST_PART : share;
+    return share < SHAPE::LEAST_PART ? SHAPE::LEAST_PART : share;
 }
 __device__ __forceinline__ int parts_of(const Request& r, int share) { return r.cost <= share ? 1 : (int)((unsigned)(r.cost - 1) / (unsigned)share) + 1; }
 __device__ __forceinline__ Unit unit_in(const PromptArgs& a, const Request& r, int b, int parts, int local, int cut)
@@ -138,12 +146,13 @@ __device__ __forceinline__ T scan(T v)
     return v;
 }
 // Up to 64 requests: each wavefront for itself, a request a lane, read once.
+template <typename SHAPE>
 __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u)
 {
     const int lane = threadIdx.x & 63;
-    Request r = request_of(a, lane < a.B ? lane : a.B - 1);
+    Request r = request_of<SHAPE>(a, lane < a.B ? lane : a.B - 1);
     if (lane >= a.B) r.tiles = 0;
-    const int share = share_of(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)), a.kv);
+    const int share = share_of<SHAPE>(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)), a.kv);
     const int parts = parts_of(r, share), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
     const int v = scan(units), c = scan(cut);
     const unsigned long long mine = __ballot(id >= v - units && id < v);
@@ -160,6 +169,7 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
     return true;
 }
 // Any number of them: all threads, a request each at a time.
+template <typename SHAPE>
 __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, int* scratch)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -168,7 +178,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     int* totals = found + 4;                                                    // 2 RG
     float work = 0.f;
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
-        const Request r = request_of(a, b);
+        const Request r = request_of<SHAPE>(a, b);
         work += (float)r.tiles * (float)r.cost;
     }
     work = scan(work);
@@ -178,13 +188,13 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     work = 0.f;
 #pragma unroll
     for (int w = 0; w < RG; ++w) work += sums[w];
-    const int share = share_of(work, a.kv);
+    const int share = share_of<SHAPE>(work, a.kv);
     int before = 0, cut_before = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int units = 0, cut = 0;
         if (b < a.B) {
-            const Request r = request_of(a, b);
+            const Request r = request_of<SHAPE>(a, b);
             const int parts = parts_of(r, share);
             units = r.tiles * parts * a.kv;
             cut = parts > 1 ? units : 0;
@@ -217,7 +227,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     }
     const int b = __builtin_amdgcn_readfirstlane(found[0]);
     if (b < 0) return false;
-    Request r = request_of(a, b);
+    Request r = request_of<SHAPE>(a, b);
     r.n = __builtin_amdgcn_readfirstlane(r.n);
     r.first = __builtin_amdgcn_readfirstlane(r.first);
     r.rows = __builtin_amdgcn_readfirstlane(r.rows);
@@ -247,18 +257,260 @@ template <int N, typename F>
 __device__ __forceinline__ void each_piece(const F& f) { each_of<N>(f, std::make_integer_sequence<int, N>{}); }
 
 // words of a partial result: (m, sum) and O of each pair
-constexpr size_t part_words(int dim) { return (size_t)TQ * (dim + 2); }
+template <typename SHAPE>
+constexpr size_t part_words(int dim) { return (size_t)SHAPE::TQ * (dim + 2); }
 
-// K in LDS: rows in groups of 1 KiB, as they come from memory, with a gap behind each group
-constexpr int k_group(int dim) { return 512 / dim; }
-constexpr int K_GAP = 64, K_GAP_256 = 32;
-constexpr int k_pitch(int dim) { return 1024 + (dim == 256 ? K_GAP_256 : K_GAP); }
-constexpr int stage_bytes(int dim) { return KT / k_group(dim) * k_pitch(dim) + KT * 2 * dim; }
-template <int DIM, int BITS>
-constexpr int lds_bytes()
+// A tile's part in LDS, fp16: K's rows in groups of 1 KiB, as they come from memory, with a gap behind each group; then V's rows.  Pieces of 16 bytes change places in the row of a key, so that the
+// lanes that read at a time meet different banks: 16 keys' pieces of the same columns; two units of 32 bytes of four keys.
+template <int DIM, int KT>
+struct Stage {
+    static constexpr int ROW = 2 * DIM, GROUP = 512 / DIM, PITCH = 1024 + (DIM == 256 ? 32 : 64);
+    static constexpr int VALUES = KT / GROUP * PITCH, BYTES = VALUES + KT * ROW;
+    static constexpr int BLOCK_OF_KEYS = 32 / GROUP * PITCH;
+    __device__ static __forceinline__ int k_turn(int key) { return DIM == 64 ? key >> 1 & 3 : (DIM == 128 ? key & 3 : key & 1); }
+    __device__ static __forceinline__ int v_turn(int key) { return 4 * (DIM == 64 ? key >> 1 & 1 : key & 3); }
+    __device__ static __forceinline__ int k_place(int key, int piece) { return key / GROUP * PITCH + key % GROUP * ROW + 16 * (piece ^ k_turn(key)); }
+    __device__ static __forceinline__ int v_place(int key, int piece) { return VALUES + key * ROW + 16 * (piece ^ v_turn(key)); }
+    // where a lane reads: K, row lane % 32: piece 2 t + lane / 32; V, transposed: rows 4 (lane / 32) + lane % 16 / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of 32
+    int k_at, k_way, v_at, v_way;
+    __device__ __forceinline__ explicit Stage(int lane)
+    {
+        const int col = lane & 31, half = lane >> 5, v_key = 4 * half + (lane & 15) / 4;
+        k_at = col / GROUP * PITCH + col % GROUP * ROW;
+        k_way = half ^ k_turn(col);
+        v_at = VALUES + v_key * ROW + 8 * (lane & 3);
+        v_way = (lane >> 4 & 1) ^ (v_turn(v_key) / 2);
+    }
+    // columns 16 t .. + 15 of keys 32 b .. + 31; keys 16 s .. + 15 of columns 32 d .. + 31
+    __device__ __forceinline__ void keys(const unsigned char* base, int b, int t, Frag& f) const { f.q = *(const u4*)(base + k_at + b * BLOCK_OF_KEYS + 16 * ((2 * t) ^ k_way)); }
+    __device__ __forceinline__ void values(const unsigned char* base, int s, int d, Frag& f) const
+    {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)(base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_way)));
+            __builtin_memcpy(&f.u[2 * e], &w, 8);
+        }
+    }
+};
+// 16 codes, times a power of two
+__device__ __forceinline__ void spread(const u4& w, float scale, Frag (&f)[2])
 {
-    constexpr int loop = 2 * stage_bytes(DIM) + BLOCK_TOKENS * DIM * BITS / 8, end = TQ * DIM * 4;
-    return loop > end ? loop : end;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[e / 2].p[2 * (e % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, false);
+        f[e / 2].p[2 * (e % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, true);
+    }
+}
+
+// A tile of pairs, and which of the keys its rows see
+template <typename SHAPE>
+struct Tile {
+    static constexpr int TQ = SHAPE::TQ, KT = SHAPE::KT;
+    Unit u;
+    int group, pair0, pair1;                   // its pairs: [pair0, pair1)
+    int from, low, high;                       // positions of the request's row 0 (below 0: rows that see nothing), of the tile's first row and of its last
+    int lo, hi, sinks, first, head;            // tokens that some row sees: [lo, hi) and those before `sinks`; tiles of keys: those from `first` on, behind `head` of the first
+    int parts, k0, k1;                         // tiles [k0, k1) of them are this workgroup's
+    const int* table;
+    __device__ __forceinline__ bool find(const PromptArgs& a, int id, int* scratch)
+    {
+        if (!(a.B <= 64 ? unit_of_few<SHAPE>(a, id, u) : unit_of<SHAPE>(a, id, u, scratch))) return false;
+        group = a.heads / a.kv;
+        const int pairs = u.r.rows * group;
+        from = u.r.n - u.r.rows;
+        pair0 = u.tile * TQ;
+        pair1 = pair0 + TQ < pairs ? pair0 + TQ : pairs;
+        low = from + pair0 / group;
+        high = from + (pair1 - 1) / group;
+        hi = high + 1 < 0 ? 0 : high + 1;
+        lo = a.window > 0 && low - a.window + 1 > 0 ? low - a.window + 1 : 0;
+        if (lo <= a.sinks) lo = 0;
+        sinks = lo > 0 ? a.sinks : 0;
+        first = lo / KT;
+        head = (sinks + KT - 1) / KT;
+        head = head < first ? head : first;
+        int tiles = (hi + KT - 1) / KT - first + head;
+        tiles = tiles > 0 ? tiles : 0;
+        parts = (tiles + SHAPE::LEAST_PART - 1) / SHAPE::LEAST_PART;
+        parts = parts < 1 ? 1 : (parts < u.parts ? parts : u.parts);
+        if (u.part >= parts) return false;
+        k0 = (int)((long long)tiles * u.part / parts);
+        k1 = (int)((long long)tiles * (u.part + 1) / parts);
+        table = a.table + (size_t)u.b * a.width;
+        return true;
+    }
+    __device__ __forceinline__ int key_of(int i) const { return (i < head ? i : i - head + first) * KT; }
+    // the block of 16 tokens that a key (a multiple of 16) begins: page, head and place in one number; -1: no page
+    __device__ __forceinline__ int block_at(const PromptArgs& a, int key) const
+    {
+        const int p = key / a.page, page = table[p];
+        return (unsigned)page < (unsigned)a.n_pages ? (page * a.kv + u.h) * (a.page / BLOCK_TOKENS) + (key - p * a.page) / BLOCK_TOKENS : -1;
+    }
+    __device__ __forceinline__ unsigned gone_at(const PromptArgs& a, int key0) const
+    {
+        unsigned gone = 0;
+        for (int g = 0; g < KT / BLOCK_TOKENS; ++g) gone |= (unsigned)(key0 + BLOCK_TOKENS * g < hi && block_at(a, key0 + BLOCK_TOKENS * g) < 0) << g;
+        return gone;
+    }
+    // whether a tile's values can go to LDS as they are: all rows see all of its tokens
+    __device__ __forceinline__ bool plain(const PromptArgs& a, int key0, unsigned gone) const
+    {
+        return gone == 0 && key0 + KT <= low + 1 && (a.window == 0 || key0 > high - a.window || key0 + KT <= a.sinks);
+    }
+    // Eight values of a token: one that no row sees becomes zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
+    __device__ __forceinline__ void clean(Frag& f, int at, bool gone, int& odd_one) const
+    {
+        const bool seen = at < hi && (at >= lo || at < sinks) && !gone;
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = seen ? f.u[e] : 0u;
+            const uint32_t low_half = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, high_half = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
+            odd |= (low_half | high_half) != 0;
+            f.u[e] = x & ~(low_half | high_half);
+        }
+        if (odd) odd_one = 1;
+    }
+};
+
+// Where pieces of four columns of the results lie in LDS, rows of fp32: they change places within their row, so that the lanes that write at a time meet different banks
+template <int DIM>
+__device__ __forceinline__ float* piece_at(float* sum, int row, int c) { return sum + row * DIM + 4 * (c ^ (row & 15)); }
+
+// Values that are not finite, in tiles of which not all rows see all: for the rows that see them, unless their score is -inf
+template <int DIM, int BITS, typename SHAPE>
+__device__ __forceinline__ void add_odd(const PromptArgs& a, const Tile<SHAPE>& t, float scale, float* sum)
+{
+    for (int e = threadIdx.x; e < SHAPE::TQ * (DIM / 4); e += THREADS) {
+        const int r = e / (DIM / 4), c = e % (DIM / 4), pair = t.pair0 + r;
+        if (pair >= t.pair1) continue;
+        const int row = pair / t.group, pos = t.from + row, head = t.u.h * t.group + pair - row * t.group;
+        f4 add = {0.f, 0.f, 0.f, 0.f};
+        for (int i = t.k0; i < t.k1; ++i) {
+            const int key0 = t.key_of(i);
+            if (t.plain(a, key0, t.gone_at(a, key0))) continue;
+            for (int key = key0; key < key0 + SHAPE::KT && key <= pos; ++key) {
+                if (!(a.window == 0 || key > pos - a.window || key < a.sinks)) continue;
+                const int block = t.block_at(a, key & ~(BLOCK_TOKENS - 1));
+                if (block < 0) continue;
+                const size_t at = ((size_t)(unsigned)block * BLOCK_TOKENS + key % BLOCK_TOKENS) * DIM;
+                bool any = false;
+                float v[4];
+                for (int k = 0; k < 4; ++k) {
+                    if constexpr (BITS == 16) v[k] = (float)((const _Float16*)a.pages_v)[at + 4 * c + k];
+                    else v[k] = (((const uint8_t*)a.pages_v)[at + 4 * c + k] & 127) == 127 ? __builtin_nanf("") : 0.f;
+                    any |= !(fabsf(v[k]) < INFINITY);
+                }
+                if (!any) continue;
+                if constexpr (BITS == 16) {
+                    const _Float16 *x = a.q + (size_t)(t.u.r.first + row) * a.q_stride + (size_t)head * DIM, *y = (const _Float16*)a.pages_k + at;
+                    float score = 0.f;
+                    for (int k = 0; k < DIM; ++k) score += (float)x[k] * (float)y[k];
+                    if (score * scale == -INFINITY) continue;
+                }
+                for (int k = 0; k < 4; ++k) add[k] += fabsf(v[k]) < INFINITY ? 0.f : v[k];
+            }
+        }
+        *(f4*)piece_at<DIM>(sum, r, c) += add;
+    }
+}
+
+// The results of a tile, or of a part of one, from LDS (O's rows, (m, sum) of each) to where they belong.  All threads, behind a barrier.
+template <int DIM, typename SHAPE>
+__device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t, float vs, float* sum, float* row_m, float* row_l, int& last)
+{
+    constexpr int TQ = SHAPE::TQ, MY = TQ * (DIM / 4) / THREADS;                 // pieces of four columns: thread after thread along the rows
+    constexpr size_t WORDS = part_words<SHAPE>(DIM);
+    const int used = t.pair1 - t.pair0, parts = t.parts;
+    if (parts > 1) {
+        // a partial result: rows of (m, sum), then rows of DIM
+        float* part = a.parts + COUNTERS + (size_t)t.u.place * WORDS;
+#pragma unroll 4
+        for (int e = 0; e < MY; ++e) {
+            const int at = threadIdx.x + e * THREADS, r = at / (DIM / 4), c = at % (DIM / 4);
+            if (r < used) {
+                const f4 x = *(const f4*)piece_at<DIM>(sum, r, c);
+                put2(part + 2 * TQ + 4 * at, x[0], x[1]);
+                put2(part + 2 * TQ + 4 * at + 2, x[2], x[3]);
+            }
+        }
+        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, row_m[threadIdx.x], row_l[threadIdx.x]);
+        arrived();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            unsigned* counter = (unsigned*)a.parts + t.u.first;
+            last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (unsigned)parts;
+            if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last) return;
+        const float* src = a.parts + COUNTERS + (size_t)t.u.first * WORDS;
+        const size_t step_words = (size_t)a.kv * WORDS;
+        for (int e = 0; e < MY; ++e) {
+            const int at = threadIdx.x + e * THREADS, r = at / (DIM / 4), c = at % (DIM / 4);
+            if (r >= used) break;
+            float m = -INFINITY, l = 0.f;
+            f4 x = {0.f, 0.f, 0.f, 0.f};
+            // (four at a time on their way)
+            for (int c0 = 0; c0 < parts; c0 += 4) {
+                float2 ml[4], y[4][2];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float* one = src + (size_t)(c0 + k < parts ? c0 + k : parts - 1) * step_words;
+                    ml[k] = get2(one + 2 * r);
+                    y[k][0] = get2(one + 2 * TQ + 4 * at);
+                    y[k][1] = get2(one + 2 * TQ + 4 * at + 2);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (c0 + k >= parts) break;
+                    const float up = fmaxf(m, ml[k].x), f = factor(m, up), g = factor(ml[k].x, up);
+                    l = (m == -INFINITY ? l : l * f) + (ml[k].x == -INFINITY ? ml[k].y : ml[k].y * g);
+                    m = up;
+                    x = x * f + f4{y[k][0].x, y[k][0].y, y[k][1].x, y[k][1].y} * g;
+                }
+            }
+            *(f4*)piece_at<DIM>(sum, r, c) = x;                                  // (its own thread reads it below)
+            if (c == 0) {
+                row_m[r] = m;
+                row_l[r] = l;
+            }
+        }
+        __syncthreads();
+    }
+    for (int e = 0; e < MY; ++e) {
+        const int at = threadIdx.x + e * THREADS, r = at / (DIM / 4), c = at % (DIM / 4);
+        if (r >= used) break;
+        const int pair = t.pair0 + r, row = pair / t.group;
+        const size_t place = (size_t)(t.u.r.first + row) * a.heads + t.u.h * t.group + (pair - row * t.group);
+        const float l = row_l[r], f = vs / l;
+        const f4 x = *(const f4*)piece_at<DIM>(sum, r, c);
+        h4 y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = (_Float16)(l == 0.f ? 0.f : x[k] * f);
+        *(h4*)(a.out + place * DIM + 4 * c) = y;
+        if (c == 0 && a.lse) a.lse[place] = LN2 * (row_m[r] + __log2f(l));
+    }
+}
+
+// The scale of the scores in powers of two, and a lane's operand of q: pair `pair` of the tile's, its sign that of the scale
+template <int DIM>
+__device__ __forceinline__ void load_q(const PromptArgs& a, const Unit& u, int group, int pair, bool there, int half, float scale, Frag (&q)[DIM / 16])
+{
+    const int row = there ? pair / group : 0, head = u.h * group + (there ? pair - row * group : 0);
+    const _Float16* at = a.q + (size_t)(u.r.first + row) * a.q_stride + (size_t)head * DIM + 8 * half;
+    const uint32_t sign = scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int t = 0; t < DIM / 16; ++t) {
+        const u4 w = *(const u4*)(at + 16 * t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[t].u[e] = there ? w[e] ^ sign : 0u;
+    }
+}
+__device__ __forceinline__ float both_halves(float v)
+{
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
 
 // Workgroups a compute unit has at a time, as registers and LDS allow
@@ -267,17 +519,13 @@ constexpr int residents(int dim) { return dim == 256 ? 1 : 2; }
 template <int DIM, int BITS, bool BLOCKS>
 __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const PromptArgs a)
 {
-    constexpr int ROW = 2 * DIM;               // bytes of a row in LDS
-    constexpr int GROUP = k_group(DIM), PITCH = k_pitch(DIM);
-    constexpr int STAGE = stage_bytes(DIM), VALUES = STAGE - KT * ROW;            // keys, then values
+    constexpr int TQ = Wide::TQ, KT = Wide::KT;
+    typedef Stage<DIM, KT> St;
+    constexpr int ROW = St::ROW, PITCH = St::PITCH, STAGE = St::BYTES, VALUES = St::VALUES;
     constexpr int NK = DIM / 16, ND = DIM / 32;                   // k-steps of the first product, blocks of O^T
     constexpr int BYTES = DIM * BITS / 8;      // of a row in memory
     constexpr int PIECES = BLOCK_TOKENS * BYTES / 1024;           // KiB of a wavefront's 16 keys (or values) of a tile
     constexpr int AHEAD = 4;                   // matrix instructions between an operand's read and its use
-    // How pieces of 16 bytes change places in the row of a key, so that the lanes that read at a time meet different banks: 16 keys' pieces of the same columns; two units of 32 bytes
-    // of four keys
-    auto k_turn_of = [](int key) { return DIM == 64 ? key >> 1 & 3 : (DIM == 128 ? key & 3 : key & 1); };
-    auto v_turn_of = [](int key) { return 4 * (DIM == 64 ? key >> 1 & 1 : key & 3); };
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ int scratch[RG + 4 + 2 * RG];
@@ -285,59 +533,26 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     __shared__ int last;
     __shared__ float row_m[TQ], row_l[TQ];
 
-    Unit u;
-    if (!(a.B <= 64 ? unit_of_few(a, (int)blockIdx.x, u) : unit_of(a, (int)blockIdx.x, u, scratch))) return;
-    const Request r = u.r;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 31, half = lane >> 5;
-    const int group = a.heads / a.kv, pairs = r.rows * group, from = r.n - r.rows;             // from: position of row 0 (below 0: rows that see nothing)
-    const int pair0 = u.tile * TQ, pair1 = pair0 + TQ < pairs ? pair0 + TQ : pairs;
-
-    // tiles of keys that some row of the tile sees
-    const int low = from + pair0 / group, high = from + (pair1 - 1) / group;                   // positions of its first and last row
-    const int hi = high + 1 < 0 ? 0 : high + 1;
-    int lo = a.window > 0 && low - a.window + 1 > 0 ? low - a.window + 1 : 0;
-    if (lo <= a.sinks) lo = 0;
-    const int sinks = lo > 0 ? a.sinks : 0;
-    const int first = lo / KT;
-    int head = (sinks + KT - 1) / KT;
-    head = head < first ? head : first;
-    const int tiles = (hi + KT - 1) / KT - first + head > 0 ? (hi + KT - 1) / KT - first + head : 0;
-    auto key_of = [&](int i) { return (i < head ? i : i - head + first) * KT; };
-    int parts = (tiles + LEAST_PART - 1) / LEAST_PART;
-    parts = parts < 1 ? 1 : (parts < u.parts ? parts : u.parts);
-    if (u.part >= parts) return;
-    const int k0 = (int)((long long)tiles * u.part / parts), k1 = (int)((long long)tiles * (u.part + 1) / parts);
-    const int steps = k1 - k0;
+    Tile<Wide> tile;
+    if (!tile.find(a, (int)blockIdx.x, scratch)) return;
+    const Unit& u = tile.u;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int steps = tile.k1 - tile.k0;
 
     // this lane's pair, and the positions that this wavefront's pairs have
-    const int pair = pair0 + 32 * wave + col;
-    const bool there = pair < pair1;
-    const int row = there ? pair / group : 0, qh = u.h * group + (there ? pair - row * group : 0);
-    const int pos = there ? from + row : -1;
-    const int w0 = pair0 + 32 * wave, w1 = w0 + 32 < pair1 ? w0 + 32 : pair1;                    // (w1 <= w0: no pair)
-    const int wlow = from + w0 / group, whigh = w1 > w0 ? from + (w1 - 1) / group : -1;
-    const bool all = w1 - w0 == 32;
+    const int w0 = tile.pair0 + 32 * wave, w1 = w0 + 32 < tile.pair1 ? w0 + 32 : tile.pair1;         // (w1 <= w0: no pair)
+    const int wlow = tile.from + w0 / tile.group, whigh = w1 > w0 ? tile.from + (w1 - 1) / tile.group : -1;
+    const bool all = w1 - w0 == 32, there = w0 + col < tile.pair1;
+    const int pos = there ? tile.from + (w0 + col) / tile.group : -1;
 
     // Blocks of 16 tokens of the next 64 groups of 16 keys: lane 4 i + g has where that of group g of its tile i begins in the cache, in bytes (0: no page, or no key that a
     // row sees: those are in `lost`), and its scales
     unsigned off_low = 0, off_high = 0;
     unsigned k_byte = 0, v_byte = 0;
     unsigned long long lost = 0;
-    const int* table = a.table + (size_t)u.b * a.width;
-    const int per_page = a.page / BLOCK_TOKENS;
-    auto block_at = [&](int key) {
-        const int p = key / a.page, page = table[p];
-        return (unsigned)page < (unsigned)a.n_pages ? (page * a.kv + u.h) * per_page + (key - p * a.page) / BLOCK_TOKENS : -1;
-    };
-    auto gone_at = [&](int key0) {
-        unsigned gone = 0;
-        for (int g = 0; g < 4; ++g) gone |= (unsigned)(key0 + 16 * g < hi && block_at(key0 + 16 * g) < 0) << g;
-        return gone;
-    };
-    auto tile_at = [&](int i) { return key_of(k0 + i); };
+    auto tile_at = [&](int i) { return tile.key_of(tile.k0 + i); };
     auto look = [&](int i0) {
-        const int i = i0 + (lane >> 2), key = i < steps ? tile_at(i) + 16 * (lane & 3) : hi, block = key < hi ? block_at(key) : -1;
+        const int i = i0 + (lane >> 2), key = i < steps ? tile_at(i) + 16 * (lane & 3) : tile.hi, block = key < tile.hi ? tile.block_at(a, key) : -1;
         lost = __ballot(block < 0);
         const size_t off = (size_t)(unsigned)(block < 0 ? 0 : block) * (BLOCK_TOKENS * BYTES);
         off_low = (unsigned)off;
@@ -348,9 +563,6 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
         }
     };
     auto gone_of = [&](int i) { return (unsigned)(lost >> (4 * (i & 15))) & 15u; };
-    // Whether a tile's values can go to LDS as they are: all rows see all of its tokens
-    auto plain = [&](int key0, unsigned gone) { return gone == 0 && key0 + KT <= low + 1 && (a.window == 0 || key0 > high - a.window || key0 + KT <= a.sinks); };
-
     // A wavefront moves the tile's group of 16 keys that has its number, a KiB at a time: this lane's row of the KiB, and its piece of 16 bytes of it
     constexpr int PR = BYTES / 16, ROWS = 64 / PR;
     const int lrow = lane / PR, lpiece = lane % PR;
@@ -360,10 +572,10 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     };
     auto power_at = [&](unsigned bytes, int i) { return BLOCKS ? power_of(__builtin_amdgcn_readlane(bytes, 4 * (i & 15) + wave)) : 1.f; };
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, aside = lds0 + 2 * STAGE;      // (what nobody reads)
-    constexpr int K_MINE = BLOCK_TOKENS / GROUP * PITCH, V_MINE = BLOCK_TOKENS * ROW;           // a wavefront's part of a stage
+    constexpr int K_MINE = BLOCK_TOKENS / St::GROUP * PITCH, V_MINE = BLOCK_TOKENS * ROW;           // a wavefront's part of a stage
     // fp16: pieces change places on the way, as the addresses say.  8 bits: codes as they are, at the beginning of the wavefront's part; it spreads them out there itself
-    const unsigned linear = 16u * lane, k_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ k_turn_of(lrow))) : linear;
-    const unsigned v_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ v_turn_of(lrow))) : linear;
+    const unsigned linear = 16u * lane, k_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ St::k_turn(lrow))) : linear;
+    const unsigned v_off = BITS == 16 ? (unsigned)(lrow * ROW + 16 * (lpiece ^ St::v_turn(lrow))) : linear;
     auto send_keys = [&](const char* base, auto piece, int stage) {
         constexpr int e = decltype(piece)::value, far = e / 4 * 4096, off = e % 4 * 1024;
         memory_to_lds<off>(base + far, k_off, lds0 + (unsigned)(stage * STAGE + wave * K_MINE + (BITS == 16 ? e * PITCH - off : far)));
@@ -373,15 +585,6 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
         memory_to_lds<off>(base + far, BITS == 16 && DIM == 256 && e % 2 ? v_off ^ 128u : v_off, to + far);
     };
     auto values_to = [&](int stage) { return lds0 + (unsigned)(stage * STAGE + VALUES + wave * V_MINE); };
-    auto codes = [](const u4& w, float scale, Frag (&f)[2]) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[e / 2].p[2 * (e % 2)] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, false);
-            f[e / 2].p[2 * (e % 2) + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], scale, true);
-        }
-    };
-    auto k_place = [&](int key, int piece) { return key / GROUP * PITCH + key % GROUP * ROW + 16 * (piece ^ k_turn_of(key)); };
-    auto v_place = [&](int key, int piece) { return VALUES + key * ROW + 16 * (piece ^ v_turn_of(key)); };
     auto spread_keys = [&](int stage, float scale) {
         unsigned char* to = smem + stage * STAGE;
         u4 w[PIECES];
@@ -390,24 +593,10 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
             Frag f[2];
-            codes(w[e], scale, f);
+            spread(w[e], scale, f);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) *(u4*)(to + k_place(BLOCK_TOKENS * wave + e * ROWS + lrow, 2 * lpiece + h)) = f[h].q;
+            for (int h = 0; h < 2; ++h) *(u4*)(to + St::k_place(BLOCK_TOKENS * wave + e * ROWS + lrow, 2 * lpiece + h)) = f[h].q;
         }
-    };
-    // Tokens that no row sees become zeros, and so do values that are not finite where some rows see them and others do not: those are added at the end.
-    auto clean = [&](Frag& f, int key, int key0, unsigned gone) {
-        const int at = key0 + key;
-        const bool seen = at < hi && (at >= lo || at < sinks) && !(gone >> wave & 1);
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t x = seen ? f.u[e] : 0u;
-            const uint32_t low_half = (x & 0x7c00u) == 0x7c00u ? 0xffffu : 0u, high_half = (x & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
-            odd |= (low_half | high_half) != 0;
-            f.u[e] = x & ~(low_half | high_half);
-        }
-        if (odd) odd_one = 1;
     };
     auto spread_values = [&](int stage, float scale, int key0, unsigned gone, bool as_it_is) {
         unsigned char* to = smem + stage * STAGE;
@@ -417,12 +606,12 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
             Frag f[2];
-            codes(w[e], scale, f);
+            spread(w[e], scale, f);
             const int key = BLOCK_TOKENS * wave + e * ROWS + lrow;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (!as_it_is) clean(f[h], key, key0, gone);
-                *(u4*)(to + v_place(key, 2 * lpiece + h)) = f[h].q;
+                if (!as_it_is) tile.clean(f[h], key0 + key, gone >> wave & 1, odd_one);
+                *(u4*)(to + St::v_place(key, 2 * lpiece + h)) = f[h].q;
             }
         }
     };
@@ -434,33 +623,21 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 #pragma unroll
         for (int e = 0; e < PIECES; ++e) {
             const int key = BLOCK_TOKENS * wave + e * ROWS + lrow;
-            clean(f[e], key, key0, gone);
-            *(u4*)(smem + stage * STAGE + v_place(key, lpiece)) = f[e].q;
+            tile.clean(f[e], key0 + key, gone >> wave & 1, odd_one);
+            *(u4*)(smem + stage * STAGE + St::v_place(key, lpiece)) = f[e].q;
         }
     };
 
     // q, its sign that of the scale
     const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
     Frag q[NK];
-    {
-        const _Float16* at = a.q + (size_t)(r.first + row) * a.q_stride + (size_t)qh * DIM + 8 * half;
-        const uint32_t sign = scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-        for (int t = 0; t < NK; ++t) {
-            const u4 w = *(const u4*)(at + 16 * t);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[t].u[e] = there ? w[e] ^ sign : 0u;
-        }
-    }
+    load_q<DIM>(a, u, tile.group, w0 + col, there, half, scale, q);
     f16x O[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) O[d] = f16x{};
     float m = -INFINITY, l = 0.f;
 
-    // where this lane reads: K, row col: piece 2 t + half; V, transposed: rows 4 half + lane % 16 / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of 32
-    constexpr int BLOCK_OF_KEYS = 32 / GROUP * PITCH;
-    const int k_at = col / GROUP * PITCH + col % GROUP * ROW, k_turn = half ^ k_turn_of(col);
-    const int v_key = 4 * half + (lane & 15) / 4, v_at = VALUES + v_key * ROW + 8 * (lane & 3), v_turn = (lane >> 4 & 1) ^ (v_turn_of(v_key) / 2);
+    const St st(lane);
     auto first_product = [&](const unsigned char* base, f16x (&S)[2]) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -468,7 +645,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 #pragma unroll
             for (int t = 0; t < NK; ++t) {
                 Frag k;
-                k.q = *(const u4*)(base + k_at + b * BLOCK_OF_KEYS + 16 * ((2 * t) ^ k_turn));
+                st.keys(base, b, t, k);
                 z = mfma32(k.v, q[t].v, z);
             }
             S[b] = z;
@@ -491,7 +668,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     if (steps > 0) {
         gone = gone_of(0);
         const int key0 = tile_at(0), second = steps > 1 ? 1 : 0;
-        const bool as_it_is = plain(key0, gone);
+        const bool as_it_is = tile.plain(a, key0, gone);
         const unsigned long long here = block_of(0), there_on = block_of(second);
         const char *k0_at = (const char*)a.pages_k + here, *v0_at = (const char*)a.pages_v + here, *k1_at = (const char*)a.pages_k + there_on;
         each_piece<PIECES>([&](auto e) { send_keys(k0_at, e, 0); });
@@ -519,7 +696,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
         const char* v_base = (const char*)a.pages_v + block_of(iv);
         const float v_by = power_at(v_byte, iv);
         gone_next = gone_of(iv);
-        const bool as_it_is = plain(key_next, gone_next);
+        const bool as_it_is = tile.plain(a, key_next, gone_next);
         if (BITS == 16 && more && !as_it_is) put_values(v_base, stage ^ 1, key_next, gone_next);
         const unsigned v_to = more && (BITS == 8 || as_it_is) ? values_to(stage ^ 1) : aside;
         if (((i + 2) & 15) == 0 && i + 2 < steps) look(i + 2);
@@ -553,16 +730,8 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
             // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
             const unsigned char* next = smem + (stage ^ 1) * STAGE;
             Frag kf[AHEAD], vf[AHEAD], p[4];
-            auto read_k = [&](int x) { kf[x % AHEAD].q = *(const u4*)(next + k_at + x % 2 * BLOCK_OF_KEYS + 16 * ((2 * (x / 2)) ^ k_turn)); };
-            auto read_v = [&](int x) {
-                const int s = x / ND, d = x % ND;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const unsigned char* at = base + v_at + (16 * s + 8 * e) * ROW + 32 * ((2 * d) ^ v_turn);
-                    const auto w = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds)at);
-                    __builtin_memcpy(&vf[x % AHEAD].u[2 * e], &w, 8);
-                }
-            };
+            auto read_k = [&](int x) { st.keys(next, x % 2, x / 2, kf[x % AHEAD]); };
+            auto read_v = [&](int x) { st.values(base, x / ND, x % ND, vf[x % AHEAD]); };
             auto weights = [&](int x) {        // elements 2 x and 2 x + 1
                 const int b = x / 8, e = 2 * x % 16;
                 const float v = exp2_(__builtin_fmaf(S[b][e], by, -ref)), w = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
@@ -610,146 +779,231 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
         step(i, Sa, Sb, 0);
         if (i + 1 < steps) step(i + 1, Sb, Sa, 1);
     }
-    {
-        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-        l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
-    }
+    l = both_halves(l);
 
-    // The results go to LDS, as rows of fp32 (all have passed the loop's last barrier).  This lane's elements: columns 32 d + 8 q + 4 half of row 32 wave + col; pieces of
-    // 16 bytes change places within their row, so that the lanes that write at a time meet different banks.
+    // The results go to LDS (all have passed the loop's last barrier).  This lane's elements: columns 32 d + 8 q + 4 half of row 32 wave + col
     float* sum = (float*)smem;
-    const int my_row = 32 * wave + col;
-    auto piece_at = [&](int r, int c) { return sum + r * DIM + 4 * (c ^ (r & 15)); };
     if (half == 0) {
-        row_m[my_row] = m;
-        row_l[my_row] = l;
+        row_m[32 * wave + col] = m;
+        row_l[32 * wave + col] = l;
     }
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *(f4*)piece_at(my_row, 8 * d + 2 * e + half) = f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
+        for (int e = 0; e < 4; ++e) *(f4*)piece_at<DIM>(sum, 32 * wave + col, 8 * d + 2 * e + half) = f4{O[d][4 * e], O[d][4 * e + 1], O[d][4 * e + 2], O[d][4 * e + 3]};
     __syncthreads();
     if (odd_one) {
-        // Values that are not finite, in tiles of which not all rows see all: for the rows that see them, unless their score is -inf
-        for (int e = threadIdx.x; e < TQ * (DIM / 4); e += THREADS) {
-            const int r2 = e / (DIM / 4), c = e % (DIM / 4), pr = pair0 + r2;
-            if (pr >= pair1) continue;
-            const int rw = pr / group, at_pos = from + rw, head2 = u.h * group + pr - rw * group;
-            f4 add = {0.f, 0.f, 0.f, 0.f};
-            for (int i = k0; i < k1; ++i) {
-                const int key0 = key_of(i);
-                for (int key = key0; key < key0 + KT && key <= at_pos; ++key) {
-                    if (!(a.window == 0 || key > at_pos - a.window || key < a.sinks)) continue;
-                    const int block = block_at(key & ~(BLOCK_TOKENS - 1));
-                    if (block < 0) continue;
-                    const size_t at = ((size_t)(unsigned)block * BLOCK_TOKENS + key % BLOCK_TOKENS) * DIM;
-                    bool any = false;
-                    float v[4];
-#pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4) {
-                        if constexpr (BITS == 16) v[q4] = (float)((const _Float16*)a.pages_v)[at + 4 * c + q4];
-                        else v[q4] = (((const uint8_t*)a.pages_v)[at + 4 * c + q4] & 127) == 127 ? __builtin_nanf("") : 0.f;
-                        any |= !(fabsf(v[q4]) < INFINITY);
-                    }
-                    if (!any || plain(key0, gone_at(key0))) continue;
-                    if constexpr (BITS == 16) {
-                        const _Float16 *x = a.q + (size_t)(r.first + rw) * a.q_stride + (size_t)head2 * DIM, *y = (const _Float16*)a.pages_k + at;
-                        float score = 0.f;
-                        for (int t = 0; t < DIM; ++t) score += (float)x[t] * (float)y[t];
-                        if (score * scale == -INFINITY) continue;
-                    }
-#pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4) add[q4] += fabsf(v[q4]) < INFINITY ? 0.f : v[q4];
-                }
-            }
-            *(f4*)piece_at(r2, c) += add;
-        }
+        add_odd<DIM, BITS>(a, tile, scale, sum);
         __syncthreads();
     }
-
-    const float vs = BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f;
-    // Pieces of four columns: thread after thread along the rows
-    constexpr int MY = TQ * (DIM / 4) / THREADS;
-    const int used = pair1 - pair0;
-    if (parts > 1) {
-        // a partial result: rows of (m, sum), then rows of DIM
-        float* part = a.parts + COUNTERS + (size_t)u.place * part_words(DIM);
-#pragma unroll 4
-        for (int e = 0; e < MY; ++e) {
-            const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
-            if (r2 < used) {
-                const f4 x = *(const f4*)piece_at(r2, c);
-                put2(part + 2 * TQ + 4 * at, x[0], x[1]);
-                put2(part + 2 * TQ + 4 * at + 2, x[2], x[3]);
-            }
-        }
-        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, row_m[threadIdx.x], row_l[threadIdx.x]);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            unsigned* counter = (unsigned*)a.parts + u.first;
-            last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (unsigned)parts;
-            if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (!last) return;
-        const float* src = a.parts + COUNTERS + (size_t)u.first * part_words(DIM);
-        const size_t step_words = (size_t)a.kv * part_words(DIM);
-        for (int e = 0; e < MY; ++e) {
-            const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
-            if (r2 >= used) break;
-            float mm = -INFINITY, ll = 0.f;
-            f4 x = {0.f, 0.f, 0.f, 0.f};
-            // (four at a time on their way)
-            for (int c0 = 0; c0 < parts; c0 += 4) {
-                float2 ml[4], y[4][2];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float* one = src + (size_t)(c0 + k < parts ? c0 + k : parts - 1) * step_words;
-                    ml[k] = get2(one + 2 * r2);
-                    y[k][0] = get2(one + 2 * TQ + 4 * at);
-                    y[k][1] = get2(one + 2 * TQ + 4 * at + 2);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (c0 + k >= parts) break;
-                    const float up = fmaxf(mm, ml[k].x), f = factor(mm, up), g = factor(ml[k].x, up);
-                    ll = (mm == -INFINITY ? ll : ll * f) + (ml[k].x == -INFINITY ? ml[k].y : ml[k].y * g);
-                    mm = up;
-                    x = x * f + f4{y[k][0].x, y[k][0].y, y[k][1].x, y[k][1].y} * g;
-                }
-            }
-            *(f4*)piece_at(r2, c) = x;         // (its own thread reads it below)
-            if (c == 0) {
-                row_m[r2] = mm;
-                row_l[r2] = ll;
-            }
-        }
-        __syncthreads();
-    }
-    for (int e = 0; e < MY; ++e) {
-        const int at = threadIdx.x + e * THREADS, r2 = at / (DIM / 4), c = at % (DIM / 4);
-        if (r2 >= used) break;
-        const int pr = pair0 + r2, rw = pr / group;
-        const size_t place = (size_t)(r.first + rw) * a.heads + u.h * group + (pr - rw * group);
-        const float ll = row_l[r2], f = vs / ll;
-        const f4 x = *(const f4*)piece_at(r2, c);
-        h4 y;
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) y[q4] = (_Float16)(ll == 0.f ? 0.f : x[q4] * f);
-        *(h4*)(a.out + place * DIM + 4 * c) = y;
-        if (c == 0 && a.lse) a.lse[place] = LN2 * (row_m[r2] + __log2f(ll));
-    }
+    finish<DIM>(a, tile, BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f, sum, row_m, row_l, last);
 }
+
+// Few rows, which leave the matrix instructions idle: bound by memory.  Tiles of 32 pairs (one column block) by 32 keys; each wavefront has every fourth tile of keys for itself, with LDS
+// of its own and no barrier, the next one on its way to its registers meanwhile.  The four add up at the end.
+template <int DIM, int BITS, bool BLOCKS>
+__global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const PromptArgs a)
+{
+    constexpr int TQ = Narrow::TQ, KT = Narrow::KT;
+    typedef Stage<DIM, KT> St;
+    constexpr int NK = DIM / 16, ND = DIM / 32;
+    constexpr int BYTES = DIM * BITS / 8, PIECES = BLOCK_TOKENS * BYTES / 1024, PR = BYTES / 16, ROWS = 64 / PR;      // of a row in memory; KiB of 16 keys; pieces of a row, rows of a KiB
+
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    __shared__ int scratch[RG + 4 + 2 * RG];
+    __shared__ int odd_one, last;
+    __shared__ float red_m[RG][TQ], red_l[RG][TQ], row_m[TQ], row_l[TQ];
+
+    Tile<Narrow> tile;
+    if (!tile.find(a, (int)blockIdx.x, scratch)) return;
+    const Unit& u = tile.u;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int mine = (tile.k1 - tile.k0 - wave + RG - 1) / RG;                   // tiles of keys
+    const bool all = tile.pair1 - tile.pair0 == TQ, there = tile.pair0 + col < tile.pair1;
+    const int pos = there ? tile.from + (tile.pair0 + col) / tile.group : -1;
+    if (threadIdx.x == 0) odd_one = 0;
+    __syncthreads();
+
+    // Blocks of 16 tokens of the next 32 tiles: lane 2 i + g has that of group g of tile i (-1: no page, or no key that a row sees)
+    int block_of = -1;
+    unsigned k_byte = 0, v_byte = 0;
+    auto key_at = [&](int i) { return tile.key_of(tile.k0 + wave + RG * i); };
+    auto look = [&](int i0) {
+        const int i = i0 + (lane >> 1), key = i < mine ? key_at(i) + BLOCK_TOKENS * (lane & 1) : tile.hi;
+        block_of = key < tile.hi ? tile.block_at(a, key) : -1;
+        if constexpr (BLOCKS) {
+            k_byte = block_of < 0 ? 0 : a.k_scales[block_of];
+            v_byte = block_of < 0 ? 0 : a.v_scales[block_of];
+        }
+    };
+    u4 mk[2][PIECES], mv[2][PIECES];
+    float k_by[2], v_by[2];
+    unsigned gone = 0;
+    auto load = [&](int i) {
+        gone = 0;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int from = 2 * (i & 31) + g, block = __builtin_amdgcn_readlane(block_of, from);
+            gone |= (unsigned)(block < 0) << g;
+            const size_t at = (size_t)(unsigned)(block < 0 ? 0 : block) * (BLOCK_TOKENS * BYTES);
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) {
+                mk[g][e] = *(const u4*)((const char*)a.pages_k + at + (e * 1024 + 16u * lane));
+                mv[g][e] = *(const u4*)((const char*)a.pages_v + at + (e * 1024 + 16u * lane));
+            }
+            k_by[g] = BLOCKS ? power_of(__builtin_amdgcn_readlane(k_byte, from)) : 1.f;
+            v_by[g] = BLOCKS ? power_of(__builtin_amdgcn_readlane(v_byte, from)) : 1.f;
+        }
+    };
+    unsigned char* base = smem + wave * St::BYTES;
+    auto put = [&](int key0) {
+        const bool as_it_is = tile.plain(a, key0, gone);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) {
+                constexpr int HALVES = BITS == 16 ? 1 : 2;
+                const int key = BLOCK_TOKENS * g + e * ROWS + lane / PR, piece = HALVES * (lane % PR);
+                Frag k[2], v[2];
+                if constexpr (BITS == 16) {
+                    k[0].q = mk[g][e];
+                    v[0].q = mv[g][e];
+                } else {
+                    spread(mk[g][e], k_by[g], k);
+                    spread(mv[g][e], v_by[g], v);
+                }
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    if (!as_it_is) tile.clean(v[h], key0 + key, gone >> g & 1, odd_one);
+                    *(u4*)(base + St::k_place(key, piece + h)) = k[h].q;
+                    *(u4*)(base + St::v_place(key, piece + h)) = v[h].q;
+                }
+            }
+    };
+
+    const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
+    Frag q[NK];
+    load_q<DIM>(a, u, tile.group, tile.pair0 + col, there, half, scale, q);
+    f16x O[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) O[d] = f16x{};
+    float m = -INFINITY, l = 0.f;
+    const St st(lane);
+    if (mine > 0) {
+        look(0);
+        load(0);
+    }
+    for (int i = 0; i < mine; ++i) {
+        const int key0 = key_at(i);
+        const unsigned missing = gone;
+        put(key0);
+        if (i + 1 < mine) {
+            if (((i + 1) & 31) == 0) look(i + 1);
+            load(i + 1);
+        }
+        f16x S = {};
+#pragma unroll
+        for (int t = 0; t < NK; ++t) {
+            Frag k;
+            st.keys(base, 0, t, k);
+            S = mfma32(k.v, q[t].v, S);
+        }
+        const bool whole = all && missing == 0 && key0 + KT <= tile.low + 1 && (a.window == 0 || key0 > tile.high - a.window || key0 + KT <= a.sinks);
+        if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int key = key0 + 8 * (e / 4) + 4 * half + e % 4;
+                const bool seen = key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks) && !(missing >> (e / 8) & 1);
+                S[e] = seen ? S[e] : -INFINITY;
+            }
+        }
+        float top = S[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
+        top *= by;
+        if (__any(top > m + (RAISE + LOWER))) {
+            top = max_of_halves(top);
+            const float up = top > m + (RAISE + LOWER) ? top - LOWER : m, f = m == up ? 1.f : exp2_(m - up);
+            m = up;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) O[d] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        Frag p[2];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float x = exp2_(__builtin_fmaf(S[e], by, -ref)), y = exp2_(__builtin_fmaf(S[e + 1], by, -ref));
+            l += x;
+            l += y;
+            p[e / 8].p[e % 8 / 2] = h2{(_Float16)x, (_Float16)y};
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                Frag v;
+                st.values(base, s, d, v);
+                O[d] = mfma32(v.v, p[s].v, O[d]);
+            }
+    }
+    l = both_halves(l);
+
+    // The four wavefronts' results, added up in LDS
+    if (half == 0) {
+        red_m[wave][col] = m;
+        red_l[wave][col] = l;
+    }
+    __syncthreads();
+    float up = red_m[0][col];
+#pragma unroll
+    for (int w = 1; w < RG; ++w) up = fmaxf(up, red_m[w][col]);
+    const float f = factor(m, up);
+    float* sum = (float*)smem;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            *(f4*)piece_at<DIM>(sum + wave * TQ * DIM, col, 8 * d + 2 * e + half) = f4{O[d][4 * e] * f, O[d][4 * e + 1] * f, O[d][4 * e + 2] * f, O[d][4 * e + 3] * f};
+    if (wave == 0 && half == 0) {
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < RG; ++w) total += red_m[w][col] == -INFINITY ? red_l[w][col] : red_l[w][col] * exp2_(red_m[w][col] - up);
+        row_m[col] = up;
+        row_l[col] = total;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < TQ * (DIM / 4); e += THREADS) {
+        f4 x = *(const f4*)(sum + 4 * e);
+#pragma unroll
+        for (int w = 1; w < RG; ++w) x += *(const f4*)(sum + w * TQ * DIM + 4 * e);
+        *(f4*)(sum + 4 * e) = x;
+    }
+    __syncthreads();
+    if (odd_one) {
+        add_odd<DIM, BITS>(a, tile, scale, sum);
+        __syncthreads();
+    }
+    finish<DIM>(a, tile, BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f, sum, row_m, row_l, last);
+}
+
+// Tiles of tq pairs at most, and the parts that some are cut into
+long long units_of(int M, int B, int heads, int kv, int tq) { return (((long long)M * (heads / kv) + tq - 1) / tq + B) * kv + MAX_PARTS; }
+
+// From so many pairs of a row and a query head of a kv head a request on, on the average, wide tiles
+constexpr int MANY_PAIRS = 33;
 
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    constexpr int lds = lds_bytes<DIM, BITS>();
-    const auto kern = prompt_kernel<DIM, BITS, BLOCKS>;
+    const bool few = (long long)a.M * (a.heads / a.kv) < (long long)MANY_PAIRS * a.B;
+    constexpr int sums = 128 * DIM * 4;        // (128 rows of O, or four times 32)
+    constexpr int wide = 2 * Stage<DIM, Wide::KT>::BYTES + BLOCK_TOKENS * DIM * BITS / 8, narrow = RG * Stage<DIM, Narrow::KT>::BYTES;
+    const int lds = few ? (narrow > sums ? narrow : sums) : (wide > sums ? wide : sums);
+    const auto kern = few ? few_kernel<DIM, BITS, BLOCKS> : prompt_kernel<DIM, BITS, BLOCKS>;
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    kern<<<(unsigned)prompt_units(a.M, a.B, a.heads, a.kv), THREADS, lds, stream>>>(a);
+    kern<<<(unsigned)units_of(a.M, a.B, a.heads, a.kv, few ? Narrow::TQ : Wide::TQ), THREADS, lds, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -762,12 +1016,9 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
 
 }  // namespace
 
-long long prompt_units(int M, int B, int heads, int kv)
-{
-    return (((long long)M * (heads / kv) + TQ - 1) / TQ + B) * kv + MAX_PARTS;
-}
+long long prompt_units(int M, int B, int heads, int kv) { return units_of(M, B, heads, kv, Narrow::TQ); }
 
-size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words(dim)) * sizeof(float); }
+size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words<Wide>(dim)) * sizeof(float); }
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream)
 {
