@@ -33,15 +33,18 @@ namespace {
 constexpr int RG = 4, THREADS = 64 * RG;       // wavefronts of a workgroup
 // Pairs and keys of a tile, and keys of a part of it at least: of many rows (a wavefront a quarter of the pairs), and of few (a wavefront every fourth tile of keys)
 struct Wide {
-    static constexpr int TQ = 128, KT = 64, LEAST_PART = 4;
+    static constexpr int TQ = 128, KT = 64, LEAST_PART = 8;
 };
 struct Narrow {
     static constexpr int TQ = 32, KT = 32, LEAST_PART = 16;
 };
 constexpr int CUS = 256;
-// Parts that all tiles together are cut into at least, where they have the work; partial results that there are: see share_of()
-constexpr int WANT = 2 * CUS;
-constexpr int MAX_PARTS = 2 * WANT;
+// Workgroups a compute unit has at a time, as registers and LDS allow
+constexpr int residents(int dim) { return dim == 256 ? 1 : 2; }
+// Parts that all tiles together are cut into at least, where they have the work (as many as the chip has at a time: 32 requests of 5 rows of 4096 tokens, heads of 256 in 8 bits, with
+// twice as many 157 us, with these 136); partial results that there are: see share_of()
+constexpr int want_of(int dim) { return CUS * residents(dim); }
+constexpr int MAX_PARTS = 2 * want_of(128);
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr float RAISE = 4.f, LOWER = 11.f;
@@ -105,12 +108,13 @@ struct Unit {
     int b, h, tile, part, parts;
     int place, first;
 };
-// Tiles of a request are cut into ceil(cost / share) parts, share = a WANT-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have at most 2 WANT parts.
+// Tiles of a request are cut into ceil(cost / share) parts, share = a want_of(dim)-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have at
+// most twice as many parts.
 // (The work is added up in floats, in one order: everyone finds the same share.)
 template <typename SHAPE>
-__device__ __forceinline__ int share_of(float work, int kv)
+__device__ __forceinline__ int share_of(const PromptArgs& a, float work)
 {
-    const float x = work * (float)kv * (1.f / WANT);
+    const float x = work * (float)a.kv / (float)want_of(a.dim);
     const int share = x < 1e9f ? (int)x + 1 : 0x7fffffff;
     return share < SHAPE::LEAST_PART ? SHAPE::LEAST_PART : share;
 }
@@ -152,7 +156,7 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
     const int lane = threadIdx.x & 63;
     Request r = request_of<SHAPE>(a, lane < a.B ? lane : a.B - 1);
     if (lane >= a.B) r.tiles = 0;
-    const int share = share_of<SHAPE>(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)), a.kv);
+    const int share = share_of<SHAPE>(a, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)));
     const int parts = parts_of(r, share), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
     const int v = scan(units), c = scan(cut);
     const unsigned long long mine = __ballot(id >= v - units && id < v);
@@ -188,7 +192,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     work = 0.f;
 #pragma unroll
     for (int w = 0; w < RG; ++w) work += sums[w];
-    const int share = share_of<SHAPE>(work, a.kv);
+    const int share = share_of<SHAPE>(a, work);
     int before = 0, cut_before = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
@@ -446,34 +450,55 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
         if (!last) return;
         const float* src = a.parts + COUNTERS + (size_t)t.u.first * WORDS;
         const size_t step_words = (size_t)a.kv * WORDS;
-        for (int e = 0; e < MY; ++e) {
-            const int at = threadIdx.x + e * THREADS, r = at / (DIM / 4), c = at % (DIM / 4);
-            if (r >= used) break;
-            float m = -INFINITY, l = 0.f;
-            f4 x = {0.f, 0.f, 0.f, 0.f};
-            // (four at a time on their way)
-            for (int c0 = 0; c0 < parts; c0 += 4) {
-                float2 ml[4], y[4][2];
+        // (eight requests a thread on their way at a time: one after the other, 16 pieces of two parts would take 20 us)
+        constexpr int BATCH = 4, AT_ONCE = 2;
+        static_assert(MY % BATCH == 0 || MY < BATCH, "");
+        for (int e0 = 0; e0 < MY; e0 += BATCH) {
+            if ((threadIdx.x + e0 * THREADS) / (DIM / 4) >= used) break;
+            int at[BATCH], r[BATCH], c[BATCH];
+            float m[BATCH], l[BATCH];
+            f4 x[BATCH];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float* one = src + (size_t)(c0 + k < parts ? c0 + k : parts - 1) * step_words;
-                    ml[k] = get2(one + 2 * r);
-                    y[k][0] = get2(one + 2 * TQ + 4 * at);
-                    y[k][1] = get2(one + 2 * TQ + 4 * at + 2);
+            for (int i = 0; i < BATCH; ++i) {
+                const int e = e0 + i < MY ? e0 + i : MY - 1, there = threadIdx.x + e * THREADS;
+                at[i] = there / (DIM / 4) < used ? there : threadIdx.x + e0 * THREADS;          // (behind the last row: the first of the batch again)
+                r[i] = at[i] / (DIM / 4);
+                c[i] = at[i] % (DIM / 4);
+                m[i] = -INFINITY;
+                l[i] = 0.f;
+                x[i] = f4{0.f, 0.f, 0.f, 0.f};
+            }
+            for (int p0 = 0; p0 < parts; p0 += AT_ONCE) {
+                float2 ml[AT_ONCE][BATCH], y[AT_ONCE][BATCH][2];
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const float* one = src + (size_t)(p0 + k < parts ? p0 + k : parts - 1) * step_words;
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        ml[k][i] = get2(one + 2 * r[i]);
+                        y[k][i][0] = get2(one + 2 * TQ + 4 * at[i]);
+                        y[k][i][1] = get2(one + 2 * TQ + 4 * at[i] + 2);
+                    }
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (c0 + k >= parts) break;
-                    const float up = fmaxf(m, ml[k].x), f = factor(m, up), g = factor(ml[k].x, up);
-                    l = (m == -INFINITY ? l : l * f) + (ml[k].x == -INFINITY ? ml[k].y : ml[k].y * g);
-                    m = up;
-                    x = x * f + f4{y[k][0].x, y[k][0].y, y[k][1].x, y[k][1].y} * g;
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    if (p0 + k >= parts) break;
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        const float mk = ml[k][i].x, up = fmaxf(m[i], mk), f = factor(m[i], up), g = factor(mk, up);
+                        l[i] = (m[i] == -INFINITY ? l[i] : l[i] * f) + (mk == -INFINITY ? ml[k][i].y : ml[k][i].y * g);
+                        m[i] = up;
+                        x[i] = x[i] * f + f4{y[k][i][0].x, y[k][i][0].y, y[k][i][1].x, y[k][i][1].y} * g;
+                    }
                 }
             }
-            *(f4*)piece_at<DIM>(sum, r, c) = x;                                  // (its own thread reads it below)
-            if (c == 0) {
-                row_m[r] = m;
-                row_l[r] = l;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                *(f4*)piece_at<DIM>(sum, r[i], c[i]) = x[i];                     // (its own thread reads it below)
+                if (c[i] == 0) {
+                    row_m[r[i]] = m[i];
+                    row_l[r[i]] = l[i];
+                }
             }
         }
         __syncthreads();
@@ -512,9 +537,6 @@ __device__ __forceinline__ float both_halves(float v)
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
-
-// Workgroups a compute unit has at a time, as registers and LDS allow
-constexpr int residents(int dim) { return dim == 256 ? 1 : 2; }
 
 template <int DIM, int BITS, bool BLOCKS>
 __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const PromptArgs a)
@@ -990,17 +1012,21 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
 // Tiles of tq pairs at most, and the parts that some are cut into
 long long units_of(int M, int B, int heads, int kv, int tq) { return (((long long)M * (heads / kv) + tq - 1) / tq + B) * kv + MAX_PARTS; }
 
-// From so many pairs of a row and a query head of a kv head a request on, on the average, wide tiles
-constexpr int MANY_PAIRS = 33;
+// Narrow tiles up to so many pairs of a request's rows and a kv head's query heads, on the average (32 requests of 8192 tokens, 32 / 8 heads of 128 in 8 bits, 5, 16, 20 rows each: narrow 110,
+// 147, 276 us, wide 213, 165, 246), or so many wide tiles in all, which would leave much of the chip idle (256, 512, 768 rows of one request: narrow 11.1, 15.8, 28, wide 15.7, 20.5, 26;
+// 512 rows behind 7680 tokens: 131, 103).  Heads of 256 in fp16 have no registers for a narrow tile on its way (32 x 5 rows of 4096: narrow 302 us, wide 275).
+constexpr int FEW_PAIRS = 64, FEW_TILES = 96;
 
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    const bool few = (long long)a.M * (a.heads / a.kv) < (long long)MANY_PAIRS * a.B;
+    const bool few = (DIM < 256 || BITS == 8) &&
+                     ((long long)a.M * (a.heads / a.kv) <= (long long)FEW_PAIRS * a.B || (long long)a.M * a.heads <= (long long)FEW_TILES * Wide::TQ);
     constexpr int sums = 128 * DIM * 4;        // (128 rows of O, or four times 32)
     constexpr int wide = 2 * Stage<DIM, Wide::KT>::BYTES + BLOCK_TOKENS * DIM * BITS / 8, narrow = RG * Stage<DIM, Narrow::KT>::BYTES;
     const int lds = few ? (narrow > sums ? narrow : sums) : (wide > sums ? wide : sums);
-    const auto kern = few ? few_kernel<DIM, BITS, BLOCKS> : prompt_kernel<DIM, BITS, BLOCKS>;
+    auto kern = prompt_kernel<DIM, BITS, BLOCKS>;
+    if constexpr (DIM < 256 || BITS == 8) kern = few ? few_kernel<DIM, BITS, BLOCKS> : kern;
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     kern<<<(unsigned)units_of(a.M, a.B, a.heads, a.kv, few ? Narrow::TQ : Wide::TQ), THREADS, lds, stream>>>(a);
@@ -1018,7 +1044,16 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
 
 long long prompt_units(int M, int B, int heads, int kv) { return units_of(M, B, heads, kv, Narrow::TQ); }
 
-size_t prompt_workspace_bytes(int dim) { return (COUNTERS + MAX_PARTS * part_words<Wide>(dim)) * sizeof(float); }
+size_t prompt_workspace_bytes(int dim)
+{
+    // (a workspace for wide heads also serves narrower ones, of which there are more at a time)
+    size_t words = 0;
+    for (int d = 64; d <= dim; d *= 2) {
+        const size_t one = 2 * (size_t)want_of(d) * part_words<Wide>(d);
+        words = one > words ? one : words;
+    }
+    return (COUNTERS + words) * sizeof(float);
+}
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream)
 {

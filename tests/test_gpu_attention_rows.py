@@ -122,6 +122,7 @@ class Rows:
         return out[:used], lse[:used]
 
 
+# tokens and rows
 EDGES = [(1, 1), (2, 2), (15, 3), (16, 16), (17, 1), (31, 31), (32, 7), (33, 33), (63, 2), (64, 64), (65, 65), (127, 30), (128, 128), (129, 1), (130, 129), (200, 77)]
 SHAPES = [
     # (tokens, rows) of the requests, heads, kv, dim, form, page
@@ -160,6 +161,17 @@ def test_many_pairs(gpu, requests, heads, kv, dim, form, page):
     assert c.M * heads >= 2 ** 17
     c.check(gpu)
     c.check(gpu, 50, 7)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("form", ["fp16", "heads", "blocks"])
+@pytest.mark.parametrize("heads,kv,page", [(32, 2, 16), (45, 3, 48)])
+def test_wide_tiles(gpu, dim, form, heads, kv, page):
+    """Every length at which tiles of rows and keys begin and end, where there are rows enough for tiles of 128 pairs."""
+    c = Rows(56 + dim, EDGES, heads, kv, dim, form, page, tail=1)
+    assert c.M * heads > 96 * 128 and c.M * heads // kv > 64 * c.B
+    c.check(gpu)
+    c.check(gpu, 33, 20)
 
 
 def test_many_pairs_cut_along_the_keys(gpu):
