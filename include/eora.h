@@ -436,6 +436,7 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  *      t <= p  with  t > p - window  or  t < sinks          (window 0: all t <= p),
  * for query head i of kv head i / (n_heads / n_kv_heads) as in eora_cache_attention(), with pages, scores and lse as there.  A row that sees nothing (a position below 0, all
  * masked) has out = 0 and lse = -inf.  What a row does not see is never used for it, NaN and infinities included, also where other rows see it.
+ * A value that is not finite makes its column of out infinite or NaN for the rows that see it.
  * row_starts: B + 1 int32, not decreasing, taken as 0 .. M; rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
  * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.
  * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits in the form for single tokens,
@@ -444,8 +445,8 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  * workspace: eora_cache_attention_rows_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the first call, the rest
  * may hold anything; every call leaves it usable for the next, of whatever sizes and of either form.
  * Constraints: M >= 0, 0 <= B <= 8192 (M or B 0: no-op), n_heads % n_kv_heads == 0, q_stride % 8 == 0, max_pages >= 1, max_pages * page_size <= 2^30,
- * window >= 0, sinks >= 0, scale finite, (M * n_heads / 128 + B * n_kv_heads) < 8e6, M * (n_heads / n_kv_heads) < 2^31; without row_starts as
- * eora_cache_attention(); the cache's.
+ * window >= 0, sinks >= 0, scale finite; with row_starts M * (n_heads / n_kv_heads) < 2^31, M * n_heads / 32 + B * n_kv_heads < 8e6 and
+ * n_pages * page_size * n_kv_heads < 2^35 - 16; without as eora_cache_attention(); the cache's.
  * Errors: EORA_ERR_NULL / UNSUPPORTED (head_dim, cache_bits, scale_block) / SHAPE / VALUE (scale) / ALIGN / WORKSPACE / LAUNCH. */
 size_t eora_cache_attention_rows_workspace_bytes(int M, int B, int n_heads, int n_kv_heads, int head_dim, int max_tokens);      /* 0: invalid */
 int eora_cache_attention_rows(const void* q, const void* pages_k, const void* pages_v, const void* k_scale, const void* v_scale,

@@ -157,6 +157,7 @@ __device__ __forceinline__ void blocks_of(const BlocksArgs& a, int r0, int h, bo
     float w[8];
     if (weight) col.fetch(weight, w);
     for (int i = LOOK; i < LOOK + a.look; ++i) {
+        if (r0 - LOOK + i >= a.m0 + a.tokens) break;                            // (of the next launch)
         const int b = __builtin_amdgcn_readlane(block, i);
         if (b < 0) continue;
         const unsigned long long same = __ballot(block == b);

@@ -2,26 +2,34 @@
 //
 //      s_rt = scale q_r . k_t,   out_r = sum_t 2^(s_rt log2 e - m) v_t / sum_t 2^(s_rt log2 e - m)      t <= p_r, and t > p_r - window or t < sinks
 //
-// Row r of a request's n sits at p_r = length - n + r.  Bound by the matrix instructions: 4 dim flops for each pair of a query head's row and a token.
+// Row r of a request's n sits at p_r = length - n + r.  Bound by the matrix instructions where there are many rows (4 dim flops for each pair of a query head's row and a token), by memory
+// where there are few.  64 / 8 heads of 128: 8192 rows in fp16 in 1118 us, 984 TF; 32 / 8 heads: 2048 rows in 58 us in fp16, 66 in 8 bits; 32 requests of 5 rows and 8192 tokens in 8 bits
+// (537 MB) in 107 us, 5.1 TB/s; 17 rows of 17 in 9 us.
 //
 // Tile: 128 pairs of a row and a query head of one kv head (32 a wavefront) by 64 keys.  A column of the matrix instructions is a pair, all query heads of a kv head share the keys.
 // S^T = K Q^T (32 x 32 x 16): a lane holds one pair's scores of 16 keys of 32, so that softmax needs no exchange between lanes but one of the largest score, and the scores are,
 // as fp16 weights, the second operand of O^T = V^T P^T, if that takes its keys in the order in which they lie: 8 (e / 4) + 4 half + e % 4 of 16.
-// K and V lie in LDS as fp16 rows, in two stages; V's operand is read transposed (ds_read_tr16_b64: four keys of a column a lane).  Pieces of a row are
-// moved around by the row's number, so that the lanes that read at a time meet different banks.  Codes of a cache in 8 bits become fp16, exactly, once, on their way to LDS.
+// K and V lie in LDS as fp16 rows, in two stages; V's operand is read transposed (ds_read_tr16_b64: four keys of a column a lane).  fp16 tiles go from memory to LDS without registers
+// (by way of them a wavefront's 32 words of a tile on its way spilled: 3749 us where 1418 were left without); codes of 8 bits go there as they are, and become fp16, exactly, once,
+// by the wavefront that moved them.
 //
-// Two teams of four wavefronts work on the same 128 pairs, on every other tile of keys, and add up in LDS at the end: so there is one unit a compute unit at a time, of all its
-// wavefronts, and units in the order of falling work even out.  (Heads of 256: one team.)
+// A step: the scores of the next tile beside the softmax of this one, then this one's O, one matrix instruction a slot in an order that the compiler keeps, operands read four ahead (left to itself it
+// reads one, waits, multiplies: 1418 us -> 1395).  Alone on its compute unit a workgroup takes 2860 cycles a step, 1024 of matrix instructions: 740 before the first (scalar work, masks, the
+// first operands), 1340 beside the softmax, 580 beside V, 210 for tiles and the barrier.  So there are two workgroups a compute unit, which fill each other's gaps (8192 rows: 53 % of the
+// cycles have a matrix instruction).  What did not help: two teams of wavefronts on one tile of pairs (1378 us), eight wavefronts on tiles of 256 (1206, and 71 where 2048 rows take 59), 64 pairs a wavefront
+// (twice the work for an operand, one wavefront a SIMD: 1.4 times as long), O one step later (registers), waits of a step and a half for tiles, scalar work between the matrix instructions.
+//
+// Few rows: tiles of 32 pairs by 32 keys (few_kernel() below).
 //
 // Softmax: as for single tokens, m is a reference (LOWER below the largest score when it is set, raised when a score has risen by RAISE more), the largest weight 2^11 to 2^15.  A weight meets
-// V as one fp16, rounded to nearest: off by 2^-12 of itself at most, which in a sum over tokens stays below the result's own rounding; two of them, as for single
-// tokens, would take half as long again.  Scores, sums and O are fp32.
+// V as one fp16, rounded to nearest: off by 2^-11 of itself at most, as the result is by its own rounding, and by less in a sum over tokens; two of them, as for single
+// tokens, would take half as long again.  The sum of the weights is of those that were not rounded: lse would show it.  Scores, sums and O are fp32.
 //
 // What rows may not see: a tile that all rows of a wavefront see as a whole takes no test.  Tokens that no row of the tile sees are zeros in LDS; where some rows see a token and others do not, a value
-// that is not finite would spoil a product with weights of 0: then the tile takes a slower way, in which such values are added to the rows that see them one by one.
+// that is not finite would spoil a product with weights of 0: it is a zero there too, and added at the end, to the rows that see it (add_odd()).
 //
 // Split: tiles with more than their share of all work are cut along the keys, into equal parts by a rule on the lengths of all requests; the last part to
-// arrive adds up the results of all, in the order of the keys.
+// arrive adds up the results of all, in the order of the keys.  Units in the order of falling work, kv heads side by side: with eight of them each XCD has the keys of one.
 #include "heads.hpp"
 #include "serving.hpp"
 
@@ -822,7 +830,8 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 }
 
 // Few rows, which leave the matrix instructions idle: bound by memory.  Tiles of 32 pairs (one column block) by 32 keys; each wavefront has every fourth tile of keys for itself, with LDS
-// of its own and no barrier, the next one on its way to its registers meanwhile.  The four add up at the end.
+// of its own and no barrier, the next one on its way to its registers meanwhile: 64 KiB on their way a compute unit in fp16.  The four add up at the end.  (32 requests of 5 rows and 8192 tokens:
+// 107 us; with the tiles of many rows, of which three wavefronts of four have no pair and all wait for each other at every tile, 213.)
 template <int DIM, int BITS, bool BLOCKS>
 __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const PromptArgs a)
 {

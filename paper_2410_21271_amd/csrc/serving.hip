@@ -305,6 +305,8 @@ int eora_cache_attention_rows(const void* q, const void* pages_k, const void* pa
     rc = check_attention(q, page_table, lengths, out, lse, n_heads, n_kv_heads, head_dim, q_stride, page_size, max_pages, scale);
     if (rc != EORA_OK) return rc;
     if (!row_starts && too_many_tiles(B, n_heads, n_kv_heads, page_size, max_pages)) return EORA_ERR_SHAPE;
+    // (blocks of 16 tokens are counted in 32 bits)
+    if (row_starts && (double)n_pages * page_size * n_kv_heads >= 16.0 * 0x7fffffff) return EORA_ERR_SHAPE;
     if (row_starts && ((long long)M * (n_heads / n_kv_heads) > 0x7fffffff || prompt_units(M, B, n_heads, n_kv_heads) > 0x7fffff)) return EORA_ERR_SHAPE;
     if (!aligned_to(row_starts, 4)) return EORA_ERR_ALIGN;
     if (!workspace) return EORA_ERR_WORKSPACE;

@@ -44,7 +44,7 @@ def test_read(code, kw):
     (UNSUPPORTED, dict(dim=32, q_stride=256)),
     (SHAPE, dict(M=-1)), (SHAPE, dict(B=-1)), (SHAPE, dict(B=8193)), (SHAPE, dict(starts=None)), (SHAPE, dict(heads=7, q_stride=448)), (SHAPE, dict(heads=0)), (SHAPE, dict(kv=0)),
     (SHAPE, dict(width=0)), (SHAPE, dict(window=-1)), (SHAPE, dict(sinks=-1)), (SHAPE, dict(q_stride=511)), (SHAPE, dict(page=8)), (SHAPE, dict(width=2 ** 26 + 1)),
-    (SHAPE, dict(M=2 ** 30)), (SHAPE, dict(M=8192, starts=None, B=8192, heads=2 ** 12, kv=2 ** 12, q_stride=2 ** 18, width=128)),
+    (SHAPE, dict(M=2 ** 30)), (SHAPE, dict(n_pages=2 ** 26, heads=64, kv=64, q_stride=64 * 64)), (SHAPE, dict(M=8192, starts=None, B=8192, heads=2 ** 12, kv=2 ** 12, q_stride=2 ** 18, width=128)),
     (VALUE, dict(scale=NAN)), (VALUE, dict(scale=-INF)),
     (ALIGN, dict(q=G + 2)), (ALIGN, dict(out=G + 8)), (ALIGN, dict(table=G + 2)), (ALIGN, dict(lengths=G + 1)), (ALIGN, dict(starts=G + 2)), (ALIGN, dict(lse=G + 2)),
     (ALIGN, dict(ws=G + 4)), (ALIGN, dict(bits=8, ks=G + 2, vs=G)),
