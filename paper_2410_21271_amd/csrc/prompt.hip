@@ -58,6 +58,7 @@ static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr float RAISE = 4.f, LOWER = 11.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef float f16x __attribute__((ext_vector_type(16)));
 typedef __fp16 tr4 __attribute__((__vector_size__(8)));
 typedef __attribute__((address_space(3))) tr4* tr4_lds;
@@ -116,13 +117,14 @@ struct Unit {
     int b, h, tile, part, parts;
     int place, first;
 };
-// Tiles of a request are cut into ceil(cost / share) parts, share = a want_of(dim)-th of all work: with parts > 1 a request has less than 2 cost / share, so all of them have at
-// most twice as many parts.
-// (The work is added up in floats, in one order: everyone finds the same share.)
+// Tiles of a request are cut into ceil(cost / share) parts, share = a want_of(dim)-th of all work or a little more: with parts > 1 a request has less than 2 cost / share, so all of
+// them have at most twice as many parts.  All tiles alike, as if each saw as much as the last (each by what it sees: 1536 rows of 32 / 8 heads 52 -> 47.6 us, but 2048 rows, whose tiles fill
+// the chip once, 56 -> 67: parts that then wait for a place).
+// (The work is added up in floats, in one order: everyone finds the same share.  What is added covers their roundings, at most 50 of 2^-24.)
 template <typename SHAPE>
 __device__ __forceinline__ int share_of(const PromptArgs& a, float work)
 {
-    const float x = work * (float)a.kv / (float)want_of(a.dim);
+    const float x = work * (float)a.kv * (1.0001f / (float)want_of(a.dim));
     const int share = x < 1e9f ? (int)x + 1 : 0x7fffffff;
     return share < SHAPE::LEAST_PART ? SHAPE::LEAST_PART : share;
 }
@@ -249,17 +251,16 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     return true;
 }
 
-// Stores and loads of partial results go past the caches of an XCD, eight bytes each (relaxed, agent scope).
-__device__ __forceinline__ void put2(float* p, float x, float y)
-{
-    const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
-    __hip_atomic_store((unsigned long long*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get2(const float* p)
-{
-    const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
-}
+// Stores and loads of partial results go past the caches of an XCD (agent scope: SC1), 16 bytes each, or a pair
+constexpr int AGENT = 16;
+struct Partial {
+    __amdgpu_buffer_rsrc_t at;
+    __device__ __forceinline__ Partial(float* p, size_t words) : at(__builtin_amdgcn_make_buffer_rsrc(p, 0, (int)(words * sizeof(float)), 0x00027000)) {}
+    __device__ __forceinline__ void put(int word, f4 x) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), at, 4 * word, 0, AGENT); }
+    __device__ __forceinline__ void put(int word, float2 x) const { __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, x), at, 4 * word, 0, AGENT); }
+    __device__ __forceinline__ f4 get(int word) const { return __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(at, 4 * word, 0, AGENT)); }
+    __device__ __forceinline__ float2 get2(int word) const { return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(at, 4 * word, 0, AGENT)); }
+};
 __device__ __forceinline__ float factor(float m, float to) { return m == -INFINITY ? 0.f : exp2_(m - to); }
 
 // f(0) .. f(N - 1), each number a type
@@ -436,17 +437,13 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
     const int used = t.pair1 - t.pair0, parts = t.parts;
     if (parts > 1) {
         // a partial result: rows of (m, sum), then rows of DIM
-        float* part = a.parts + COUNTERS + (size_t)t.u.place * WORDS;
+        const Partial part(a.parts + COUNTERS + (size_t)t.u.place * WORDS, WORDS);
 #pragma unroll 4
         for (int e = 0; e < MY; ++e) {
             const int at = threadIdx.x + e * THREADS, r = at / (DIM / 4), c = at % (DIM / 4);
-            if (r < used) {
-                const f4 x = *(const f4*)piece_at<DIM>(sum, r, c);
-                put2(part + 2 * TQ + 4 * at, x[0], x[1]);
-                put2(part + 2 * TQ + 4 * at + 2, x[2], x[3]);
-            }
+            if (r < used) part.put(2 * TQ + 4 * at, *(const f4*)piece_at<DIM>(sum, r, c));
         }
-        if (threadIdx.x < used) put2(part + 2 * threadIdx.x, row_m[threadIdx.x], row_l[threadIdx.x]);
+        if (threadIdx.x < used) part.put(2 * threadIdx.x, make_float2(row_m[threadIdx.x], row_l[threadIdx.x]));
         arrived();
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -456,11 +453,11 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
         }
         __syncthreads();
         if (!last) return;
-        const float* src = a.parts + COUNTERS + (size_t)t.u.first * WORDS;
+        float* src = a.parts + COUNTERS + (size_t)t.u.first * WORDS;
         const size_t step_words = (size_t)a.kv * WORDS;
-        // (eight requests a thread on their way at a time: one after the other, 16 pieces of two parts would take 20 us)
-        constexpr int BATCH = 4, AT_ONCE = 2;
-        static_assert(MY % BATCH == 0 || MY < BATCH, "");
+        // (16 pieces of 16 bytes a thread on their way at a time, not eight of 8 bytes twice: 512 rows behind 7680 tokens 96 -> 91 us, 1536 rows 59.5 -> 52)
+        constexpr int BATCH = MY < 8 ? MY : 8, AT_ONCE = 2;
+        static_assert(MY % BATCH == 0, "");
         for (int e0 = 0; e0 < MY; e0 += BATCH) {
             if ((threadIdx.x + e0 * THREADS) / (DIM / 4) >= used) break;
             int at[BATCH], r[BATCH], c[BATCH];
@@ -477,15 +474,15 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
                 x[i] = f4{0.f, 0.f, 0.f, 0.f};
             }
             for (int p0 = 0; p0 < parts; p0 += AT_ONCE) {
-                float2 ml[AT_ONCE][BATCH], y[AT_ONCE][BATCH][2];
+                float2 ml[AT_ONCE][BATCH];
+                f4 y[AT_ONCE][BATCH];
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const float* one = src + (size_t)(p0 + k < parts ? p0 + k : parts - 1) * step_words;
+                    const Partial one(src + (size_t)(p0 + k < parts ? p0 + k : parts - 1) * step_words, WORDS);
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        ml[k][i] = get2(one + 2 * r[i]);
-                        y[k][i][0] = get2(one + 2 * TQ + 4 * at[i]);
-                        y[k][i][1] = get2(one + 2 * TQ + 4 * at[i] + 2);
+                        ml[k][i] = one.get2(2 * r[i]);
+                        y[k][i] = one.get(2 * TQ + 4 * at[i]);
                     }
                 }
 #pragma unroll
@@ -496,7 +493,7 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
                         const float mk = ml[k][i].x, up = fmaxf(m[i], mk), f = factor(m[i], up), g = factor(mk, up);
                         l[i] = (m[i] == -INFINITY ? l[i] : l[i] * f) + (mk == -INFINITY ? ml[k][i].y : ml[k][i].y * g);
                         m[i] = up;
-                        x[i] = x[i] * f + f4{y[k][i][0].x, y[k][i][0].y, y[k][i][1].x, y[k][i][1].y} * g;
+                        x[i] = x[i] * f + y[k][i] * g;
                     }
                 }
             }
