@@ -1,11 +1,11 @@
 """The attention half of a decoder layer, served to requests that have adapters of their own and share a paged cache.
 
-    python examples/attention_block.py [--requests 8] [--prompt 40] [--tokens 64] [--cache-bits 8]
+    python examples/attention_block.py [--requests 8] [--prompt 40] [--tokens 64] [--cache-bits 8 [--block-scales]] [--window 256 [--sinks 4]]
 
 Six calls a step:  q, k, v = compensated 4-bit linears of x (one launch)  ->  q += the request's own pair  ->  norm, rotation and store into the
-cache  ->  attention over the request's pages  ->  compensated output linear, += the request's own pair.  A prompt is a step whose rows are its
-tokens, each with the length that it may see; tokens after it are generated by replays of one captured graph, which
-moves positions, slots and lengths on by itself.  Weights and inputs are drawn.
+cache  ->  attention over the request's pages  ->  compensated output linear, += the request's own pair.  The prompts of all requests are one step, whose rows
+are their tokens; tokens after them are generated by replays of one captured graph, which moves positions, slots and lengths on by itself.  The cache holds fp16, or 8 bits with a scale a
+head (given) or for each 16 tokens of a head (found as they are stored).  Weights and inputs are drawn.
 """
 import argparse
 import os
@@ -55,7 +55,7 @@ class Pairs:
 
 
 class Block:
-    def __init__(self, requests, most_tokens, most_rows, cache_bits=16, seed=7):
+    def __init__(self, requests, most_tokens, most_rows, cache_bits=16, seed=7, block_scales=False, window=0, sinks=0):
         self.q, self.k, self.v, self.o = (Linear(seed + i, D, n) for i, n in enumerate((HEADS * DIM, KV * DIM, KV * DIM, D)))
         self.pairs_q, self.pairs_o = Pairs(seed + 4, D, HEADS * DIM), Pairs(seed + 5, HEADS * DIM, D)
         rng = np.random.default_rng(seed + 6)
@@ -69,30 +69,44 @@ class Block:
         self.n_pages, self.most_tokens = requests * self.width, most_tokens
         kind = torch.float16 if cache_bits == 16 else torch.uint8
         self.pages = [torch.zeros((self.n_pages, KV, PAGE, DIM), dtype=kind, device="cuda") for _ in range(2)]
-        # what a code of 1 stands for: keys are normed, so a few units at most; values have a deviation of 0.7
-        self.scales = [torch.full((KV,), s, device="cuda") for s in (0.02, 0.01)] if cache_bits == 8 else [None, None]
+        self.scale_block, self.window, self.sinks = 16 if block_scales else 0, window, sinks
+        if block_scales:
+            self.scales = [torch.zeros((self.n_pages, KV, PAGE // 16), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        else:                                        # what a code of 1 stands for: keys are normed, so a few units at most; values have a deviation of 0.7
+            self.scales = [torch.full((KV,), s, device="cuda") for s in (0.02, 0.01)] if cache_bits == 8 else [None, None]
         self.table = dev(rng.permutation(self.n_pages).astype(np.int32).reshape(requests, self.width))
         self.w_layer = eora.new_workspace(most_rows, D, D, RANK, n_members=3)
         self.w_pairs = eora.new_adapters_workspace(most_rows, D, D, PAIR_RANK)
-        self.w_attention = eora.new_attention_workspace(most_rows, HEADS, KV, DIM, self.width * PAGE)
+        self.w_attention = eora.new_attention_rows_workspace(most_rows, requests, HEADS, KV, DIM, self.width * PAGE)
 
     def slots(self, request, positions):
         return self.table[request.long(), (positions // PAGE).long()].long() * PAGE + positions % PAGE
 
-    def __call__(self, x, y, ids, positions, slots, lengths, table):
-        """x, y: rows x D; row m is token positions[m] of a request with the pages table[m], and sees lengths[m] tokens."""
-        M = x.shape[0]
+    def __call__(self, x, y, ids, positions, slots, lengths, starts=None):
+        """x, y: rows x D; rows starts[b] .. starts[b + 1] - 1 are the last tokens of request b, which has lengths[b] with them (None: a row each)."""
+        M, B = x.shape[0], self.table.shape[0]
         q, k, v = (torch.empty((M, n * DIM), dtype=torch.float16, device="cuda") for n in (HEADS, KV, KV))
         eora.linear_q_group(x, [self.q.member(q), self.k.member(k), self.v.member(v)], M, D, RANK, W_BITS, GROUP, 16, self.w_layer)
         eora.linear_adapters(x, self.pairs_q.A, self.pairs_q.B, None, None, None, None, ids, q, q, M, D, HEADS * DIM, PAIR_RANK, PAIRS, 16, self.w_pairs)
-        eora.cache_append(q, k, v, self.d_norms[0], self.d_norms[1], self.d_rotations, positions, slots, q, self.pages[0], self.pages[1], self.scales[0],
-                          self.scales[1], M, HEADS, KV, DIM, HEADS * DIM, KV * DIM, KV * DIM, DIM, False, self.most_tokens, EPS, self.n_pages, PAGE, self.bits)
+        rows = (q, k, v, self.d_norms[0], self.d_norms[1], self.d_rotations, positions, slots, q, *self.pages, *self.scales)
+        sizes = (M, HEADS, KV, DIM, HEADS * DIM, KV * DIM, KV * DIM, DIM, False, self.most_tokens, EPS, self.n_pages, PAGE)
+        if self.scale_block:
+            eora.cache_append_blocks(*rows, *sizes)
+        else:
+            eora.cache_append(*rows, *sizes, self.bits)
         out = torch.empty_like(q)
-        eora.cache_attention(q, self.pages[0], self.pages[1], self.scales[0], self.scales[1], table, lengths, out, None, M, HEADS, KV, DIM, HEADS * DIM,
-                             self.n_pages, PAGE, self.bits, self.width, 0, SCALE, self.w_attention)
+        eora.cache_attention_rows(q, *self.pages, *self.scales, self.table, lengths, starts, out, None, M, B, HEADS, KV, DIM, HEADS * DIM, self.n_pages, PAGE, self.bits,
+                                  self.scale_block, self.width, self.window, self.sinks, SCALE, self.w_attention)
         o = self.o
         eora.linear_q(out, *o.stored, None, None, y, M, o.d_in, o.d_out, RANK, W_BITS, GROUP, 16, self.w_layer)
         eora.linear_adapters(out, self.pairs_o.A, self.pairs_o.B, None, None, None, None, ids, y, y, M, o.d_in, o.d_out, PAIR_RANK, PAIRS, 16, self.w_pairs)
+
+    def cached(self, request, tokens):
+        """The first tokens of a request as the cache has them: keys and values, tokens x KV x DIM."""
+        k, v = (torch.empty((tokens, KV, DIM), dtype=torch.float16, device="cuda") for _ in range(2))
+        slots = self.slots(torch.tensor(request, device="cuda"), torch.arange(tokens, device="cuda"))
+        eora.cache_read(*self.pages, *self.scales, slots, k, v, tokens, KV, DIM, self.n_pages, PAGE, self.bits, self.scale_block)
+        return k, v
 
     def check(self):
         eora.workspace_error(self.w_layer)
@@ -108,9 +122,9 @@ def following(x, y):
 class Server:
     """Requests with one prompt length, each with an adapter or none."""
 
-    def __init__(self, requests, prompt, tokens, cache_bits=16):
+    def __init__(self, requests, prompt, tokens, cache_bits=16, **options):
         self.n, self.prompt_tokens = requests, prompt
-        self.block = Block(requests, prompt + tokens, max(requests, prompt), cache_bits)
+        self.block = Block(requests, prompt + tokens, requests * prompt, cache_bits, **options)
         rng = np.random.default_rng(3)
         self.x_prompt = dev(rng.standard_normal((requests, prompt, D)).astype(np.float16))
         self.ids = torch.arange(requests, dtype=torch.int32, device="cuda") % (PAIRS + 1) - 1       # -1: no adapter
@@ -121,19 +135,18 @@ class Server:
         self.graph = None
 
     def prompt(self):
-        """All prompts, one after the other; returns y of their tokens."""
+        """All prompts at once; returns y of their tokens."""
         P, b = self.prompt_tokens, self.block
-        places = torch.arange(P, dtype=torch.int32, device="cuda")
+        request, places = self.request.repeat_interleave(P), torch.arange(P, dtype=torch.int32, device="cuda").repeat(self.n)
+        starts = torch.arange(self.n + 1, dtype=torch.int32, device="cuda") * P
         ys = torch.empty_like(self.x_prompt)
-        for i in range(self.n):
-            request = self.request[i].expand(P).contiguous()
-            b(self.x_prompt[i], ys[i], self.ids[i].expand(P).contiguous(), places, b.slots(request, places), places + 1, b.table[i].expand(P, -1).contiguous())
+        b(self.x_prompt.view(-1, D), ys.view(-1, D), self.ids.repeat_interleave(P), places, b.slots(request, places), torch.full_like(self.request, P), starts)
         self.x.copy_(following(self.x_prompt[:, -1], ys[:, -1]))
         return ys
 
     def token(self):
         b = self.block
-        b(self.x, self.y, self.ids, self.positions, b.slots(self.request, self.positions), self.positions + 1, b.table)
+        b(self.x, self.y, self.ids, self.positions, b.slots(self.request, self.positions), self.positions + 1)
         self.x.copy_(following(self.x, self.y))
         self.positions.add_(1)
 
@@ -150,8 +163,13 @@ def main():
     ap.add_argument("--prompt", type=int, default=40)
     ap.add_argument("--tokens", type=int, default=64)
     ap.add_argument("--cache-bits", type=int, default=16, choices=(16, 8))
+    ap.add_argument("--block-scales", action="store_true", help="8 bits: a scale for each 16 tokens of a head, found as they are stored")
+    ap.add_argument("--window", type=int, default=0, help="tokens that a token sees, 0: all")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible beside the window")
     args = ap.parse_args()
-    s = Server(args.requests, args.prompt, args.tokens, args.cache_bits)
+    if args.block_scales and args.cache_bits != 8:
+        ap.error("--block-scales: with --cache-bits 8")
+    s = Server(args.requests, args.prompt, args.tokens, args.cache_bits, block_scales=args.block_scales, window=args.window, sinks=args.sinks)
     s.prompt()
     s.token()
     s.capture()

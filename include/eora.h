@@ -436,8 +436,9 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  *      t <= p  with  t > p - window  or  t < sinks          (window 0: all t <= p),
  * for query head i of kv head i / (n_heads / n_kv_heads) as in eora_cache_attention(), with pages, scores and lse as there.  A row that sees nothing (a position below 0, all
  * masked) has out = 0 and lse = -inf.  What a row does not see is never used for it, NaN and infinities included, also where other rows see it.
- * A value that is not finite makes its column of out infinite or NaN for the rows that see it.
- * row_starts: B + 1 int32, not decreasing, taken as 0 .. M; rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
+ * A value that is not finite makes its column of out infinite or NaN for the rows that see it (where its score is -inf, it may or may not).
+ * row_starts: B + 1 int32, not decreasing (where they decrease, out and lse are undefined, and the workspace's first 48 KiB have to be zeroed before the next call), taken as 0 .. M;
+ * rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
  * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.
  * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits in the form for single tokens,
  * else as one fp16 (rounded to nearest, the largest 2^11 or more).  Equal inputs give bit-equal outputs; how tokens are split between workgroups, and so the last bits, depends on

@@ -8,7 +8,9 @@
 // that become subnormal.  From 2^-15 on every code stands for a number that fp16 holds (the least step is 2^-24), up to 2^8 as well with codes to 240 there: whatever reads
 // the cache converts without a rounding, and no scale has to be carried through a sum.
 //
-// Bound by memory for many tokens, by the time of its dependent reads (slots, rows, the block's scale) for few.  Queries: a workgroup for a token, as where nothing is scaled by blocks.
+// Bound by memory for many tokens, by the time of its dependent reads (slots, rows, the block's scale) for few: 8192 tokens of 64 + 8 + 8 heads of 128, with norm, stored and read back
+// (373 MB) in 78.7 us, 4.7 TB/s, as a copy; one token in 12 (two launches).  Queries: a workgroup for a token, as where nothing is scaled by blocks, behind all keys and
+// values, whose chains are longer (85.4 us with them last).
 // Keys and values: a wavefront for a block of a head, in registers (8 to 64 values a lane), so that the block's largest value is known before anything is stored and every value is read once.
 // Who handles a block: the first of its rows, which are among 16 consecutive rows of the call; a wavefront looks through some rows for first ones (one row where there
 // are few, so that requests with one new token each run side by side; up to 16, a block of a prompt).
@@ -177,6 +179,7 @@ __device__ __forceinline__ void blocks_of(const BlocksArgs& a, int r0, int h, bo
         for (int t = 0; t < TPS; ++t) {
             const int lane_of = __shfl(from, sub + SUBS * t, 64);
             has[t] = lane_of > 0;
+            if (__ballot(has[t]) == 0) continue;                                // (single tokens: 1024 requests 13.3 us, without this 22.5)
             const int token = has[t] ? r0 - LOOK + lane_of - 1 : r0 - LOOK + i;
             col.fetch(x_rows + (size_t)token * stride + (size_t)h * DIM, x[t]);
             if (weight) C::norm(x[t], w, a.eps);
@@ -216,18 +219,19 @@ __device__ __forceinline__ void blocks_of(const BlocksArgs& a, int r0, int h, bo
     }
 }
 
+// (Seven wavefronts a SIMD: reads of a block's rows on their way together take registers of which only three are left, 8192 tokens 78.7 -> 97 us; six 81.)
 template <int DIM, bool INTERLEAVED>
-__global__ __launch_bounds__(THREADS) void append_blocks_kernel(const BlocksArgs a)
+__global__ __launch_bounds__(THREADS, DIM == 256 ? 4 : 7) void append_blocks_kernel(const BlocksArgs a)
 {
-    const unsigned first = (unsigned)a.tokens * (unsigned)a.slices;             // workgroups of queries
-    if (blockIdx.x < first) {
-        const unsigned token = blockIdx.x / (unsigned)a.slices;
-        queries<DIM, INTERLEAVED>(a, a.m0 + (int)token, (int)(blockIdx.x - token * (unsigned)a.slices));
+    const unsigned groups = (unsigned)((a.tokens + a.look - 1) / a.look), first = (groups * 2u * (unsigned)a.kv + NW - 1) / NW;       // workgroups of keys and values
+    if (blockIdx.x >= first) {
+        const unsigned id = blockIdx.x - first, token = id / (unsigned)a.slices;
+        queries<DIM, INTERLEAVED>(a, a.m0 + (int)token, (int)(id - token * (unsigned)a.slices));
         return;
     }
-    const unsigned unit = (blockIdx.x - first) * NW + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = 2u * (unsigned)a.kv;
+    const unsigned unit = blockIdx.x * NW + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = 2u * (unsigned)a.kv;
     const unsigned group = unit / heads, h = unit - group * heads;
-    if (group >= (unsigned)((a.tokens + a.look - 1) / a.look)) return;
+    if (group >= groups) return;
     blocks_of<DIM, INTERLEAVED>(a, a.m0 + (int)group * a.look, (int)(h % (unsigned)a.kv), h >= (unsigned)a.kv);
 }
 
@@ -286,8 +290,9 @@ hipError_t launch_append_blocks(BlocksArgs a, hipStream_t stream)
         a.tokens = a.M - a.m0 < LAUNCH ? a.M - a.m0 : LAUNCH;
         a.slices = (1024 + a.tokens - 1) / a.tokens;
         a.slices = a.slices > most ? most : a.slices;
-        // wavefronts enough for the chip, then rows for each
-        const size_t look = (size_t)a.tokens * 2 * a.kv / 8192;
+        // wavefronts enough for the chip, then rows for each (32 + 8 + 8 heads of 128, prompts of 1024, 2048, 4096 tokens: with 8192 wavefronts 16.6, 18.0, 28.2 us, with 4096 10.9, 13.7,
+        // 22.7, with 2048 10.3, 12.5, 23.5, but a token of each of 1024 requests then 19.8, not 13.4)
+        const size_t look = (size_t)a.tokens * 2 * a.kv / 4096;
         a.look = look < 1 ? 1 : (look > BLOCK_TOKENS ? BLOCK_TOKENS : (int)look);
         const size_t units = (size_t)((a.tokens + a.look - 1) / a.look) * 2 * a.kv, grid = (size_t)a.tokens * a.slices + (units + NW - 1) / NW;
         if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
