@@ -255,3 +255,30 @@ def test_read(gpu, kv, dim, page, form):
             with np.errstate(over="ignore"):
                 assert np.array_equal(got[m], exact.astype(np.float16), equal_nan=True) if form != "heads" else np.all(
                     (np.abs(got[m] - exact) <= U * 1.001 * np.abs(exact) + TINY) | (np.isnan(got[m]) & np.isnan(exact)) | (np.abs(exact) >= 65500)), "row %d" % m
+
+
+def test_more_rows_than_a_launch_takes(gpu):
+    """2^18 rows are a launch: a block whose rows are in two of them, and all behind it, are as a call with the last rows alone stores them."""
+    import torch
+    M, page, dim = (1 << 18) + 40, 16, 64
+    first = (1 << 18) - 9 - 32                               # a row whose slot, 9 further on, begins a block
+    pages = (M + 9) // page + 1
+    torch.manual_seed(3)
+    q, k, v = (torch.randn((M, dim), device="cuda").half() for _ in range(3))
+    slots = torch.arange(9, M + 9, device="cuda")
+    assert int(slots[first]) % 16 == 0
+    results = []
+    for m in (0, first):
+        cache = [torch.full((pages, 1, page, dim), 0x38, dtype=torch.uint8, device="cuda") for _ in range(2)] + [torch.full((pages, 1, 1), 120, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        out = torch.empty_like(q[m:])
+        gpu.cache_append_blocks(q[m:], k[m:], v[m:], None, None, None, None, slots[m:], out, *cache, M - m, 1, 1, dim, dim, dim, dim, 0, False, 0, 0.0, pages, page)
+        torch.cuda.synchronize()
+        begin = int(slots[first]) // page
+        results.append([out[first - m:]] + [c[begin:] for c in cache])
+        if m == 0:                                           # and all of the first rows came there: codes of values whose largest is 448 2^e at most, 224 2^e at least
+            got = [torch.empty((M, 1, dim), dtype=torch.float16, device="cuda") for _ in range(2)]
+            gpu.cache_read(*cache, slots, *got, M, 1, dim, pages, page, 8, 16)
+            for x, y in zip((k, v), got):                    # half a step of a code, 2^-4, or half of the least step 2^(e - 9), e <= -6 for |x| < 7
+                assert torch.all((x - y[:, 0]).abs() <= torch.maximum(x.abs() * 2.0 ** -4, torch.tensor(2.0 ** -16, device="cuda")))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
