@@ -49,10 +49,11 @@ struct Narrow {
 constexpr int CUS = 256;
 // Workgroups a compute unit has at a time, as registers and LDS allow
 constexpr int residents(int dim) { return dim == 256 ? 1 : 2; }
-// Parts that all tiles together are cut into at least, where they have the work (as many as the chip has at a time: 32 requests of 5 rows of 4096 tokens, heads of 256 in 8 bits, with
-// twice as many 157 us, with these 136); partial results that there are: see share_of()
+// Parts that all tiles that are cut have together, where they have the work: as many as the chip has at a time (32 requests of 5 rows of 4096 tokens, heads of 256 in 8 bits, with twice as many
+// 157 us, with these 136); room for an eighth more
 constexpr int want_of(int dim) { return CUS * residents(dim); }
-constexpr int MAX_PARTS = 2 * want_of(128);
+constexpr int most_of(int dim) { return want_of(dim) * 9 / 8; }
+constexpr int MAX_PARTS = most_of(128);
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr float RAISE = 4.f, LOWER = 11.f;
@@ -117,18 +118,19 @@ struct Unit {
     int b, h, tile, part, parts;
     int place, first;
 };
-// Tiles of a request are cut into ceil(cost / share) parts, share = a want_of(dim)-th of all work or a little more: with parts > 1 a request has less than 2 cost / share, so all of
-// them have at most twice as many parts.  All tiles alike, as if each saw as much as the last (each by what it sees: 1536 rows of 32 / 8 heads 52 -> 47.6 us, but 2048 rows, whose tiles fill
-// the chip once, 56 -> 67: parts that then wait for a place).
-// (The work is added up in floats, in one order: everyone finds the same share.  What is added covers their roundings, at most 50 of 2^-24.)
+// Tiles of a request are cut into cost / share parts, rounded down, up from an eighth below: share = a want_of(dim)-th of all work, so all of them have hardly more parts than the chip
+// holds workgroups.  (Rounded up, parts that do not fit wait for others to end: 1536 rows of 32 / 8 heads 52 us, these 42; always rounded down, 11 requests of 200 rows and 2000 tokens with a window of
+// 1000, 1.94 shares each, 15 / 3 heads of 64: 51 us, these 43.  All tiles of a request alike, as if each saw as much as the last: each by what
+// it sees, 2048 rows, whose tiles fill the chip once, would take 67 in place of 56.)
+// The work is added up in floats, in one order: everyone finds the same parts.  With two or more of them cost / share is 1.875 or more: together they are 1.07 want_of(dim) at most.
 template <typename SHAPE>
-__device__ __forceinline__ int share_of(const PromptArgs& a, float work)
+__device__ __forceinline__ float shares_of(const PromptArgs& a, float work) { return (float)want_of(a.dim) / fmaxf(work * (float)a.kv, 1.f); }
+template <typename SHAPE>
+__device__ __forceinline__ int parts_of(const Request& r, float shares)
 {
-    const float x = work * (float)a.kv * (1.0001f / (float)want_of(a.dim));
-    const int share = x < 1e9f ? (int)x + 1 : 0x7fffffff;
-    return share < SHAPE::LEAST_PART ? SHAPE::LEAST_PART : share;
+    const int most = (r.cost + SHAPE::LEAST_PART - 1) / SHAPE::LEAST_PART, parts = (int)fminf(__builtin_fmaf((float)r.cost, shares, 0.125f), (float)MAX_PARTS);
+    return parts < 1 ? 1 : (parts < most ? parts : most);
 }
-__device__ __forceinline__ int parts_of(const Request& r, int share) { return r.cost <= share ? 1 : (int)((unsigned)(r.cost - 1) / (unsigned)share) + 1; }
 __device__ __forceinline__ Unit unit_in(const PromptArgs& a, const Request& r, int b, int parts, int local, int cut)
 {
     Unit u;
@@ -166,8 +168,8 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
     const int lane = threadIdx.x & 63;
     Request r = request_of<SHAPE>(a, lane < a.B ? lane : a.B - 1);
     if (lane >= a.B) r.tiles = 0;
-    const int share = share_of<SHAPE>(a, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)));
-    const int parts = parts_of(r, share), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
+    const float shares = shares_of<SHAPE>(a, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)));
+    const int parts = parts_of<SHAPE>(r, shares), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
     const int v = scan(units), c = scan(cut);
     const unsigned long long mine = __ballot(id >= v - units && id < v);
     if (mine == 0) return false;
@@ -202,14 +204,14 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     work = 0.f;
 #pragma unroll
     for (int w = 0; w < RG; ++w) work += sums[w];
-    const int share = share_of<SHAPE>(a, work);
+    const float shares = shares_of<SHAPE>(a, work);
     int before = 0, cut_before = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int units = 0, cut = 0;
         if (b < a.B) {
             const Request r = request_of<SHAPE>(a, b);
-            const int parts = parts_of(r, share);
+            const int parts = parts_of<SHAPE>(r, shares);
             units = r.tiles * parts * a.kv;
             cut = parts > 1 ? units : 0;
         }
@@ -247,7 +249,7 @@ __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, in
     r.rows = __builtin_amdgcn_readfirstlane(r.rows);
     r.tiles = __builtin_amdgcn_readfirstlane(r.tiles);
     r.cost = __builtin_amdgcn_readfirstlane(r.cost);
-    u = unit_in(a, r, b, parts_of(r, share), __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[2]));
+    u = unit_in(a, r, b, parts_of<SHAPE>(r, shares), __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[2]));
     return true;
 }
 
@@ -1055,7 +1057,7 @@ size_t prompt_workspace_bytes(int dim)
     // (a workspace for wide heads also serves narrower ones, of which there are more at a time)
     size_t words = 0;
     for (int d = 64; d <= dim; d *= 2) {
-        const size_t one = 2 * (size_t)want_of(d) * part_words<Wide>(d);
+        const size_t one = (size_t)most_of(d) * part_words<Wide>(d);
         words = one > words ? one : words;
     }
     return (COUNTERS + words) * sizeof(float);
