@@ -3,8 +3,8 @@
 //      s_rt = scale q_r . k_t,   out_r = sum_t 2^(s_rt log2 e - m) v_t / sum_t 2^(s_rt log2 e - m)      t <= p_r, and t > p_r - window or t < sinks
 //
 // Row r of a request's n sits at p_r = length - n + r.  Bound by the matrix instructions where there are many rows (4 dim flops for each pair of a query head's row and a token), by memory
-// where there are few.  64 / 8 heads of 128: 8192 rows in fp16 in 1118 us, 984 TF; 32 / 8 heads: 2048 rows in 58 us in fp16, 66 in 8 bits; 32 requests of 5 rows and 8192 tokens in 8 bits
-// (537 MB) in 107 us, 5.1 TB/s; 17 rows of 17 in 9 us.
+// where there are few.  64 / 8 heads of 128: 8192 rows in fp16 in 1120 us, 982 TF (on a card where a large matrix product reaches 1470); 32 / 8 heads: 2048 rows in 56 us in fp16, 67 in 8 bits;
+// 32 requests of 5 rows and 8192 tokens in 8 bits (537 MB) in 107 us, 5.1 TB/s; 17 rows of 17 in 9 us.
 //
 // Tile: 128 pairs of a row and a query head of one kv head (32 a wavefront) by 64 keys.  A column of the matrix instructions is a pair, all query heads of a kv head share the keys.
 // S^T = K Q^T (32 x 32 x 16): a lane holds one pair's scores of 16 keys of 32, so that softmax needs no exchange between lanes but one of the largest score, and the scores are,
@@ -15,8 +15,8 @@
 //
 // A step: the scores of the next tile beside the softmax of this one, then this one's O, one matrix instruction a slot in an order that the compiler keeps, operands read four ahead (left to itself it
 // reads one, waits, multiplies: 1418 us -> 1395).  Alone on its compute unit a workgroup takes 2860 cycles a step, 1024 of matrix instructions: 740 before the first (scalar work, masks, the
-// first operands), 1340 beside the softmax, 580 beside V, 210 for tiles and the barrier.  So there are two workgroups a compute unit, which fill each other's gaps (8192 rows: 53 % of the
-// cycles have a matrix instruction).  What did not help: two teams of wavefronts on one tile of pairs (1378 us), eight wavefronts on tiles of 256 (1206, and 71 where 2048 rows take 59), 64 pairs a wavefront
+// first operands), 1340 beside the softmax, 580 beside V, 210 for tiles and the barrier.  So there are two workgroups a compute unit, which fill each other's gaps (8192 rows: 56 % of the
+// cycles have a matrix instruction, at a clock that the card's power holds at 1.6 GHz; a workgroup alone on a chip three quarters idle takes 1.02 us a step, all together 1.05 a step and compute unit).  What did not help: two teams of wavefronts on one tile of pairs (1378 us), eight wavefronts on tiles of 256 (1206, and 71 where 2048 rows take 59), 64 pairs a wavefront
 // (twice the work for an operand, one wavefront a SIMD: 1.4 times as long), O one step later (registers), waits of a step and a half for tiles, scalar work between the matrix instructions.
 //
 // Few rows: tiles of 32 pairs by 32 keys (few_kernel() below).
