@@ -443,7 +443,7 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits in the form for single tokens,
  * else as one fp16 (rounded to nearest, the largest 2^11 or more).  Equal inputs give bit-equal outputs; how tokens are split between workgroups, and so the last bits, depends on
  * the lengths and rows of all requests.
- * workspace: eora_cache_attention_rows_workspace_bytes() of the largest call (max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the first call, the rest
+ * workspace: eora_cache_attention_rows_workspace_bytes() of the largest call (B, heads, head_dim; max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the first call, the rest
  * may hold anything; every call leaves it usable for the next, of whatever sizes and of either form.
  * Constraints: M >= 0, 0 <= B <= 8192 (M or B 0: no-op), n_heads % n_kv_heads == 0, q_stride % 8 == 0, max_pages >= 1, max_pages * page_size <= 2^30,
  * window >= 0, sinks >= 0, scale finite; with row_starts M * (n_heads / n_kv_heads) < 2^31, M * n_heads / 32 + B * n_kv_heads < 8e6 and

@@ -56,6 +56,7 @@ constexpr int most_of(int dim) { return want_of(dim) * 9 / 8; }
 constexpr int MAX_PARTS = most_of(128);
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
+constexpr int PLAN_BYTES = 32;                 // of a request's plan, behind the partial results
 constexpr float RAISE = 4.f, LOWER = 11.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -184,73 +185,88 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
     u = unit_in(a, q, b, of(parts), id - of(v - units), of(c - cut));
     return true;
 }
-// Any number of them: all threads, a request each at a time.
+// More of them: a launch before this one has written down for each request where its units end and what they are, each wavefront looks for its own.  (In place of every workgroup adding up
+// all requests for itself: 5 rows of each of 128, 512, 2048 requests of 100 tokens,
+// 32 / 8 heads of 128 in 8 bits, 26, 105, 593 -> 25, 83, 304 us.)
+struct Planned {
+    int4 at, what;                             // end of its units, parts before it, n, first; rows, tiles, parts, cost
+};
+static_assert(sizeof(Planned) == PLAN_BYTES, "");
+constexpr int PLAN_THREADS = 1024;
 template <typename SHAPE>
-__device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u, int* scratch)
+__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(const PromptArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float* sums = (float*)scratch;                                              // RG
-    int* found = scratch + RG;                                                  // b, id within the request, parts before
-    int* totals = found + 4;                                                    // 2 RG
+    constexpr int WAVES = PLAN_THREADS / 64;
+    __shared__ float sums[WAVES];
+    __shared__ int totals[WAVES][2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, each = (a.B + PLAN_THREADS - 1) / PLAN_THREADS;
+    const int b0 = threadIdx.x * each < a.B ? threadIdx.x * each : a.B, b1 = b0 + each < a.B ? b0 + each : a.B;
     float work = 0.f;
-    for (int b = threadIdx.x; b < a.B; b += THREADS) {
+    for (int b = b0; b < b1; ++b) {
         const Request r = request_of<SHAPE>(a, b);
         work += (float)r.tiles * (float)r.cost;
     }
     work = scan(work);
     if (lane == 63) sums[wave] = work;
-    if (threadIdx.x == 0) found[0] = -1;
     __syncthreads();
     work = 0.f;
-#pragma unroll
-    for (int w = 0; w < RG; ++w) work += sums[w];
+    for (int w = 0; w < WAVES; ++w) work += sums[w];
     const float shares = shares_of<SHAPE>(a, work);
-    int before = 0, cut_before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        const int b = b0 + (int)threadIdx.x;
-        int units = 0, cut = 0;
-        if (b < a.B) {
-            const Request r = request_of<SHAPE>(a, b);
-            const int parts = parts_of<SHAPE>(r, shares);
-            units = r.tiles * parts * a.kv;
-            cut = parts > 1 ? units : 0;
-        }
-        int v = scan(units), c = scan(cut);
-        if (lane == 63) {
-            totals[2 * wave] = v;
-            totals[2 * wave + 1] = c;
-        }
-        __syncthreads();
-        int sum = 0, cut_sum = 0;
-#pragma unroll
-        for (int w = 0; w < RG; ++w) {
-            v += w < wave ? totals[2 * w] : 0;
-            c += w < wave ? totals[2 * w + 1] : 0;
-            sum += totals[2 * w];
-            cut_sum += totals[2 * w + 1];
-        }
-        v += before;
-        c += cut_before;
-        if (id >= v - units && id < v) {
-            found[0] = b;
-            found[1] = id - (v - units);
-            found[2] = c - cut;
-        }
-        before += sum;
-        cut_before += cut_sum;
-        __syncthreads();
-        if (id < before) break;
+    int units = 0, cut = 0;
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_of<SHAPE>(a, b);
+        const int parts = parts_of<SHAPE>(r, shares);
+        units += r.tiles * parts * a.kv;
+        cut += parts > 1 ? r.tiles * parts * a.kv : 0;
     }
-    const int b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (b < 0) return false;
-    Request r = request_of<SHAPE>(a, b);
-    r.n = __builtin_amdgcn_readfirstlane(r.n);
-    r.first = __builtin_amdgcn_readfirstlane(r.first);
-    r.rows = __builtin_amdgcn_readfirstlane(r.rows);
-    r.tiles = __builtin_amdgcn_readfirstlane(r.tiles);
-    r.cost = __builtin_amdgcn_readfirstlane(r.cost);
-    u = unit_in(a, r, b, parts_of<SHAPE>(r, shares), __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[2]));
-    return true;
+    const int v = scan(units), c = scan(cut);
+    if (lane == 63) {
+        totals[wave][0] = v;
+        totals[wave][1] = c;
+    }
+    __syncthreads();
+    int end = v - units, before = c - cut;
+    for (int w = 0; w < wave; ++w) {
+        end += totals[w][0];
+        before += totals[w][1];
+    }
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_of<SHAPE>(a, b);
+        const int parts = parts_of<SHAPE>(r, shares), mine = r.tiles * parts * a.kv;
+        end += mine;
+        Planned& to = ((Planned*)a.plan)[b];
+        to.at = make_int4(end, before, r.n, r.first);
+        to.what = make_int4(r.rows, r.tiles, parts, r.cost);
+        before += parts > 1 ? mine : 0;
+    }
+}
+__device__ __forceinline__ bool unit_planned(const PromptArgs& a, int id, Unit& u)
+{
+    const Planned* plan = (const Planned*)a.plan;
+    const int lane = threadIdx.x & 63, each = (a.B + 63) / 64;
+    // the first of 64 stretches of requests that ends behind this unit, then the first request of it
+    const int stop = (lane + 1) * each < a.B ? (lane + 1) * each : a.B;
+    const unsigned long long stretches = __ballot(id < plan[stop - 1].at.x);
+    if (stretches == 0) return false;
+    const int begin = __builtin_ctzll(stretches) * each;
+    for (int b0 = begin; b0 < begin + each; b0 += 64) {
+        const int b = b0 + lane < a.B ? b0 + lane : a.B - 1;
+        const int4 at = plan[b].at, what = plan[b].what;
+        const unsigned long long mine = __ballot(id < at.x);
+        if (mine == 0) continue;               // (a stretch of more than 64 requests)
+        const int from = __builtin_ctzll(mine);
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
+        Request r;
+        r.n = of(at.z);
+        r.first = of(at.w);
+        r.rows = of(what.x);
+        r.tiles = of(what.y);
+        r.cost = of(what.w);
+        const int parts = of(what.z);
+        u = unit_in(a, r, b0 + from, parts, id - (of(at.x) - r.tiles * parts * a.kv), of(at.y));
+        return true;
+    }
+    return false;
 }
 
 // Stores and loads of partial results go past the caches of an XCD (agent scope: SC1), 16 bytes each, or a pair
@@ -327,9 +343,9 @@ struct Tile {
     int lo, hi, sinks, first, head;            // tokens that some row sees: [lo, hi) and those before `sinks`; tiles of keys: those from `first` on, behind `head` of the first
     int parts, k0, k1;                         // tiles [k0, k1) of them are this workgroup's
     const int* table;
-    __device__ __forceinline__ bool find(const PromptArgs& a, int id, int* scratch)
+    __device__ __forceinline__ bool find(const PromptArgs& a, int id)
     {
-        if (!(a.B <= 64 ? unit_of_few<SHAPE>(a, id, u) : unit_of<SHAPE>(a, id, u, scratch))) return false;
+        if (!(a.B <= 64 ? unit_of_few<SHAPE>(a, id, u) : unit_planned(a, id, u))) return false;
         group = a.heads / a.kv;
         const int pairs = u.r.rows * group;
         from = u.r.n - u.r.rows;
@@ -557,13 +573,12 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     constexpr int AHEAD = 4;                   // matrix instructions between an operand's read and its use
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    __shared__ int scratch[RG + 4 + 2 * RG];
     __shared__ int odd_one;                    // some value that not all rows see is not finite
     __shared__ int last;
     __shared__ float row_m[TQ], row_l[TQ];
 
     Tile<Wide> tile;
-    if (!tile.find(a, (int)blockIdx.x, scratch)) return;
+    if (!tile.find(a, (int)blockIdx.x)) return;
     const Unit& u = tile.u;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int steps = tile.k1 - tile.k0;
@@ -840,12 +855,11 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
     constexpr int BYTES = DIM * BITS / 8, PIECES = BLOCK_TOKENS * BYTES / 1024, PR = BYTES / 16, ROWS = 64 / PR;      // of a row in memory; KiB of 16 keys; pieces of a row, rows of a KiB
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    __shared__ int scratch[RG + 4 + 2 * RG];
     __shared__ int odd_one, last;
     __shared__ float red_m[RG][TQ], red_l[RG][TQ], row_m[TQ], row_l[TQ];
 
     Tile<Narrow> tile;
-    if (!tile.find(a, (int)blockIdx.x, scratch)) return;
+    if (!tile.find(a, (int)blockIdx.x)) return;
     const Unit& u = tile.u;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int mine = (tile.k1 - tile.k0 - wave + RG - 1) / RG;                   // tiles of keys
@@ -1037,6 +1051,12 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
     if constexpr (DIM < 256 || BITS == 8) kern = few ? few_kernel<DIM, BITS, BLOCKS> : kern;
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
+    if (a.B > 64) {
+        if (few) plan_kernel<Narrow><<<1, PLAN_THREADS, 0, stream>>>(a);
+        else plan_kernel<Wide><<<1, PLAN_THREADS, 0, stream>>>(a);
+        const hipError_t p = hipGetLastError();
+        if (p != hipSuccess) return p;
+    }
     kern<<<(unsigned)units_of(a.M, a.B, a.heads, a.kv, few ? Narrow::TQ : Wide::TQ), THREADS, lds, stream>>>(a);
     return hipGetLastError();
 }
@@ -1052,9 +1072,9 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
 
 long long prompt_units(int M, int B, int heads, int kv) { return units_of(M, B, heads, kv, Narrow::TQ); }
 
-size_t prompt_workspace_bytes(int dim)
+// bytes before the plan: counters, partial results (a workspace for wide heads also serves narrower ones, of which there are more at a time)
+static size_t before_plan(int dim)
 {
-    // (a workspace for wide heads also serves narrower ones, of which there are more at a time)
     size_t words = 0;
     for (int d = 64; d <= dim; d *= 2) {
         const size_t one = (size_t)most_of(d) * part_words<Wide>(d);
@@ -1062,9 +1082,11 @@ size_t prompt_workspace_bytes(int dim)
     }
     return (COUNTERS + words) * sizeof(float);
 }
+size_t prompt_workspace_bytes(int B, int dim) { return before_plan(dim) + (size_t)B * PLAN_BYTES; }
 
-hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream)
+hipError_t launch_prompt(PromptArgs a, hipStream_t stream)
 {
+    a.plan = (char*)a.parts + before_plan(a.dim);
     return a.dim == 64 ? start<64>(a, stream) : (a.dim == 128 ? start<128>(a, stream) : start<256>(a, stream));
 }
 

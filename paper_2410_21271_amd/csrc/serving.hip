@@ -288,7 +288,7 @@ size_t eora_cache_attention_rows_workspace_bytes(int M, int B, int n_heads, int 
 {
     const size_t tokens = eora_cache_attention_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_tokens);       // (single tokens: checks of all but M)
     if (tokens == 0 || M < 0) return 0;
-    const size_t rows = round256(prompt_workspace_bytes(head_dim));
+    const size_t rows = round256(prompt_workspace_bytes(B, head_dim));
     return rows > tokens ? rows : tokens;
 }
 

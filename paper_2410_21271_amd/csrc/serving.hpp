@@ -116,12 +116,13 @@ struct PromptArgs {
     _Float16* out;                  // M x heads x dim
     float* lse;                     // M x heads, or null
     float* parts;                   // arrival counters, partial results of tiles that several workgroups share
+    void* plan;                     // (set by the launcher) of many requests: their units
     int M, B, heads, kv, dim, q_stride, n_pages, page, bits, width, window, sinks;
     float scale;
 };
-size_t prompt_workspace_bytes(int dim);
+size_t prompt_workspace_bytes(int B, int dim);
 long long prompt_units(int M, int B, int heads, int kv);               // workgroups of a launch at most
-hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream);
+hipError_t launch_prompt(PromptArgs a, hipStream_t stream);
 
 struct AdapterArgs {
     const _Float16* x;              // M x d_in

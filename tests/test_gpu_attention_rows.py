@@ -236,6 +236,16 @@ def test_many_requests(gpu):
     Rows(36, [(n, 1) for n, _ in sizes], 2, 1, 64, "blocks", 16, single=True).check(gpu, 9, 3)
 
 
+@pytest.mark.parametrize("requests, heads, kv, dim, form", [
+    ([(40 + i % 7, 33 + i % 9) for i in range(66)], 8, 2, 64, "fp16"),                                     # tiles of many rows
+    ([(60, 40)] * 40 + [(900, 90)] + [(5, 0), (0, 0)] * 10 + [(1500, 1)] * 9, 8, 2, 128, "blocks"),        # some of them cut along the keys
+    ([(20, 2)] * 68 + [(9000, 3)] + [(30, 1)] * 5, 4, 1, 64, "fp16"),                                       # few rows, one request cut
+    ([(i % 5, i % 3) for i in range(4170)], 2, 1, 64, "fp16"),                                              # more than 64 in each of 64 stretches
+    ([(3, 1)] * 65, 1, 1, 256, "heads")])
+def test_more_requests_than_a_wavefront_plans(gpu, requests, heads, kv, dim, form):
+    Rows(61, requests, heads, kv, dim, form, 16).check(gpu)
+
+
 def test_lengths_beyond_the_table_and_missing_pages(gpu):
     for dim, form in ((64, "fp16"), (128, "blocks"), (256, "heads")):
         c = Rows(37, [(90, 50), (64, 3), (33, 33), (50, 20)], 4, 2, dim, form, 16, width=6)
