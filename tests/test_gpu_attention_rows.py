@@ -146,7 +146,7 @@ SHAPES = [
 ]
 
 
-# 2^17 pairs of a row and a query head and more: tiles of 256
+# many query heads: tiles of many pairs
 MANY = [
     ([(300, 200), (77, 30), (1, 1), (64, 34)], 512, 1, 64, "fp16", 16),
     ([(257, 150), (40, 50), (120, 80)], 480, 2, 128, "fp16", 48),
