@@ -1035,15 +1035,18 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
 long long units_of(int M, int B, int heads, int kv, int tq) { return (((long long)M * (heads / kv) + tq - 1) / tq + B) * kv + MAX_PARTS; }
 
 // Narrow tiles up to so many pairs of a request's rows and a kv head's query heads, on the average (32 requests of 8192 tokens, 32 / 8 heads of 128 in 8 bits, 5, 16, 20 rows each: narrow 110,
-// 147, 276 us, wide 213, 165, 246), or so many wide tiles in all, which would leave much of the chip idle (256, 512, 768 rows of one request: narrow 11.1, 15.8, 28, wide 15.7, 20.5, 26;
-// 512 rows behind 7680 tokens: 131, 103).  Heads of 256 in fp16 have no registers for a narrow tile on its way (32 x 5 rows of 4096: narrow 302 us, wide 275).
-constexpr int FEW_PAIRS = 64, FEW_TILES = 96;
+// 147, 276 us, wide 213, 165, 246), or so many wide tiles in all, which would leave much of the chip idle: as many as make narrow ones for the chip once where the table has room for short contexts only, fewer where
+// it has for long ones, over which wide ones read LDS less often (384, 512, 640 rows of 32 / 8 heads in fp16: narrow 13.2, 14.8, 22.1 us, wide 17.7, 19.8, 23.5; behind 1024 tokens 25.9, 28.2, 49.3 and 31.3, 33.6, 35.7;
+// behind 4096 63, 71, 114 and 51, 62, 69; 256 rows 11.0, 21.9, 43.8 and 15.6, 27.4, 51.1; heads of 64 and 8 bits alike).  Heads of 256 in fp16 have no registers for a narrow tile on its way (32 x 5 rows of
+// 4096: narrow 302 us, wide 275).
+constexpr int FEW_PAIRS = 64, FEW_TILES = 64, FEW_TILES_SHORT = 128, SHORT = 2048;
 
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
+    const int tiles = DIM < 256 && (long long)a.width * a.page <= SHORT ? FEW_TILES_SHORT : FEW_TILES;
     const bool few = (DIM < 256 || BITS == 8) &&
-                     ((long long)a.M * (a.heads / a.kv) <= (long long)FEW_PAIRS * a.B || (long long)a.M * a.heads <= (long long)FEW_TILES * Wide::TQ);
+                     ((long long)a.M * (a.heads / a.kv) <= (long long)FEW_PAIRS * a.B || (long long)a.M * a.heads <= (long long)tiles * Wide::TQ);
     constexpr int sums = 128 * DIM * 4;        // (128 rows of O, or four times 32)
     constexpr int wide = 2 * Stage<DIM, Wide::KT>::BYTES + BLOCK_TOKENS * DIM * BITS / 8, narrow = RG * Stage<DIM, Narrow::KT>::BYTES;
     const int lds = few ? (narrow > sums ? narrow : sums) : (wide > sums ? wide : sums);
