@@ -448,3 +448,39 @@ def test_together_on_another_stream_and_in_a_graph(gpu):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
         step()                               # eager work between the replays, in the same workspace
+
+
+@pytest.mark.parametrize("B", [7, 70])
+def test_a_captured_call_follows_lengths_and_rows(gpu, B):
+    """Lengths and rows are read on the device: a captured call takes those of each replay, and gives the eager bits; so it does where other calls use the workspace between."""
+    import torch
+    heads, kv, dim, page, width, M = 8, 2, 128, 16, 20, 40 * B
+    torch.manual_seed(B)
+    q = torch.randn((M, heads, dim), device="cuda").half()
+    k, v = (torch.randn((B * width, kv, page, dim), device="cuda").half() for _ in range(2))
+    table = torch.randperm(B * width, device="cuda").int().view(B, width)
+    lengths, starts = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    ws = gpu.new_attention_rows_workspace(M, B, heads, kv, dim, width * page)
+
+    def call(out, n=lengths, s=starts):
+        gpu.cache_attention_rows(q, k, v, None, None, table, n, s, out, None, M, B, heads, kv, dim, heads * dim, B * width, page, 16, 0, width, 0, 0, 0.1, ws)
+
+    rng = np.random.default_rng(B)
+    held = torch.full_like(q, 7.0)
+    call(held)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(held)
+    for _ in range(4):
+        n = rng.integers(1, width * page + 1, B)
+        s = np.concatenate([[0], np.cumsum(np.minimum(rng.integers(0, 41, B), n))])
+        lengths.copy_(torch.from_numpy(n.astype(np.int32)))
+        starts.copy_(torch.from_numpy(s.astype(np.int32)))
+        want = torch.full_like(q, 7.0)
+        call(want, lengths.clone(), starts.clone())
+        held.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want) and bool((want[:int(s[-1])] != 7.0).any()) and bool((want[int(s[-1]):] == 7.0).all())
+        assert not ws[:49152].any()
