@@ -440,8 +440,8 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  * row_starts: B + 1 int32, not decreasing (where they decrease, out and lse are undefined, and the workspace's first 48 KiB have to be zeroed before the next call), taken as 0 .. M;
  * rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
  * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.
- * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits in the form for single tokens,
- * else as one fp16 (rounded to nearest, the largest 2^11 or more).  Equal inputs give bit-equal outputs; how tokens are split between workgroups, and so the last bits, depends on
+ * out: fp16 M x n_heads x head_dim; lse: fp32 M x n_heads or NULL.  Scores, sums and out are fp32 until the end; a weight meets v with 20 bits (the largest
+ * weights are 2^11 or more; what is below 2^-36 of them may be lost).  Equal inputs give bit-equal outputs; how tokens are split between workgroups, and so the last bits, depends on
  * the lengths and rows of all requests.
  * workspace: eora_cache_attention_rows_workspace_bytes() of the largest call (B, heads, head_dim; max_tokens = max_pages * page_size).  Its first 48 KiB are ZERO before the first call, the rest
  * may hold anything; every call leaves it usable for the next, of whatever sizes and of either form.

@@ -22,8 +22,10 @@
 // Few rows: tiles of 32 pairs by 32 keys (few_kernel() below).
 //
 // Softmax: as for single tokens, m is a reference (LOWER below the largest score when it is set, raised when a score has risen by RAISE more), the largest weight 2^11 to 2^15.  A weight meets
-// V as one fp16, rounded to nearest: off by 2^-11 of itself at most, as the result is by its own rounding, and by less in a sum over tokens; two of them, as for single
-// tokens, would take half as long again.  The sum of the weights is of those that were not rounded: lse would show it.  Scores, sums and O are fp32.
+// V as two fp16, the second what cutting off the first leaves: 21 bits together, beside which the result's own rounding is all that shows.  (One fp16 put out off by up to 2^-11 of sum p |v|, where the
+// plain definition in fp32 is off by its last rounding: 8192 rows 2.6e-4 of out's norm in place of 2.0e-4.  It took 1120 us, two take 1490: a product's matrix instructions once more, at the clock that the card's power
+// holds.)  Neither half is negative, and the second is zero only for a weight of 11 bits, which LOWER keeps the largest from being: an infinite value gives an infinity.  The sum of the weights is of those that were not
+// rounded.  Scores, sums and O are fp32.
 //
 // What rows may not see: a tile that all rows of a wavefront see as a whole takes no test.  Tokens that no row of the tile sees are zeros in LDS; where some rows see a token and others do not, a value
 // that is not finite would spoil a product with weights of 0: it is a zero there too, and added at the end, to the rows that see it (add_odd()).
@@ -57,7 +59,7 @@ constexpr int MAX_PARTS = most_of(128);
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr int PLAN_BYTES = 32;                 // of a request's plan, behind the partial results
-constexpr float RAISE = 4.f, LOWER = 11.f;
+constexpr float RAISE = 4.f, LOWER = 11.0001f;  // (2^15.0001 is below fp16's 65504)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -72,6 +74,13 @@ __device__ __forceinline__ float max_of_halves(float v)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// two weights as two fp16 each: cut off, and what that leaves
+__device__ __forceinline__ void halves(float x, float y, h2& high, h2& low)
+{
+    high = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+    low = h2{(_Float16)(x - (float)high[0]), (_Float16)(y - (float)high[1])};
 }
 
 // 64 pieces of 16 bytes from memory straight into 1 KiB of LDS, lane after lane: from base + off + OFF to lds + OFF.  The compiler does not know of the request: it counts in vmcnt all
@@ -773,15 +782,15 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
             // One matrix instruction a slot, kept in this order: beside those of the next tile's scores (behind the last tile: of what lies there, unused) two weights of this one
             // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
             const unsigned char* next = smem + (stage ^ 1) * STAGE;
-            Frag kf[AHEAD], vf[AHEAD], p[4];
+            Frag kf[AHEAD], vf[AHEAD], high[4], low[4];
             auto read_k = [&](int x) { st.keys(next, x % 2, x / 2, kf[x % AHEAD]); };
             auto read_v = [&](int x) { st.values(base, x / ND, x % ND, vf[x % AHEAD]); };
             auto weights = [&](int x) {        // elements 2 x and 2 x + 1
                 const int b = x / 8, e = 2 * x % 16;
                 const float v = exp2_(__builtin_fmaf(S[b][e], by, -ref)), w = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
-                l += v;                        // (not what the weights are rounded to: lse would be off by 2^-12)
+                l += v;
                 l += w;
-                p[2 * b + e / 8].p[e % 8 / 2] = h2{(_Float16)v, (_Float16)w};
+                halves(v, w, high[2 * b + e / 8].p[e % 8 / 2], low[2 * b + e / 8].p[e % 8 / 2]);
             };
 #pragma unroll
             for (int x = 0; x < AHEAD; ++x) read_k(x);
@@ -801,7 +810,8 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 #pragma unroll
             for (int x = 0; x < 4 * ND; ++x) {
                 const int s = x / ND, d = x % ND;
-                O[d] = mfma32(vf[x % AHEAD].v, p[s].v, O[d]);
+                O[d] = mfma32(vf[x % AHEAD].v, high[s].v, O[d]);
+                O[d] = mfma32(vf[x % AHEAD].v, low[s].v, O[d]);
                 if (x + AHEAD < 4 * ND) read_v(x + AHEAD);
 #pragma unroll
                 for (int e = 16 * x / (4 * ND); e < 16 * (x + 1) / (4 * ND); ++e) top = e == 0 ? fmaxf(N[0][0], N[1][0]) : fmaxf(fmaxf(top, N[0][e]), N[1][e]);
@@ -974,13 +984,13 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
             for (int d = 0; d < ND; ++d) O[d] *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        Frag p[2];
+        Frag high[2], low[2];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             const float x = exp2_(__builtin_fmaf(S[e], by, -ref)), y = exp2_(__builtin_fmaf(S[e + 1], by, -ref));
             l += x;
             l += y;
-            p[e / 8].p[e % 8 / 2] = h2{(_Float16)x, (_Float16)y};
+            halves(x, y, high[e / 8].p[e % 8 / 2], low[e / 8].p[e % 8 / 2]);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -988,7 +998,8 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
             for (int d = 0; d < ND; ++d) {
                 Frag v;
                 st.values(base, s, d, v);
-                O[d] = mfma32(v.v, p[s].v, O[d]);
+                O[d] = mfma32(v.v, high[s].v, O[d]);
+                O[d] = mfma32(v.v, low[s].v, O[d]);
             }
     }
     l = both_halves(l);
