@@ -455,6 +455,11 @@ int eora_cache_attention_rows(const void* q, const void* pages_k, const void* pa
                               int M, int B, int n_heads, int n_kv_heads, int head_dim, int q_stride,
                               int n_pages, int page_size, int cache_bits, int scale_block, int max_pages, int window, int sinks, float scale,
                               void* workspace, size_t workspace_bytes, void* stream);
+/* HOST, test hook: what workgroup `unit` of such a call with row_starts does (lengths and row_starts: HOST memory; nothing is enqueued).  plan: ten integers, 1 if its tiles are those for
+ * few rows, the workgroups of the launch, the request (-1: nothing to do), kv head, tile of its pairs of a row and a query head, tiles of the request, part of the tile along the keys, parts of
+ * that tile, tiles of keys of this part, and the number of its partial results (-1: the tile is not cut).  Errors: EORA_ERR_NULL / UNSUPPORTED / SHAPE. */
+int eora_debug_attention_rows_unit(const int* lengths, const int* row_starts, int M, int B, int n_heads, int n_kv_heads, int head_dim, int page_size, int cache_bits,
+                                   int max_pages, int window, int sinks, int unit, int* plan);
 
 /* ---------------------------------------------------------------------------------------------
  * Parity exports (integer / exact work, compared bit for bit against the CPU oracle).

@@ -15,5 +15,5 @@ from .binding import (  # noqa: F401
     factors_workspace_bytes, factors, linear_q_multi, factors_store_f16, factors_store_q, linear_sp24_group,
     adapters_workspace_bytes, new_adapters_workspace, linear_adapters, cache_append,
     cache_attention_workspace_bytes, new_attention_workspace, cache_attention,
-    cache_append_blocks, cache_read, cache_attention_rows_workspace_bytes, new_attention_rows_workspace, cache_attention_rows,
+    cache_append_blocks, cache_read, cache_attention_rows_workspace_bytes, new_attention_rows_workspace, cache_attention_rows, debug_attention_rows_unit,
 )

@@ -91,6 +91,7 @@ def _load():
         "eora_cache_read": (ci, [vp] * 7 + [ci] * 7 + [vp]),
         "eora_cache_attention_rows_workspace_bytes": (sz, [ci] * 6),
         "eora_cache_attention_rows": (ci, [vp] * 10 + [ci] * 13 + [ctypes.c_float, vp, sz, vp]),
+        "eora_debug_attention_rows_unit": (ci, [ctypes.POINTER(ci)] * 2 + [ci] * 11 + [ctypes.POINTER(ci)]),
         "eora_factors_workspace_bytes": (sz, [ci, ci, ci]),
         "eora_factors_store_f16": (ci, [vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp]),
         "eora_factors_store_q": (ci, [vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp]),
@@ -114,7 +115,7 @@ EXPORTS = ["eora_status_string", "eora_qweight_bytes", "eora_qzeros_bytes", "eor
            "eora_debug_last_launch", "eora_debug_probe", "eora_linear_q_static", "eora_debug_set_resident_min_blocks", "eora_debug_set_factors_route",
            "eora_debug_prefill_parts", "eora_debug_factors_near", "eora_debug_factors_parts", "eora_debug_prefill_plan", "eora_debug_last_prefill",
            "eora_adapters_workspace_bytes", "eora_linear_adapters", "eora_cache_append", "eora_cache_attention_workspace_bytes", "eora_cache_attention",
-           "eora_cache_append_blocks", "eora_cache_read", "eora_cache_attention_rows_workspace_bytes", "eora_cache_attention_rows"]
+           "eora_cache_append_blocks", "eora_cache_read", "eora_cache_attention_rows_workspace_bytes", "eora_cache_attention_rows", "eora_debug_attention_rows_unit"]
 
 
 def status_string(status):
@@ -470,6 +471,14 @@ def cache_attention_rows(q, pages_k, pages_v, k_scale, v_scale, page_table, leng
     _check(lib.eora_cache_attention_rows(_dp(q), _dp(pages_k), _dp(pages_v), _dp(k_scale), _dp(v_scale), _dp(page_table), _dp(lengths), _dp(row_starts),
                                          _dp(out), _dp(lse), M, B, n_heads, n_kv_heads, head_dim, q_stride, n_pages, page_size, cache_bits, scale_block,
                                          max_pages, window, sinks, scale, _dp(workspace), _nbytes(workspace), _stream()), "cache_attention_rows")
+
+
+def debug_attention_rows_unit(lengths, row_starts, M, n_heads, n_kv_heads, head_dim, page_size, cache_bits, max_pages, window, sinks, unit):
+    """(few rows, workgroups, request, kv head, tile, tiles, part, parts, tiles of keys, partial result) of a workgroup; host only, lengths and row_starts: numpy int32."""
+    plan, ip = (ctypes.c_int * 10)(), ctypes.POINTER(ctypes.c_int)
+    _check(lib.eora_debug_attention_rows_unit(lengths.ctypes.data_as(ip), row_starts.ctypes.data_as(ip), M, len(lengths), n_heads, n_kv_heads, head_dim, page_size, cache_bits, max_pages,
+                                              window, sinks, unit, plan), "debug_attention_rows_unit")
+    return tuple(plan)
 
 
 # ------------------------------------------------------------------ calibration (Alg. 1 steps 1-6)

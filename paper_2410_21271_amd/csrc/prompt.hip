@@ -36,6 +36,7 @@
 #include "serving.hpp"
 
 #include <utility>
+#include <vector>
 
 namespace eora {
 namespace {
@@ -101,7 +102,7 @@ struct Request {
     int n, first, rows, tiles, cost;
 };
 template <typename SHAPE>
-__device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
+__host__ __device__ __forceinline__ Request request_of(const PromptArgs& a, int b)
 {
     constexpr int TQ = SHAPE::TQ, KT = SHAPE::KT;
     Request r;
@@ -133,15 +134,14 @@ struct Unit {
 // 1000, 1.94 shares each, 15 / 3 heads of 64: 51 us, these 43.  All tiles of a request alike, as if each saw as much as the last: each by what
 // it sees, 2048 rows, whose tiles fill the chip once, would take 67 in place of 56.)
 // The work is added up in floats, in one order: everyone finds the same parts.  With two or more of them cost / share is 1.875 or more: together they are 1.07 want_of(dim) at most.
+__host__ __device__ __forceinline__ float shares_of(const PromptArgs& a, float work) { return (float)want_of(a.dim) / fmaxf(work * (float)a.kv, 1.f); }
 template <typename SHAPE>
-__device__ __forceinline__ float shares_of(const PromptArgs& a, float work) { return (float)want_of(a.dim) / fmaxf(work * (float)a.kv, 1.f); }
-template <typename SHAPE>
-__device__ __forceinline__ int parts_of(const Request& r, float shares)
+__host__ __device__ __forceinline__ int parts_of(const Request& r, float shares)
 {
     const int most = (r.cost + SHAPE::LEAST_PART - 1) / SHAPE::LEAST_PART, parts = (int)fminf(__builtin_fmaf((float)r.cost, shares, 0.125f), (float)MAX_PARTS);
     return parts < 1 ? 1 : (parts < most ? parts : most);
 }
-__device__ __forceinline__ Unit unit_in(const PromptArgs& a, const Request& r, int b, int parts, int local, int cut)
+__host__ __device__ __forceinline__ Unit unit_in(const PromptArgs& a, const Request& r, int b, int parts, int local, int cut)
 {
     Unit u;
     u.r = r;
@@ -178,7 +178,7 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
     const int lane = threadIdx.x & 63;
     Request r = request_of<SHAPE>(a, lane < a.B ? lane : a.B - 1);
     if (lane >= a.B) r.tiles = 0;
-    const float shares = shares_of<SHAPE>(a, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)));
+    const float shares = shares_of(a, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scan((float)r.tiles * (float)r.cost)), 63)));
     const int parts = parts_of<SHAPE>(r, shares), units = r.tiles * parts * a.kv, cut = parts > 1 ? units : 0;
     const int v = scan(units), c = scan(cut);
     const unsigned long long mine = __ballot(id >= v - units && id < v);
@@ -200,6 +200,33 @@ __device__ __forceinline__ bool unit_of_few(const PromptArgs& a, int id, Unit& u
 struct Planned {
     int4 at, what;                             // end of its units, parts before it, n, first; rows, tiles, parts, cost
 };
+// Units are counted up to here, beyond all that a launch may have (2^23): where row_starts decrease, requests share rows, and all of them together may have more units than 32 bits hold
+constexpr int MOST_UNITS = 1 << 24;
+__host__ __device__ __forceinline__ int counted(int units) { return units < MOST_UNITS ? units : MOST_UNITS; }
+// requests [b0, b1): their units and, of them, those of tiles that are cut; then their plans, behind `end` units and `before` parts
+template <typename SHAPE>
+__host__ __device__ __forceinline__ void count_units(const PromptArgs& a, int b0, int b1, float shares, int& units, int& cut)
+{
+    units = cut = 0;
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_of<SHAPE>(a, b);
+        const int parts = parts_of<SHAPE>(r, shares), mine = r.tiles * parts * a.kv;
+        units = counted(units + mine);
+        cut = counted(cut + (parts > 1 ? mine : 0));
+    }
+}
+template <typename SHAPE>
+__host__ __device__ __forceinline__ void write_plans(const PromptArgs& a, int b0, int b1, float shares, int end, int before, Planned* plan)
+{
+    for (int b = b0; b < b1; ++b) {
+        const Request r = request_of<SHAPE>(a, b);
+        const int parts = parts_of<SHAPE>(r, shares), mine = r.tiles * parts * a.kv;
+        end += mine;
+        plan[b].at = make_int4(end, before, r.n, r.first);
+        plan[b].what = make_int4(r.rows, r.tiles, parts, r.cost);
+        before += parts > 1 ? mine : 0;
+    }
+}
 static_assert(sizeof(Planned) == PLAN_BYTES, "");
 constexpr int PLAN_THREADS = 1024;
 template <typename SHAPE>
@@ -220,18 +247,13 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(const PromptArgs a)
     __syncthreads();
     work = 0.f;
     for (int w = 0; w < WAVES; ++w) work += sums[w];
-    const float shares = shares_of<SHAPE>(a, work);
-    int units = 0, cut = 0;
-    for (int b = b0; b < b1; ++b) {
-        const Request r = request_of<SHAPE>(a, b);
-        const int parts = parts_of<SHAPE>(r, shares);
-        units += r.tiles * parts * a.kv;
-        cut += parts > 1 ? r.tiles * parts * a.kv : 0;
-    }
+    const float shares = shares_of(a, work);
+    int units, cut;
+    count_units<SHAPE>(a, b0, b1, shares, units, cut);
     const int v = scan(units), c = scan(cut);
     if (lane == 63) {
-        totals[wave][0] = v;
-        totals[wave][1] = c;
+        totals[wave][0] = counted(v);
+        totals[wave][1] = counted(c);
     }
     __syncthreads();
     int end = v - units, before = c - cut;
@@ -239,15 +261,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(const PromptArgs a)
         end += totals[w][0];
         before += totals[w][1];
     }
-    for (int b = b0; b < b1; ++b) {
-        const Request r = request_of<SHAPE>(a, b);
-        const int parts = parts_of<SHAPE>(r, shares), mine = r.tiles * parts * a.kv;
-        end += mine;
-        Planned& to = ((Planned*)a.plan)[b];
-        to.at = make_int4(end, before, r.n, r.first);
-        to.what = make_int4(r.rows, r.tiles, parts, r.cost);
-        before += parts > 1 ? mine : 0;
-    }
+    write_plans<SHAPE>(a, b0, b1, shares, end, before, (Planned*)a.plan);
 }
 __device__ __forceinline__ bool unit_planned(const PromptArgs& a, int id, Unit& u)
 {
@@ -354,7 +368,10 @@ struct Tile {
     const int* table;
     __device__ __forceinline__ bool find(const PromptArgs& a, int id)
     {
-        if (!(a.B <= 64 ? unit_of_few<SHAPE>(a, id, u) : unit_planned(a, id, u))) return false;
+        return (a.B <= 64 ? unit_of_few<SHAPE>(a, id, u) : unit_planned(a, id, u)) && set(a);
+    }
+    __host__ __device__ __forceinline__ bool set(const PromptArgs& a)            // u is known
+    {
         group = a.heads / a.kv;
         const int pairs = u.r.rows * group;
         from = u.r.n - u.r.rows;
@@ -1052,12 +1069,17 @@ long long units_of(int M, int B, int heads, int kv, int tq) { return (((long lon
 // 4096: narrow 302 us, wide 275).
 constexpr int FEW_PAIRS = 64, FEW_TILES = 64, FEW_TILES_SHORT = 128, SHORT = 2048;
 
+bool takes_narrow(const PromptArgs& a)
+{
+    const int tiles = a.dim < 256 && (long long)a.width * a.page <= SHORT ? FEW_TILES_SHORT : FEW_TILES;
+    return (a.dim < 256 || a.bits == 8) &&
+           ((long long)a.M * (a.heads / a.kv) <= (long long)FEW_PAIRS * a.B || (long long)a.M * a.heads <= (long long)tiles * Wide::TQ);
+}
+
 template <int DIM, int BITS, bool BLOCKS>
 hipError_t start(const PromptArgs& a, hipStream_t stream)
 {
-    const int tiles = DIM < 256 && (long long)a.width * a.page <= SHORT ? FEW_TILES_SHORT : FEW_TILES;
-    const bool few = (DIM < 256 || BITS == 8) &&
-                     ((long long)a.M * (a.heads / a.kv) <= (long long)FEW_PAIRS * a.B || (long long)a.M * a.heads <= (long long)tiles * Wide::TQ);
+    const bool few = takes_narrow(a);
     constexpr int sums = 128 * DIM * 4;        // (128 rows of O, or four times 32)
     constexpr int wide = 2 * Stage<DIM, Wide::KT>::BYTES + BLOCK_TOKENS * DIM * BITS / 8, narrow = RG * Stage<DIM, Narrow::KT>::BYTES;
     const int lds = few ? (narrow > sums ? narrow : sums) : (wide > sums ? wide : sums);
@@ -1082,7 +1104,53 @@ hipError_t start(const PromptArgs& a, hipStream_t stream)
     return a.k_scales ? start<DIM, 8, true>(a, stream) : start<DIM, 8, false>(a, stream);
 }
 
+// What workgroup `id` of a launch does, found on the host as plan_kernel() and unit_planned() find it (their sum in floats may be rounded otherwise)
+template <typename SHAPE>
+PromptUnit unit_on_host(const PromptArgs& a, int id)
+{
+    float work = 0.f;
+    for (int b = 0; b < a.B; ++b) {
+        const Request r = request_of<SHAPE>(a, b);
+        work += (float)r.tiles * (float)r.cost;
+    }
+    const float shares = shares_of(a, work);
+    std::vector<Planned> plan(a.B);
+    const int each = (a.B + PLAN_THREADS - 1) / PLAN_THREADS;
+    int end = 0, before = 0;
+    for (int b = 0; b < a.B; b += each) {
+        const int stop = b + each < a.B ? b + each : a.B;
+        int units, cut;
+        count_units<SHAPE>(a, b, stop, shares, units, cut);
+        write_plans<SHAPE>(a, b, stop, shares, end, before, plan.data());
+        end = counted(end + units);
+        before = counted(before + cut);
+    }
+    PromptUnit to{};
+    to.narrow = SHAPE::TQ == Narrow::TQ;
+    to.workgroups = units_of(a.M, a.B, a.heads, a.kv, SHAPE::TQ);
+    to.request = to.place = -1;
+    int b = 0;
+    while (b < a.B && id >= plan[b].at.x) ++b;
+    if (b == a.B) return to;
+    const int4 at = plan[b].at, what = plan[b].what;
+    Tile<SHAPE> t;
+    t.u = unit_in(a, Request{at.z, at.w, what.x, what.y, what.w}, b, what.z, id - (at.x - what.y * what.z * a.kv), at.y);
+    const bool some = t.set(a);
+    to.head = t.u.h;
+    to.tile = t.u.tile;
+    to.tiles = what.y;
+    to.part = t.u.part;
+    to.parts = t.parts;
+    if (!some) return to;
+    to.request = b;
+    to.steps = t.k1 - t.k0;
+    if (t.parts > 1) to.place = t.u.place;
+    return to;
+}
+
 }  // namespace
+
+PromptUnit prompt_unit(const PromptArgs& a, int id) { return takes_narrow(a) ? unit_on_host<Narrow>(a, id) : unit_on_host<Wide>(a, id); }
 
 long long prompt_units(int M, int B, int heads, int kv) { return units_of(M, B, heads, kv, Narrow::TQ); }
 

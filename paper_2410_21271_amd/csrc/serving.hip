@@ -373,4 +373,32 @@ int eora_cache_attention_rows(const void* q, const void* pages_k, const void* pa
     return EORA_OK;
 }
 
+int eora_debug_attention_rows_unit(const int* lengths, const int* row_starts, int M, int B, int n_heads, int n_kv_heads, int head_dim, int page_size, int cache_bits,
+                                   int max_pages, int window, int sinks, int unit, int* plan)
+{
+    if (!lengths || !row_starts || !plan) return EORA_ERR_NULL;
+    if ((cache_bits != 16 && cache_bits != 8) || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return EORA_ERR_UNSUPPORTED;
+    if (M <= 0 || B <= 0 || B > ATTEND_MAX_B || n_kv_heads <= 0 || n_heads <= 0 || n_heads % n_kv_heads || page_size <= 0 || page_size % 16 || max_pages <= 0 || window < 0 ||
+        sinks < 0 || unit < 0 || (long long)max_pages * page_size > 1ll << 30)
+        return EORA_ERR_SHAPE;
+    if ((long long)M * (n_heads / n_kv_heads) > 0x7fffffff || prompt_units(M, B, n_heads, n_kv_heads) > 0x7fffff) return EORA_ERR_SHAPE;
+    PromptArgs a{};
+    a.lengths = lengths;
+    a.starts = row_starts;
+    a.M = M;
+    a.B = B;
+    a.heads = n_heads;
+    a.kv = n_kv_heads;
+    a.dim = head_dim;
+    a.page = page_size;
+    a.bits = cache_bits;
+    a.width = max_pages;
+    a.window = window >= max_pages * page_size ? 0 : window;
+    a.sinks = a.window == 0 ? 0 : (sinks < max_pages * page_size ? sinks : max_pages * page_size);
+    const PromptUnit u = prompt_unit(a, unit);
+    const int found[10] = {u.narrow, (int)u.workgroups, u.request, u.head, u.tile, u.tiles, u.part, u.parts, u.steps, u.place};
+    for (int i = 0; i < 10; ++i) plan[i] = found[i];
+    return EORA_OK;
+}
+
 }  // extern "C"

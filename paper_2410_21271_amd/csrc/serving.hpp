@@ -123,6 +123,14 @@ struct PromptArgs {
 size_t prompt_workspace_bytes(int B, int dim);
 long long prompt_units(int M, int B, int heads, int kv);               // workgroups of a launch at most
 hipError_t launch_prompt(PromptArgs a, hipStream_t stream);
+// what workgroup `id` of that launch has (a.lengths and a.starts: host memory)
+struct PromptUnit {
+    int narrow;                     // tiles of few pairs
+    long long workgroups;           // of the launch
+    int request, head, tile, tiles, part, parts;               // request -1: nothing; tiles of the request
+    int steps, place;               // tiles of keys; number of its partial results among all, -1: its tile is not cut
+};
+PromptUnit prompt_unit(const PromptArgs& a, int id);
 
 struct AdapterArgs {
     const _Float16* x;              // M x d_in
