@@ -437,6 +437,7 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  * for query head i of kv head i / (n_heads / n_kv_heads) as in eora_cache_attention(), with pages, scores and lse as there.  A row that sees nothing (a position below 0, all
  * masked) has out = 0 and lse = -inf.  What a row does not see is never used for it, NaN and infinities included, also where other rows see it.
  * A value that is not finite makes its column of out infinite or NaN for the rows that see it (where its score is -inf, it may or may not).
+ * A head's key scale that is not finite makes out and lse NaN for the rows that see a token, and so does a score that is 0 times an infinity (scale 0).
  * row_starts: B + 1 int32, not decreasing (where they decrease, out and lse are undefined, and the workspace's first 48 KiB have to be zeroed before the next call), taken as 0 .. M;
  * rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
  * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.

@@ -567,7 +567,8 @@ __device__ __forceinline__ void finish(const PromptArgs& a, const Tile<SHAPE>& t
     }
 }
 
-// The scale of the scores in powers of two, and a lane's operand of q: pair `pair` of the tile's, its sign that of the scale
+// A lane's operand of q: pair `pair` of the tile's, its sign that of the scores' scale.  The scale's size is applied to the scores, where no value of a masked one may come of it: a scale that is 0 or not
+// finite (a head's, of a cache of 8 bits) goes into q, so that scores are 0 or, of what is not finite on either side, NaN.
 template <int DIM>
 __device__ __forceinline__ void load_q(const PromptArgs& a, const Unit& u, int group, int pair, bool there, int half, float scale, Frag (&q)[DIM / 16])
 {
@@ -580,7 +581,14 @@ __device__ __forceinline__ void load_q(const PromptArgs& a, const Unit& u, int g
 #pragma unroll
         for (int e = 0; e < 4; ++e) q[t].u[e] = there ? w[e] ^ sign : 0u;
     }
+    if (scale == 0.f || !(fabsf(scale) < INFINITY)) {
+        const _Float16 by = (_Float16)(scale == 0.f ? 0.f : __builtin_nanf(""));
+#pragma unroll
+        for (int t = 0; t < DIM / 16; ++t) q[t].v *= by;
+    }
 }
+// ... and that size, for scores that are finite or -inf
+__device__ __forceinline__ float size_of(float scale) { return fabsf(scale) < INFINITY ? fmaxf(fabsf(scale), 0x1p-100f) : 1.f; }
 __device__ __forceinline__ float both_halves(float v)
 {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -699,7 +707,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
     };
 
     // q, its sign that of the scale
-    const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
+    const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = size_of(scale);
     Frag q[NK];
     load_q<DIM>(a, u, tile.group, w0 + col, there, half, scale, q);
     f16x O[ND];
@@ -952,7 +960,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
             }
     };
 
-    const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = fmaxf(fabsf(scale), 0x1p-100f);       // (a scale of 0: scores that are)
+    const float scale = a.scale * LOG2E * (BITS == 8 && !BLOCKS ? a.k_scale[u.h] : 1.f), by = size_of(scale);
     Frag q[NK];
     load_q<DIM>(a, u, tile.group, tile.pair0 + col, there, half, scale, q);
     f16x O[ND];
