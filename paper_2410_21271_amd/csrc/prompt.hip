@@ -25,7 +25,7 @@
 // V as two fp16, the second what cutting off the first leaves: 21 bits together, beside which the result's own rounding is all that shows.  (One fp16 put out off by up to 2^-11 of sum p |v|, where the
 // plain definition in fp32 is off by its last rounding: 8192 rows 2.6e-4 of out's norm in place of 2.0e-4.  It took 1120 us, two take 1490: a product's matrix instructions once more, at the clock that the card's power
 // holds.)  Neither half is negative, and the second is zero only for a weight of 11 bits, which LOWER keeps the largest from being: an infinite value gives an infinity.  The sum of the weights is of those that were not
-// rounded.  Scores, sums and O are fp32.
+// rounded, tile by tile (weight by weight, roundings of equal weights, all of one sign, put lse off by 5e-5 behind 8192 tokens and 6e-4 behind 131072; same times).  Scores, sums and O are fp32.
 //
 // What rows may not see: a tile that all rows of a wavefront see as a whole takes no test.  Tokens that no row of the tile sees are zeros in LDS; where some rows see a token and others do not, a value
 // that is not finite would spoil a product with weights of 0: it is a zero there too, and added at the end, to the rows that see it (add_odd()).
@@ -808,13 +808,14 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
             // each, beside those of O the next tile's largest score.  Operands are read AHEAD slots before.
             const unsigned char* next = smem + (stage ^ 1) * STAGE;
             Frag kf[AHEAD], vf[AHEAD], high[4], low[4];
+            float sum = 0.f;                   // of this tile's weights
             auto read_k = [&](int x) { st.keys(next, x % 2, x / 2, kf[x % AHEAD]); };
             auto read_v = [&](int x) { st.values(base, x / ND, x % ND, vf[x % AHEAD]); };
             auto weights = [&](int x) {        // elements 2 x and 2 x + 1
                 const int b = x / 8, e = 2 * x % 16;
                 const float v = exp2_(__builtin_fmaf(S[b][e], by, -ref)), w = exp2_(__builtin_fmaf(S[b][e + 1], by, -ref));
-                l += v;
-                l += w;
+                sum += v;
+                sum += w;
                 halves(v, w, high[2 * b + e / 8].p[e % 8 / 2], low[2 * b + e / 8].p[e % 8 / 2]);
             };
 #pragma unroll
@@ -832,6 +833,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
                 for (int w = 16 * x / (2 * NK); w < 16 * (x + 1) / (2 * NK); ++w) weights(w);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            l += sum;
 #pragma unroll
             for (int x = 0; x < 4 * ND; ++x) {
                 const int s = x / ND, d = x % ND;
@@ -1010,13 +1012,15 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
         }
         const float ref = m == -INFINITY ? 0.f : m;
         Frag high[2], low[2];
+        float sum = 0.f;                       // of this tile's weights
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             const float x = exp2_(__builtin_fmaf(S[e], by, -ref)), y = exp2_(__builtin_fmaf(S[e + 1], by, -ref));
-            l += x;
-            l += y;
+            sum += x;
+            sum += y;
             halves(x, y, high[e / 8].p[e % 8 / 2], low[e / 8].p[e % 8 / 2]);
         }
+        l += sum;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
