@@ -22,9 +22,9 @@
 // Few rows: tiles of 32 pairs by 32 keys (few_kernel() below).
 //
 // Softmax: as for single tokens, m is a reference (LOWER below the largest score when it is set, raised when a score has risen by RAISE more), the largest weight 2^11 to 2^15.  A weight meets
-// V as two fp16, the second what cutting off the first leaves: 21 bits together, beside which the result's own rounding is all that shows.  (One fp16 put out off by up to 2^-11 of sum p |v|, where the
+// V as two fp16, the second what cutting off the first leaves: 20.7 bits together, beside which the result's own rounding is all that shows.  (One fp16 put out off by up to 2^-11 of sum p |v|, where the
 // plain definition in fp32 is off by its last rounding: 8192 rows 2.6e-4 of out's norm in place of 2.0e-4.  It took 1120 us, two take 1490: a product's matrix instructions once more, at the clock that the card's power
-// holds.)  Neither half is negative, and the second is zero only for a weight of 11 bits, which LOWER keeps the largest from being: an infinite value gives an infinity.  The sum of the weights is of those that were not
+// holds.)  The second is positive as well: an infinite value gives an infinity (NaN where a weight is below 2^-24 of the largest).  The sum of the weights is of those that were not
 // rounded, tile by tile (weight by weight, roundings of equal weights, all of one sign, put lse off by 5e-5 behind 8192 tokens and 6e-4 behind 131072; same times).  Scores, sums and O are fp32.
 //
 // What rows may not see: a tile that all rows of a wavefront see as a whole takes no test.  Tokens that no row of the tile sees are zeros in LDS; where some rows see a token and others do not, a value
@@ -60,7 +60,7 @@ constexpr int MAX_PARTS = most_of(128);
 constexpr int COUNTERS = ATTEND_COUNTERS;      // words before the partial results: the first of them one for each tile that is cut
 static_assert(MAX_PARTS <= COUNTERS, "a counter for each tile that is cut");
 constexpr int PLAN_BYTES = 32;                 // of a request's plan, behind the partial results
-constexpr float RAISE = 4.f, LOWER = 11.0001f;  // (2^15.0001 is below fp16's 65504)
+constexpr float RAISE = 4.f, LOWER = 11.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -77,11 +77,12 @@ __device__ __forceinline__ float max_of_halves(float v)
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// two weights as two fp16 each: cut off, and what that leaves
+// Two weights as two fp16 each: cut off, and what that leaves of ABOVE times the weight, which is positive whatever the weight is.  (The results are divided by ABOVE in the end.)
+constexpr float ABOVE = 1.f + 0x1p-12f;
 __device__ __forceinline__ void halves(float x, float y, h2& high, h2& low)
 {
     high = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
-    low = h2{(_Float16)(x - (float)high[0]), (_Float16)(y - (float)high[1])};
+    low = h2{(_Float16)__builtin_fmaf(x, ABOVE, -(float)high[0]), (_Float16)__builtin_fmaf(y, ABOVE, -(float)high[1])};
 }
 
 // 64 pieces of 16 bytes from memory straight into 1 KiB of LDS, lane after lane: from base + off + OFF to lds + OFF.  The compiler does not know of the request: it counts in vmcnt all
@@ -877,7 +878,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
         add_odd<DIM, BITS>(a, tile, scale, sum);
         __syncthreads();
     }
-    finish<DIM>(a, tile, BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f, sum, row_m, row_l, last);
+    finish<DIM>(a, tile, (BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f) * (1.f / ABOVE), sum, row_m, row_l, last);
 }
 
 // Few rows, which leave the matrix instructions idle: bound by memory.  Tiles of 32 pairs (one column block) by 32 keys; each wavefront has every fourth tile of keys for itself, with LDS
@@ -1068,7 +1069,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
         add_odd<DIM, BITS>(a, tile, scale, sum);
         __syncthreads();
     }
-    finish<DIM>(a, tile, BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f, sum, row_m, row_l, last);
+    finish<DIM>(a, tile, (BITS == 8 && !BLOCKS ? a.v_scale[u.h] : 1.f) * (1.f / ABOVE), sum, row_m, row_l, last);
 }
 
 // Tiles of tq pairs at most, and the parts that some are cut into
