@@ -110,7 +110,7 @@ LEAST_POWER, MOST_POWER = -15, 8
 
 
 def block_power(values):
-    """The least e of -15 .. 8 with |x| <= 448 2^e for all finite values (8 where there is none)."""
+    """The least e of -15 .. 8 with |x| <= 448 2^e for all finite values (-15 where there is none; 8 where no e is large enough)."""
     x = np.abs(np.asarray(values, np.float64))
     top = x[np.isfinite(x)].max(initial=0.0)
     e = LEAST_POWER

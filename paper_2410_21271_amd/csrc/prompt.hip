@@ -3,28 +3,29 @@
 //      s_rt = scale q_r . k_t,   out_r = sum_t 2^(s_rt log2 e - m) v_t / sum_t 2^(s_rt log2 e - m)      t <= p_r, and t > p_r - window or t < sinks
 //
 // Row r of a request's n sits at p_r = length - n + r.  Bound by the matrix instructions where there are many rows (4 dim flops for each pair of a query head's row and a token), by memory
-// where there are few.  64 / 8 heads of 128: 8192 rows in fp16 in 1120 us, 982 TF (on a card where a large matrix product reaches 1470); 32 / 8 heads: 2048 rows in 56 us in fp16, 67 in 8 bits;
-// 32 requests of 5 rows and 8192 tokens in 8 bits (537 MB) in 107 us, 5.1 TB/s; 17 rows of 17 in 9 us.
+// where there are few.  64 / 8 heads of 128: 8192 rows in fp16 in 1510 us, 728 TF (1090 with the second halves of the weights, on a card where a large matrix product reaches
+// 1470); 32 / 8 heads: 2048 rows in 70 us in fp16, 79 in 8 bits; 32 requests of 5 rows and 8192 tokens in 8 bits (537 MB) in 110 to 115 us, 4.8 TB/s; 17 rows of 17 in 9.6 us.  Times of what was not
+// kept, here and below, were taken beside a kernel with one fp16 a weight, which took 1120, 56, 67, 107 and 9.2 for these.
 //
 // Tile: 128 pairs of a row and a query head of one kv head (32 a wavefront) by 64 keys.  A column of the matrix instructions is a pair, all query heads of a kv head share the keys.
 // S^T = K Q^T (32 x 32 x 16): a lane holds one pair's scores of 16 keys of 32, so that softmax needs no exchange between lanes but one of the largest score, and the scores are,
-// as fp16 weights, the second operand of O^T = V^T P^T, if that takes its keys in the order in which they lie: 8 (e / 4) + 4 half + e % 4 of 16.
+// as weights, two fp16 each, the second operand of O^T = V^T P^T, if that takes its keys in the order in which they lie: 8 (e / 4) + 4 half + e % 4 of 16.
 // K and V lie in LDS as fp16 rows, in two stages; V's operand is read transposed (ds_read_tr16_b64: four keys of a column a lane).  fp16 tiles go from memory to LDS without registers
 // (by way of them a wavefront's 32 words of a tile on its way spilled: 3749 us where 1418 were left without); codes of 8 bits go there as they are, and become fp16, exactly, once,
 // by the wavefront that moved them.
 //
 // A step: the scores of the next tile beside the softmax of this one, then this one's O, one matrix instruction a slot in an order that the compiler keeps, operands read four ahead (left to itself it
-// reads one, waits, multiplies: 1418 us -> 1395).  Alone on its compute unit a workgroup takes 2860 cycles a step, 1024 of matrix instructions: 740 before the first (scalar work, masks, the
-// first operands), 1340 beside the softmax, 580 beside V, 210 for tiles and the barrier.  So there are two workgroups a compute unit, which fill each other's gaps (8192 rows: 56 % of the
-// cycles have a matrix instruction, at a clock that the card's power holds at 1.6 GHz; a workgroup alone on a chip three quarters idle takes 1.02 us a step, all together 1.05 a step and compute unit).  What did not help: two teams of wavefronts on one tile of pairs (1378 us), eight wavefronts on tiles of 256 (1206, and 71 where 2048 rows take 59), 64 pairs a wavefront
+// reads one, waits, multiplies: 1418 us -> 1395).  Alone on its compute unit a workgroup takes 3480 cycles a step, 1536 of matrix instructions: 860 before the first (scalar work, masks, the
+// first operands), 1420 beside the softmax, 1045 beside V, 155 for tiles and the barrier.  So there are two workgroups a compute unit, which fill each other's gaps (8192 rows: 4600 cycles a step of both, 67 % with a
+// matrix instruction, at a clock that the card's power holds at 1.6 GHz).  What did not help: two teams of wavefronts on one tile of pairs (1378 us), eight wavefronts on tiles of 256 (1206, and 71 where 2048 rows take 59), 64 pairs a wavefront
 // (twice the work for an operand, one wavefront a SIMD: 1.4 times as long), O one step later (registers), waits of a step and a half for tiles, scalar work between the matrix instructions.
 //
 // Few rows: tiles of 32 pairs by 32 keys (few_kernel() below).
 //
 // Softmax: as for single tokens, m is a reference (LOWER below the largest score when it is set, raised when a score has risen by RAISE more), the largest weight 2^11 to 2^15.  A weight meets
 // V as two fp16, the second what cutting off the first leaves: 20.7 bits together, beside which the result's own rounding is all that shows.  (One fp16 put out off by up to 2^-11 of sum p |v|, where the
-// plain definition in fp32 is off by its last rounding: 8192 rows 2.6e-4 of out's norm in place of 2.0e-4.  It took 1120 us, two take 1490: a product's matrix instructions once more, at the clock that the card's power
-// holds.)  The second is positive as well: an infinite value gives an infinity (NaN where a weight is below 2^-24 of the largest).  The sum of the weights is of those that were not
+// plain definition in fp32 is off by its last rounding: 8192 rows 2.6e-4 of out's norm in place of 2.0e-4.  It took 1120 us, two take 1510: a product's matrix instructions once more, at the clock that the card's power
+// holds; fewer vector instructions or another order of the two products change nothing.)  The second is positive as well: an infinite value gives an infinity (NaN where a weight is below 2^-24 of the largest).  The sum of the weights is of those that were not
 // rounded, tile by tile (weight by weight, roundings of equal weights, all of one sign, put lse off by 5e-5 behind 8192 tokens and 6e-4 behind 131072; same times).  Scores, sums and O are fp32.
 //
 // What rows may not see: a tile that all rows of a wavefront see as a whole takes no test.  Tokens that no row of the tile sees are zeros in LDS; where some rows see a token and others do not, a value
@@ -883,7 +884,7 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void prompt_kernel(const P
 
 // Few rows, which leave the matrix instructions idle: bound by memory.  Tiles of 32 pairs (one column block) by 32 keys; each wavefront has every fourth tile of keys for itself, with LDS
 // of its own and no barrier, the next one on its way to its registers meanwhile: 64 KiB on their way a compute unit in fp16.  The four add up at the end.  (32 requests of 5 rows and 8192 tokens:
-// 107 us; with the tiles of many rows, of which three wavefronts of four have no pair and all wait for each other at every tile, 213.)
+// 110 us; with the tiles of many rows, of which three wavefronts of four have no pair and all wait for each other at every tile, 270.)
 template <int DIM, int BITS, bool BLOCKS>
 __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const PromptArgs a)
 {
@@ -1076,10 +1077,11 @@ __global__ __launch_bounds__(THREADS, residents(DIM)) void few_kernel(const Prom
 long long units_of(int M, int B, int heads, int kv, int tq) { return (((long long)M * (heads / kv) + tq - 1) / tq + B) * kv + MAX_PARTS; }
 
 // Narrow tiles up to so many pairs of a request's rows and a kv head's query heads, on the average (32 requests of 8192 tokens, 32 / 8 heads of 128 in 8 bits, 5, 16, 20 rows each: narrow 110,
-// 147, 276 us, wide 213, 165, 246), or so many wide tiles in all, which would leave much of the chip idle: as many as make narrow ones for the chip once where the table has room for short contexts only, fewer where
-// it has for long ones, over which wide ones read LDS less often (384, 512, 640 rows of 32 / 8 heads in fp16: narrow 13.2, 14.8, 22.1 us, wide 17.7, 19.8, 23.5; behind 1024 tokens 25.9, 28.2, 49.3 and 31.3, 33.6, 35.7;
-// behind 4096 63, 71, 114 and 51, 62, 69; 256 rows 11.0, 21.9, 43.8 and 15.6, 27.4, 51.1; heads of 64 and 8 bits alike).  Heads of 256 in fp16 have no registers for a narrow tile on its way (32 x 5 rows of
-// 4096: narrow 302 us, wide 275).
+// 162, 299 us, wide 270, 179, 281), or so many wide tiles in all, which would leave much of the chip idle: as many as make narrow ones for the chip once where the table has room for short contexts only, fewer where
+// it has for long ones, over which wide ones read LDS less often (384, 512, 640 rows of 32 / 8 heads in fp16: narrow 14.2, 15.8, 23.4 us, wide 19.6, 22.5, 25.7; behind 1024 tokens 28, 32, 55 and 37, 39, 42;
+// behind 4096 72, 83, 130 and 62, 76, 87; 256 rows 11.7, 24.8, 51.0 and 17.2, 30.4, 57.7; heads of 64 and 8 bits alike).  The lengths are on the device: in a table with more room short contexts get what
+// suits long ones (384 and 512 rows in one for 131072 tokens 19.6 and 22.7 us).  Heads of 256 in fp16 have no registers for a narrow tile on its way (32 x 5 rows of
+// 4096: narrow 302 us, wide 275, with one fp16 a weight).
 constexpr int FEW_PAIRS = 64, FEW_TILES = 64, FEW_TILES_SHORT = 128, SHORT = 2048;
 
 bool takes_narrow(const PromptArgs& a)
