@@ -415,8 +415,8 @@ int eora_cache_attention(const void* q, const void* pages_k, const void* pages_v
  * eora_cache_append() into such a cache, the scales found as the tokens come: e is the least with max |x| <= 448 * 2^e over the block's finite values (at most
  * 8, at least -15).  A call that stores token 0 of a block begins it anew, from the values of this call alone; otherwise e only grows from what the block has,
  * and codes that are there already are rounded again, ties to even, to the new power (exact unless they become subnormal).  Stored is the nearest code of x / 2^e,
- * saturating at 448 (240 with e = 8); NaN is kept.  An infinity becomes the largest code, of the power that the block's finite values ask for: 448 * 2^e, no more than the largest magnitudes beside
- * it (2^-15 * 448 where a block that is begun has no finite value but 0).
+ * saturating at 448 (240 with e = 8); NaN is kept.  An infinity becomes the largest code at the power that the block's finite values ask for: less than twice the largest magnitude beside
+ * it, and 448 * 2^-15 where a block that is begun has no finite value but 0.
  * The rows of a call whose slots share a block lie among 16 consecutive rows (as the tokens of a request do that are given in order; rows that are not
  * stored may lie between).  Where they do not, the contents of that block, and its scales, are undefined.  Two rows with one slot: which is stored is undefined.
  * All else, and the errors, as for eora_cache_append() with cache_bits 8; bytes of scales need no alignment. */
@@ -438,7 +438,7 @@ int eora_cache_read(const void* pages_k, const void* pages_v, const void* k_scal
  * for query head i of kv head i / (n_heads / n_kv_heads) as in eora_cache_attention(), with pages, scores and lse as there.  A row that sees nothing (a position below 0, all
  * masked) has out = 0 and lse = -inf.  What a row does not see is never used for it, NaN and infinities included, also where other rows see it.
  * A value that is not finite makes its column of out infinite or NaN for the rows that see it (where its score is -inf, it may or may not).
- * A head's key scale that is not finite makes out and lse NaN for the rows that see a token, and so does a score that is 0 times an infinity (scale 0).
+ * A head's key scale that is NaN (with row_starts: or infinite) makes out and lse NaN for the rows that see a token, and so does a score that is 0 times an infinity (scale 0).
  * row_starts: B + 1 int32, not decreasing (where they decrease, out and lse are undefined, and the workspace's first 48 KiB have to be zeroed before the next call), taken as 0 .. M;
  * rows of no request are left as they were.  NULL: one row a request (M == B), the form for single tokens.
  * scale_block 0: k_scale, v_scale by head (cache_bits 8) or NULL (16); 16 (cache_bits 8 only): bytes by block, as eora_cache_append_blocks() writes them.
