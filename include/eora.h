@@ -415,8 +415,8 @@ int eora_cache_attention(const void* q, const void* pages_k, const void* pages_v
  * eora_cache_append() into such a cache, the scales found as the tokens come: e is the least with max |x| <= 448 * 2^e over the block's finite values (at most
  * 8, at least -15).  A call that stores token 0 of a block begins it anew, from the values of this call alone; otherwise e only grows from what the block has,
  * and codes that are there already are rounded again, ties to even, to the new power (exact unless they become subnormal).  Stored is the nearest code of x / 2^e,
- * saturating at 448 (240 with e = 8); NaN is kept.  An infinity becomes the largest code at the power that the block's finite values ask for: less than twice the largest magnitude beside
- * it, and 448 * 2^-15 where a block that is begun has no finite value but 0.
+ * saturating at 448 (240 with e = 8); NaN is kept.  An infinity becomes the largest code at the block's power, which is found without it
+ * (448 * 2^-15 where a block that is begun has no finite value but 0).
  * The rows of a call whose slots share a block lie among 16 consecutive rows (as the tokens of a request do that are given in order; rows that are not
  * stored may lie between).  Where they do not, the contents of that block, and its scales, are undefined.  Two rows with one slot: which is stored is undefined.
  * All else, and the errors, as for eora_cache_append() with cache_bits 8; bytes of scales need no alignment. */
